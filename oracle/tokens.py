@@ -1,0 +1,177 @@
+"""Plain float64 definitions of the token operators: which keys a query sees, attention and
+its gradients with bounds on what rounding may change, and the token cache's pages."""
+
+import numpy as np
+
+BF16 = 2.0 ** -8      # relative half step
+FP32 = 2.0 ** -24
+
+
+def sees(pos, keys, window=0, sinks=0):
+    """bool [queries, keys] from their positions."""
+    i, j = np.asarray(pos)[:, None], np.asarray(keys)[None, :]
+    near = (i - j < window) | (j < sinks) if window else np.ones((i.shape[0], j.shape[1]), bool)
+    return (j <= i) & near
+
+
+def tree_sees(held, bits, window=0, sinks=0):
+    """bool [nodes, held + nodes]: ``bits`` are the nodes that each node sees, as integers."""
+    n = len(bits)
+    node = np.array([[(int(b) >> t) & 1 for t in range(n)] for b in bits], bool).reshape(n, n)
+    pos = held + np.maximum(node.sum(1) - 1, 0)
+    return np.concatenate([sees(pos, np.arange(held), window, sinks), node], axis=1)
+
+
+def attend(q, k, v, see, scale):
+    """One sequence and head: q [n, D], k and v [m, D], see [n, m].  Returns o, lse, p."""
+    s = (q @ k.T) * scale
+    top = np.where(see, s, -np.inf).max(axis=1, initial=-np.inf)
+    e = np.where(see, np.exp(np.where(see, s, -np.inf) - np.where(np.isfinite(top), top, 0.0)[:, None]), 0.0)
+    total = e.sum(1)
+    p = e / np.where(total > 0, total, 1.0)[:, None]
+    with np.errstate(divide="ignore"):
+        lse = np.where(total > 0, np.log(total) + np.where(np.isfinite(top), top, 0.0), -np.inf)
+    return p @ v, lse, p
+
+
+def score_error(q, k, scale):
+    """What fp32 products and sums may change a score by: D products and sums, the scale, exp2's argument."""
+    size = float((np.abs(q) @ np.abs(k).T).max()) * scale
+    return (q.shape[1] + 8) * FP32 * max(size, 1.0)
+
+
+def attend_bound(q, k, v, p, o, scale):
+    """Elementwise bound on |O - exact|: each weight is off by a bf16 half step and by what its score is (twice, with
+    the sum's); sums over the keys in fp32; one rounding of O to bf16."""
+    weight = BF16 + 2 * score_error(q, k, scale) + (2 * k.shape[0] + 64) * FP32
+    a = (p @ np.abs(v)) * weight
+    return a + (np.abs(o) + a) * BF16 + 1e-30
+
+
+def lse_bound(q, k, lse, scale):
+    return score_error(q, k, scale) + (k.shape[0] + 64) * FP32 + 8 * FP32 * (1 + np.where(np.isfinite(lse), np.abs(lse), 0))
+
+
+def grads(q, k, v, do, see, scale):
+    """(dq, dk, dv) of one head and their bounds."""
+    o, _, p = attend(q, k, v, see, scale)
+    delta = (do * o).sum(1, keepdims=True)
+    dp = do @ v.T
+    ds = p * (dp - delta)
+    dq, dk, dv = scale * ds @ k, scale * ds.T @ q, p.T @ do
+    # P is rounded to bf16 (and off as its score is), dS formed from it and rounded again; delta comes from O rounded to
+    # bf16, whose own error is attend_bound's; sums in fp32; one rounding of the result to bf16
+    off = 2 * score_error(q, k, scale) + (2 * max(k.shape[0], q.shape[0]) + 64) * FP32
+    d_delta = (np.abs(do) * attend_bound(q, k, v, p, o, scale)).sum(1, keepdims=True)
+    d_dp = (np.abs(do) @ np.abs(v).T + np.abs(delta)) * (do.shape[1] + 8) * FP32
+    e_ds = np.abs(ds) * (2 * BF16 + BF16 ** 2 + off) + p * (d_delta + d_dp) * (1 + 2 * BF16)
+    e_p = p * (BF16 + off)
+    b_dq, b_dk, b_dv = scale * e_ds @ np.abs(k), scale * e_ds.T @ np.abs(q), e_p.T @ np.abs(do)
+    sums = (2 * max(k.shape[0], q.shape[0]) + 64) * FP32
+    return [(g, b + s * sums + (np.abs(g) + b) * BF16 + 1e-30)
+            for g, b, s in ((dq, b_dq, scale * np.abs(ds) @ np.abs(k)), (dk, b_dk, scale * np.abs(ds).T @ np.abs(q)),
+                            (dv, b_dv, p.T @ np.abs(do)))]
+
+
+class PageModel:
+    """Pages of a token cache, and which token (any value) lies where."""
+
+    IN_PLACE = 16
+
+    def __init__(self, n_pages, max_seqs, max_tokens, page):
+        self.T, self.n_pages, self.max_tokens = page, n_pages, max_tokens
+        self.uses = [0] * n_pages
+        self.table = [[] for _ in range(max_seqs)]
+        self.rows = [[] for _ in range(max_seqs)]      # the token at each position (None: no value)
+
+    def free_pages(self):
+        return self.uses.count(0)
+
+    def take(self):
+        p = self.uses.index(0)
+        self.uses[p] = 1
+        return p
+
+    def drop(self, pages):
+        for p in pages:
+            if p >= 0:
+                self.uses[p] -= 1
+
+    def extend(self, seqs, tokens):
+        """tokens[i]: the values that sequence seqs[i] grows by.  False (and nothing done) where pages do not suffice."""
+        before = (list(self.uses), [list(t) for t in self.table])
+        try:
+            for s, new in zip(seqs, tokens):
+                if len(self.rows[s]) + len(new) > self.max_tokens:
+                    raise ValueError
+                if new and len(self.rows[s]) % self.T and self.uses[self.table[s][-1]] > 1:
+                    old = self.table[s][-1]
+                    self.table[s][-1] = self.take()
+                    self.uses[old] -= 1
+                while len(self.table[s]) * self.T < len(self.rows[s]) + len(new):
+                    self.table[s].append(self.take())
+        except ValueError:
+            self.uses, self.table = before
+            return False
+        for s, new in zip(seqs, tokens):
+            self.rows[s] = self.rows[s] + list(new)
+        return True
+
+    def fork(self, src, dst):
+        for a, b in zip(src, dst):
+            self.table[b], self.rows[b] = list(self.table[a]), list(self.rows[a])
+            for p in self.table[b]:
+                if p >= 0:
+                    self.uses[p] += 1
+
+    def copy(self, src, dst):
+        if sum(p >= 0 for a in src for p in self.table[a]) > self.free_pages():
+            return False
+        for a, b in zip(src, dst):
+            self.table[b] = [-1 if p < 0 else self.take() for p in self.table[a]]
+            self.rows[b] = list(self.rows[a])
+        return True
+
+    def keep(self, seqs, starts, index):
+        """index[i]: the positions that sequence seqs[i] keeps behind its first starts[i] tokens."""
+        plan, need = [], 0
+        for s, start, idx in zip(seqs, starts, index):
+            first, end = start // self.T, -(-(start + len(idx)) // self.T)
+            fresh = len(idx) > self.IN_PLACE or (len(idx) > 0 and any(self.uses[p] > 1 for p in self.table[s][first:end]))
+            plan.append((s, start, idx, first, end, fresh))
+            need += end - first if fresh else 0
+        if need > self.free_pages():
+            return False
+        taken = [[self.take() for _ in range(end - first)] if fresh else None for _, _, _, first, end, fresh in plan]
+        for (s, start, idx, first, end, fresh), pages in zip(plan, taken):
+            old = self.table[s]
+            if fresh:
+                self.drop(old[first:])
+                self.table[s] = old[:first] + pages
+            else:
+                self.drop(old[end:])
+                self.table[s] = old[:end]
+            self.rows[s] = self.rows[s][:start] + [self.rows[s][i] if 0 <= i < len(self.rows[s]) else 0 for i in idx]
+        return True
+
+    def trim(self, seqs, window, sinks):
+        for s in seqs:
+            n = len(self.rows[s])
+            for p in range(len(self.table[s])):
+                if p * self.T >= sinks and (p + 1) * self.T <= n - window + 1 and self.table[s][p] >= 0:
+                    self.drop([self.table[s][p]])
+                    self.table[s][p] = -1
+
+    def free(self, seqs):
+        for s in seqs:
+            self.drop(self.table[s])
+            self.table[s], self.rows[s] = [], []
+
+    def pack(self):
+        used = self.n_pages - self.free_pages()
+        holes = [p for p in range(used) if self.uses[p] == 0]
+        to = dict(zip([p for p in range(used, self.n_pages) if self.uses[p]], holes))
+        for a, b in to.items():
+            self.uses[b], self.uses[a] = self.uses[a], 0
+        self.table = [[to.get(p, p) for p in t] for t in self.table]
+        return used

@@ -11,6 +11,11 @@ cache management (iii)), behind the C ABI of ``include/uf.h`` (``libuf.so``):
 
 ``_lib`` binds the entry points under the same names; ``KVWindow`` adds
 shape checks and torch-allocated buffers.
+
+The same at the granularity of tokens (``include/uft.h``, bound by ``_tokens``):
+``TokenCache``, a paged cache of keys and values with the attention that reads it
+(a sliding window with sinks, trees of drafted tokens), and ``window_attention``
+with its gradient for whole sequences.
 """
 
 from . import _lib
@@ -50,6 +55,7 @@ from ._lib import (
     uf_tile_lists_bytes,
     uf_tile_lists_layout,
 )
+from .tokens import TokenCache, window_attention, window_attention_bwd
 from .window import KVWindow
 
 __all__ = [
@@ -60,4 +66,5 @@ __all__ = [
     "uf_attn_bwd_work_bytes", "uf_attn_split_rows_work_bytes", "uf_attn_tail_plan",
     "uf_sparse_causal_attn_fwd_split_rows", "uf_sparse_causal_attn_bwd", "uf_sparse_causal_attn_bwd_noalloc", "uf_status_string",
     "uf_tile_lists_bytes", "uf_tile_lists_layout", "KVWindow",
+    "TokenCache", "window_attention", "window_attention_bwd",
 ]

@@ -1,0 +1,734 @@
+// Gradients of the attention of whole sequences under a sliding window with sinks.
+//
+// With p = exp(scale q.k - lse) over the keys that a query sees, delta = <dO, O> and
+// dS = p (dO.v - delta):
+//   dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K,
+// where the sums of dK and dV run over the queries of every head of the group.  Rows
+// are (token, head of the group) pairs, row = token * G + head, so that a key sees the
+// rows from key * G to (key + window) * G as one range and the heads add up by
+// themselves.
+//
+// Kernels, all with 32x32x16 bf16 MFMA and fp32 accumulation:
+//  * prep: records of 128 rows, Q and dO (zero where there is no row), then
+//    -LSE/scale (-inf there, so that their weights vanish) and -delta, which seed the
+//    S and dP accumulators;
+//  * dkdv: one workgroup of eight waves per 128 keys of a head.  Waves w and w + 4
+//    share 32 keys: wave w computes S = Q K^T and P, hands P to wave w + 4 through LDS
+//    and accumulates dV^T += dO^T P, while wave w + 4 computes dP = dO V^T and, one unit
+//    of 64 rows later, dS = P dP and dK^T += Q^T dS;
+//  * dq: one workgroup of four waves per record, two per CU: per 32 keys S^T = K Q^T,
+//    dP^T = V dO^T, dS^T, then dQ^T += K^T dS^T;
+//  * sum: where a key tile's rows were cut into parts (the sinks', which every later row
+//    sees), the parts' dK and dV in fp32, added in order.
+// The transposed operands come from row-major LDS tiles through transposing reads.
+// Every output row is owned by one workgroup and sums have one order: no atomics.
+#include <type_traits>
+
+#include "token_common.h"
+
+namespace uf {
+namespace tok {
+namespace {
+
+using namespace attn;
+
+constexpr int kT = 128;                        // rows of a record, keys of a dkdv tile
+constexpr uint32_t kTile = 32768;              // [128][128] bf16
+constexpr size_t kRecord = 2 * kTile + 1024;
+constexpr size_t kPartial = size_t(2) * kT * kD * 4;   // dV, dK of a part, fp32
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+
+__device__ inline float bf16f(uint32_t x) { return __uint_as_float(x << 16); }
+
+__device__ inline int length_of(const BwdArgs& a, int b) {
+  return a.lengths != nullptr ? min(max(((const const_i32*)a.lengths)[b], 0), a.tokens) : a.tokens;
+}
+
+// ---------------------------------------------------------------- prep ----
+//
+// HBM-bound: Q, dO and O are read once and a record written; 16 lanes hold a row's
+// chunks, so delta is formed from the chunks of the copy and added over them.
+__global__ __launch_bounds__(256) void prep_kernel(BwdArgs a) {
+  const int H = a.kv_heads, G = a.group;
+  const int tile = blockIdx.x % a.tiles;
+  const int bh = blockIdx.x / a.tiles;
+  const int h = bh % H, b = bh / H;
+  const int rows = length_of(a, b) * G;
+  uint8_t* rec = a.work + (size_t(bh) * a.tiles + tile) * kRecord;
+  float* nlse = reinterpret_cast<float*>(rec + 2 * kTile);
+  const int cc = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+  uint4 vq[8], vg[8], vo[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {                // every load before the first store
+    const int row = tile * kT + r0 + 16 * k;
+    vq[k] = vg[k] = vo[k] = make_uint4(0, 0, 0, 0);
+    if (row < rows) {
+      const int t = int(uint32_t(row) / uint32_t(G)), head = h * G + row - t * G;
+      const size_t off = ((size_t(b) * a.tokens + t) * a.q_heads + head) * kD + cc * 8;
+      vq[k] = *reinterpret_cast<const uint4*>(a.q + int64_t(b) * a.q_batch + int64_t(t) * a.q_token +
+                                              int64_t(head) * a.q_head + cc * 8);
+      vg[k] = *reinterpret_cast<const uint4*>(a.dout + off);
+      vo[k] = *reinterpret_cast<const uint4*>(a.o + off);
+    }
+  }
+  if (threadIdx.x < kT) {
+    const int row = tile * kT + threadIdx.x;
+    float nl = -INFINITY;
+    if (row < rows) {
+      const int t = int(uint32_t(row) / uint32_t(G)), head = h * G + row - t * G;
+      nl = -a.lse[(size_t(b) * a.q_heads + head) * a.tokens + t] / a.scale;
+    }
+    nlse[threadIdx.x] = nl;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = r0 + 16 * k, c = r * 16 + cc;
+    reinterpret_cast<uint4*>(rec)[c] = vq[k];
+    reinterpret_cast<uint4*>(rec + kTile)[c] = vg[k];
+    const uint32_t g[4] = {vg[k].x, vg[k].y, vg[k].z, vg[k].w}, o[4] = {vo[k].x, vo[k].y, vo[k].z, vo[k].w};
+    float dl = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      dl += bf16f(o[e] & 0xffffu) * bf16f(g[e] & 0xffffu) + bf16f(o[e] >> 16) * bf16f(g[e] >> 16);
+#pragma unroll
+    for (int s = 1; s < 16; s <<= 1) dl += __shfl_xor(dl, s, 16);
+    if (cc == 0) nlse[kT + r] = -dl;
+  }
+}
+
+// ---------------------------------------------------------------- dkdv ----
+
+// LDS layout of rows of 128 dimensions: 16-byte chunk c of row r sits at position
+// perm(c) ^ f(r) of the row, perm swapping bits 1 and 3 of c and f(r) =
+// (r3, r1, r0, r2 ^ r3): row reads and transposing reads are free of bank conflicts.
+__device__ inline int swz_perm(int c) { return (c & ~10) | ((c & 2) << 2) | ((c & 8) >> 2); }
+__device__ inline int swz_f(int r) { return (r & 8) | ((r & 3) << 1) | (((r >> 2) ^ (r >> 3)) & 1); }
+__device__ inline uint32_t swz_elem(int r, int c) {
+  return uint32_t(r * 256 + ((swz_perm(c >> 3) ^ swz_f(r & 15)) << 4) + (c & 7) * 2);
+}
+
+// dma16 of the lanes in `mask` only (the whole wave is active around it).
+__device__ inline void dma16_low(const void* base, uint32_t off, uint32_t lds, uint64_t mask) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1"
+               : : "v"(off), "s"(base), "s"(lds), "s"(mask) : "memory");
+}
+
+// The key tiles' part of the launch: tiles 0 .. split-1 are cut into up to `parts` parts
+// of `part_units` units, the others are whole.
+struct Cut {
+  int32_t tiles, split, parts, part_units;
+};
+// Units (64 rows) of a sequence of `len` tokens that see keys of [k0, k0 + 128): first, end.
+__host__ __device__ inline void unit_range(int len, int G, int k0, int window, int sinks, int* first, int* end) {
+  const int64_t keys_end = k0 + kT < len ? k0 + kT : len;
+  int64_t last = int64_t(len);                 // tokens k0 .. last-1
+  if (window > 0 && k0 >= sinks && keys_end - 1 + window < last) last = keys_end - 1 + window;
+  *first = int(int64_t(k0) * G / 64);
+  *end = k0 < len ? int((last * G + 63) / 64) : *first;
+}
+
+// What bounds it: four products per pair on the matrix cores.  Phase s is unit s for
+// group 0 and for group 1's dP, unit s-1 for group 1's dS and dK, one workgroup barrier
+// after it.  Q rows live in a ring of four units, dO rows in a ring of three, so that a
+// unit is requested two phases before it is used.
+constexpr int kQRing = 4, kORing = 3, kLRing = 4;
+constexpr int kAhead = 4;                      // operands in flight ahead of their product
+constexpr int kKW = 4, W = 8, UQ = 64, NB = 2; // key blocks; waves; rows and 32-row blocks of a unit
+constexpr uint32_t UB = UQ * 256;              // bytes of a unit's Q (or dO) rows
+constexpr int kCopies = UB / 1024 / W;         // copies of a wave per unit and operand
+
+__global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float* partials) {
+  __shared__ uint4 sQ[kQRing][UQ * 16];
+  __shared__ uint4 sO[kORing][UQ * 16];
+  __shared__ uint4 sP[2][kKW][NB * 2][64];     // P operands of a unit: [parity][wave pair][block, kk][lane]
+  __shared__ float sLD[kLRing][2 * kT];        // the record's -LSE/scale, then -delta, per unit
+
+  const int H = a.kv_heads, G = a.group, BH = a.batch * H;
+  const int bh = blockIdx.x % BH;
+  const int item = blockIdx.x / BH;            // the parts of tile 0, of tile 1, ..., then whole tiles
+  const bool splits = item < cut.split * cut.parts;
+  const int t = splits ? item / cut.parts : item - cut.split * (cut.parts - 1);
+  const int part = splits ? item % cut.parts : 0;
+  const int h = bh % H, b = bh / H;
+  const int len = length_of(a, b);
+  int first, end;
+  unit_range(len, G, t * kT, a.window, a.sinks, &first, &end);
+  bool whole = true;
+  if (splits && end - first > cut.part_units) {
+    whole = false;
+    first += part * cut.part_units;
+    end = min(end, first + cut.part_units);
+    if (first >= end) return;
+  } else if (part > 0) {
+    return;
+  }
+  const int U = end - first;
+
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = wave / kKW, kw = wave % kKW;
+  const int lane = tid & 63, hl = lane >> 5, ln = lane & 31, rp = lane & 15, gg = (lane >> 4) & 1;
+  const int key = t * kT + kw * 32 + ln;       // this lane's key (result column)
+  const bool key_ok = key < len;
+  const uint8_t* qbase = a.work + size_t(bh) * a.tiles * kRecord;
+
+  bf16x8 bop[8];                               // B operands of the wave's keys: K (group 0) or V rows
+  {
+    const uint16_t* p = grp == 0 ? a.k + int64_t(b) * a.k_batch + int64_t(h) * a.k_head + int64_t(key_ok ? key : 0) * a.k_token
+                                 : a.v + int64_t(b) * a.v_batch + int64_t(h) * a.v_head + int64_t(key_ok ? key : 0) * a.v_token;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (key_ok) u = *reinterpret_cast<const uint4*>(p + 16 * ks + 8 * hl);
+      bop[ks] = as_bf16x8(u);
+    }
+  }
+  // rows that see the lane's key: [row_lo, row_hi); of the wave's keys, rows that see them all
+  const int row_lo = int(min(int64_t(key) * G, int64_t(INT32_MAX)));
+  const bool forever = a.window == 0 || key < a.sinks;
+  const int row_hi = forever ? INT32_MAX : int(min((int64_t(key) + a.window) * G, int64_t(INT32_MAX)));
+  const int k_first = t * kT + kw * 32;
+  const int64_t all_lo = int64_t(k_first + 31) * G;
+  const int64_t all_hi = a.window == 0 || k_first + 31 < a.sinks ? INT64_MAX : (int64_t(k_first) + a.window) * G;
+
+  // Copies of a unit: Q and dO rows, and the record's per-row values.  Copy i of wave w
+  // fills LDS chunks [64*(W i + w), +64), rows 4(W i + w) + lane/16, whose low four
+  // bits do not depend on i.
+  uint32_t voff;
+  {
+    const int r = 4 * wave + (lane >> 4);
+    voff = uint32_t(r * 256 + swz_perm((lane & 15) ^ swz_f(r & 15)) * 16);
+  }
+  const uint32_t lq0 = lds_addr(&sQ[0][0]), lo0 = lds_addr(&sO[0][0]), ll0 = lds_addr(&sLD[0][0]);
+  struct Source {
+    const uint8_t* rec;
+    uint32_t half, qslot, oslot;
+  };
+  // Past the end the last unit is copied again, into a slot that nothing reads any more.
+  auto source = [&](int s, uint32_t qslot, uint32_t oslot) {
+    const uint32_t u = uint32_t(first + min(s, U - 1));
+    return Source{qbase + size_t(u >> 1) * kRecord, (u & 1) * UB, qslot, oslot};
+  };
+  constexpr int kIssue = 2 * kCopies + 1;      // copies of a wave per unit
+  auto issue = [&](const Source& c, int k) {
+    if (k == 2 * kCopies) {
+      constexpr uint32_t share = 2 * kT * 4 / W;
+      dma16_low(c.rec + 2 * kTile + uint32_t(wave) * share, uint32_t(lane) * 16u,
+                ll0 + c.qslot * uint32_t(sizeof(sLD[0])) + uint32_t(wave) * share, (uint64_t(1) << (share / 16)) - 1);
+      return;
+    }
+    const uint32_t at = uint32_t(k >> 1) * W * 1024u;
+    dma16(c.rec + (k & 1) * kTile + c.half + at, voff,
+          ((k & 1) ? lo0 + c.oslot * UB : lq0 + c.qslot * UB) + uint32_t(wave) * 1024u + at);
+  };
+  auto issue_all = [&](const Source& c) {
+#pragma unroll
+    for (int k = 0; k < kIssue; ++k) issue(c, k);
+  };
+
+  f32x16 acc[4];                               // dV^T (group 0) or dK^T (group 1): [dim block][32 dims x 32 keys]
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) acc[mb] = f32x16{};
+  const float c2 = a.scale_log2;
+  const float pad = key_ok ? 0.f : -INFINITY;  // keys that are none weigh nothing
+  uint4* const pslot = &sP[0][kw][0][lane];
+  constexpr uint32_t kPStep = sizeof(sP[0]) / 16;
+  // Operand addresses within the current ring slots, advanced once per phase: tr,
+  // transposing reads (k-slot kappa = row 16 kk + swap23(kappa)) of dO (group 0) or Q
+  // (group 1); rt, row reads of Q (group 0) or dO (group 1).
+  uint32_t tr[2][4], rt[8];
+  {
+    const uint32_t bt = grp == 0 ? lo0 : lq0, br = grp == 0 ? lq0 : lo0;
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb)
+        tr[hh][cb] = bt + swz_elem(8 * hh + 4 * hl + (rp >> 2), 32 * cb + 16 * gg + 4 * (rp & 3));
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) rt[ks] = br + swz_elem(ln, 16 * ks + 8 * hl);
+  }
+  const uint32_t ld0 = ll0 + uint32_t(16 * hl + (grp == 0 ? 0 : 4 * kT));
+
+  // A unit's products of one wave: 16 row products (X K^T or X V^T), then 16 transposed
+  // ones (acc^T += X^T op).  Product i and its operand, read kAhead products earlier.
+  constexpr int kRows = 8 * NB, kAll = 16 * NB;
+  auto load = [&](int i) -> bf16x8 {
+    if (i < kRows) return lds_row(rt[i & 7] + uint32_t((i >> 3) * 32 * 256));
+    const int k = i - kRows;
+    const uint32_t at = uint32_t(16 * (k >> 2) * 256);
+    return lds_tr2(tr[0][k & 3] + at, tr[1][k & 3] + at);
+  };
+  auto row_product = [&](int i, const bf16x8& x, f32x16 (&v)[NB]) {
+    v[i >> 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, bop[i & 7], v[i >> 3], 0, 0, 0);
+  };
+  auto tr_product = [&](int i, const bf16x8& x, const bf16x8 (&op)[NB][2]) {
+    const int k = i - kRows, mb = k & 3;
+    acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, op[k >> 3][(k >> 2) & 1], acc[mb], 0, 0, 0);
+  };
+  auto seed = [&](uint32_t ld, f32x16 (&v)[NB]) {
+#pragma unroll
+    for (int qb = 0; qb < NB; ++qb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 c4 = *(const lds_f32x4*)(uintptr_t)(ld + uint32_t(4 * (qb * 32 + 8 * g)));
+        v[qb][4 * g] = c4.x;
+        v[qb][4 * g + 1] = c4.y;
+        v[qb][4 * g + 2] = c4.z;
+        v[qb][4 * g + 3] = c4.w;
+      }
+  };
+  auto put = [&](bf16x8 (&op)[2], int e, float x0, float x1) {
+    op[e >> 2][2 * (e & 3)] = (__bf16)x0;
+    op[e >> 2][2 * (e & 3) + 1] = (__bf16)x1;
+  };
+  auto advance = [&](bool wrap, int ring) {
+    const uint32_t d = wrap ? uint32_t(-(ring - 1) * int(UB)) : UB;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) rt[k] += d;
+  };
+  auto advance_tr = [&](bool wrap, int ring) {
+    const uint32_t d = wrap ? uint32_t(-(ring - 1) * int(UB)) : UB;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) tr[k][cb] += d;
+  };
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  constexpr int kGap = kAll / kIssue;          // products between two of the next unit's copies
+  // Group 0, unit at row `row`: S, P, the P slot, dV.
+  auto unit0 = [&](int row, uint32_t ld, uint32_t par, const Source& next) {
+    f32x16 sv[NB];
+    bf16x8 op[NB][2], x[kAll];
+    seed(ld, sv);
+    const bool full = row >= all_lo && row + UQ <= all_hi;
+    uint64_t see = 0;
+    if (!full) see = (bits_upto(row_hi - row) & ~bits_upto(row_lo - row)) >> (4 * hl);
+    auto mask = [&](int qb) {
+      if (full) return;
+      const uint32_t w = uint32_t(see >> (32 * qb));
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (!((w >> (8 * (r >> 2) + (r & 3))) & 1u)) sv[qb][r] = -INFINITY;
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) x[i] = load(i);
+    auto weights = [&](int qb, int e) {
+      put(op[qb], e, __builtin_amdgcn_exp2f(__builtin_fmaf(sv[qb][2 * e], c2, pad)),
+          __builtin_amdgcn_exp2f(__builtin_fmaf(sv[qb][2 * e + 1], c2, pad)));
+      if ((e & 3) == 3) pslot[par * kPStep + (qb * 2 + (e >> 2)) * 64] = __builtin_bit_cast(uint4, op[qb][e >> 2]);
+    };
+    fence();
+#pragma unroll
+    for (int i = 0; i < kAll; ++i) {
+      if (i == 8) mask(0);
+      if (i == 16) mask(1);
+      if (i < kRows) row_product(i, x[i], sv);
+      else tr_product(i, x[i], op);
+      if (i + kAhead < kAll) x[i + kAhead] = load(i + kAhead);
+      if (i >= 8 && i < kAll - 8) weights((i - 8) >> 3, i & 7);
+      if (i % kGap == kGap - 1 && i / kGap < kIssue) issue(next, i / kGap);
+      fence();
+    }
+  };
+  // Group 1: dP - delta of a unit (kDp) into nv, and dS (from the P slot and the dP of
+  // the unit before, ov) and dK of that unit (kDk).
+  auto unit1 = [&](auto dp, auto dk, uint32_t ld, uint32_t par, const f32x16 (&ov)[NB], f32x16 (&nv)[NB],
+                   const Source& next) {
+    constexpr bool kDp = decltype(dp)::value, kDk = decltype(dk)::value;
+    constexpr int i0 = kDp ? 0 : kRows, i1 = kDk ? kAll : kRows;
+    bf16x8 pk[NB][2], op[NB][2], x[kAll];
+    if (kDk) {
+#pragma unroll
+      for (int qb = 0; qb < NB; ++qb)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+          pk[qb][kk] = __builtin_bit_cast(bf16x8, pslot[par * kPStep + (qb * 2 + kk) * 64]);
+    }
+    if (kDp) seed(ld, nv);
+#pragma unroll
+    for (int i = i0; i < i0 + kAhead; ++i) x[i] = load(i);
+    auto ds = [&](int qb, int e) {
+      put(op[qb], e, float(pk[qb][e >> 2][2 * (e & 3)]) * ov[qb][2 * e],
+          float(pk[qb][e >> 2][2 * (e & 3) + 1]) * ov[qb][2 * e + 1]);
+    };
+    fence();
+    if (kDk && !kDp) {
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) ds(k >> 3, k & 7);
+    }
+#pragma unroll
+    for (int i = i0; i < i1; ++i) {
+      if (i < kRows) row_product(i, x[i], nv);
+      else tr_product(i, x[i], op);
+      if (i + kAhead < i1) x[i + kAhead] = load(i + kAhead);
+      if (kDk && i < kRows) ds(i >> 3, i & 7);
+      if (kDp && kDk && i % kGap == kGap - 1 && i / kGap < kIssue) issue(next, i / kGap);
+      fence();
+    }
+  };
+  auto run = [&](auto group) {
+    constexpr int G0 = decltype(group)::value;
+    f32x16 dpv[NB];
+    uint32_t om = 0;                           // s % 3
+    auto phase = [&](int s, auto start) {
+      constexpr bool kFirst = decltype(start)::value;
+      // unit s has landed; the slots of unit s+2 are free
+      const Source next = source(s + 2, uint32_t(s + 2) & 3u, om == 0 ? 2u : om - 1u);
+      const uint32_t ld = ld0 + (uint32_t(s) & 3u) * uint32_t(sizeof(sLD[0])) + uint32_t((first + s) & 1) * uint32_t(4 * UQ);
+      if constexpr (G0 == 0) {
+        unit0((first + s) * UQ, ld, uint32_t(s) & 1u, next);
+        advance((s & 3) == 3, kQRing);
+        advance_tr(om == 2, kORing);
+      } else {
+        f32x16 nv[NB];
+        if constexpr (kFirst) issue_all(next);
+        unit1(std::true_type{}, std::bool_constant<!kFirst>{}, ld, uint32_t(s - 1) & 1u, dpv, nv, next);
+#pragma unroll
+        for (int qb = 0; qb < NB; ++qb) dpv[qb] = nv[qb];
+        if constexpr (!kFirst) advance_tr((s & 3) == 0, kQRing);
+        advance(om == 2, kORing);
+      }
+      om = om == 2 ? 0 : om + 1;
+      meet<kIssue>();                          // unit s+1 has landed; unit s+2 may be in flight
+    };
+    meet<kIssue>();                            // unit 0 has landed, unit 1 may be in flight
+    phase(0, std::true_type{});
+    for (int s = 1; s < U; ++s) phase(s, std::false_type{});
+    if constexpr (G0 == 1) {
+      f32x16 nv[NB];
+      unit1(std::false_type{}, std::true_type{}, 0, uint32_t(U - 1) & 1u, dpv, nv, Source{});
+    }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0)); // no copy outlives the workgroup
+  };
+  if (U > 0) {
+    issue_all(source(0, 0, 0));
+    issue_all(source(1, 1, 1));
+    if (grp == 0) run(std::integral_constant<int, 0>{});
+    else run(std::integral_constant<int, 1>{});
+  }
+
+  // lane holds key `key`, dims mb*32 + 8*(r/4) + 4*hl + r%4
+  if (!whole) {
+    float* dst = partials + (((size_t(bh) * cut.split + t) * cut.parts + part) * 2 + grp) * (kT * kD) + (kw * 32 + ln) * kD;
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(dst + mb * 32 + 8 * g + 4 * hl) =
+            make_float4(acc[mb][4 * g], acc[mb][4 * g + 1], acc[mb][4 * g + 2], acc[mb][4 * g + 3]);
+    return;
+  }
+  if (key < a.tokens) {
+    uint16_t* dst = (grp ? a.dk : a.dv) + ((size_t(b) * a.tokens + key) * H + h) * kD + 4 * hl;
+    const float f = grp ? a.scale : 1.0f;
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        uint2 u = make_uint2(0, 0);
+        if (key_ok) {
+          u.x = pack_bf16x2(acc[mb][4 * g] * f, acc[mb][4 * g + 1] * f);
+          u.y = pack_bf16x2(acc[mb][4 * g + 2] * f, acc[mb][4 * g + 3] * f);
+        }
+        *reinterpret_cast<uint2*>(dst + mb * 32 + 8 * g) = u;
+      }
+  }
+}
+
+// The parts of a cut tile: a thread adds four dims of one key of dK or dV, part by part.
+__global__ __launch_bounds__(256) void sum_kernel(BwdArgs a, Cut cut, const float* partials) {
+  const int H = a.kv_heads;
+  const int rows = blockIdx.x * 8;                     // rows (bh, tile, kind, key), eight a workgroup
+  const int r = rows + (threadIdx.x >> 5), c = (threadIdx.x & 31) * 4;
+  const int k = r % kT, grp = (r / kT) & 1, bt = r / (2 * kT);
+  const int t = bt % cut.split, bh = bt / cut.split, h = bh % H, b = bh / H;
+  const int len = length_of(a, b), key = t * kT + k;
+  int first, end;
+  unit_range(len, a.group, t * kT, a.window, a.sinks, &first, &end);
+  if (end - first <= cut.part_units || key >= a.tokens) return;
+  const int n = (end - first + cut.part_units - 1) / cut.part_units;
+  const float* src = partials + ((size_t(bt) * cut.parts) * 2 + grp) * (kT * kD) + k * kD + c;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p0 = 0; p0 < n; p0 += 4) {
+    float4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float4*>(src + size_t(min(p0 + i, n - 1)) * 2 * (kT * kD));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float on = p0 + i < n ? 1.f : 0.f;
+      s.x = __builtin_fmaf(v[i].x, on, s.x);
+      s.y = __builtin_fmaf(v[i].y, on, s.y);
+      s.z = __builtin_fmaf(v[i].z, on, s.z);
+      s.w = __builtin_fmaf(v[i].w, on, s.w);
+    }
+  }
+  const float f = key < len ? (grp ? a.scale : 1.0f) : 0.f;
+  uint2 u;
+  u.x = pack_bf16x2(s.x * f, s.y * f);
+  u.y = pack_bf16x2(s.z * f, s.w * f);
+  *reinterpret_cast<uint2*>((grp ? a.dk : a.dv) + ((size_t(b) * a.tokens + key) * H + h) * kD + c) = u;
+}
+
+// ------------------------------------------------------------------ dq ----
+//
+// The walk, the unit's layout and its copies are the forward's (token_attn.hip).  What
+// bounds it: three products per pair on the matrix cores.
+constexpr uint32_t kUnitBytes = 32768;
+
+__global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
+  __shared__ uint4 sbuf[2][kUnitBytes / 16];
+
+  const int H = a.kv_heads, G = a.group, BH = a.batch * H;
+  const int bh = blockIdx.x % BH;
+  const int tile = a.tiles - 1 - blockIdx.x / BH;      // long ranges first
+  const int h = bh % H, b = bh / H;
+  const int len = length_of(a, b), rows = len * G, row0 = tile * kT;
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, hl = lane >> 5, ln = lane & 31, rp = lane & 15, g = (lane >> 4) & 1;
+  const int q = wave * 32 + ln, row = row0 + q;
+  const int token = int(uint32_t(row) / uint32_t(G)), head = h * G + row - token * G;
+  const bool stored = row < a.tokens * G;
+  uint16_t* const dst = a.dq + ((size_t(b) * a.tokens + token) * a.q_heads + head) * kD + 4 * hl;
+  if (row0 >= rows) {                                  // padding
+    if (stored)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) *reinterpret_cast<uint2*>(dst + 8 * i) = make_uint2(0, 0);
+    return;
+  }
+  const int first = row0 / G, last = (min(row0 + kT, rows) - 1) / G;
+  const Range range = key_range(first, last, a.window, a.sinks, kKeyUnit);
+  const int w0 = row0 + wave * 32;
+  const bool idle = w0 >= rows;
+  const int pmin = w0 / G, pmax = (min(w0 + 32, rows) - 1) / G;
+  const int pos = min(token, pmax);
+
+  const uint8_t* rec = a.work + (size_t(bh) * a.tiles + tile) * kRecord;
+  bf16x8 qf[8], of[8];
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) {
+    qf[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(rec + size_t(q) * 256 + (2 * ks + hl) * 16));
+    of[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(rec + kTile + size_t(q) * 256 + (2 * ks + hl) * 16));
+  }
+  const float c2 = a.scale_log2;
+  const float nl = reinterpret_cast<const float*>(rec + 2 * kTile)[q] * c2;
+  const float nd = reinterpret_cast<const float*>(rec + 2 * kTile)[kT + q];
+  f32x16 negd;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) negd[r] = nd;
+
+  const uint32_t lds0 = lds_addr(&sbuf[0][0]);
+  uint32_t kr[4], kt[2][2];                            // K rows (V rows 16 KB behind); K transposed
+#pragma unroll
+  for (int k = 0; k < 4; ++k) kr[k] = lds0 + uint32_t(ln * 128 + 16 * ((2 * k + hl) ^ swz_k(ln & 15)));
+#pragma unroll
+  for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int r = 8 * hh + 4 * hl + (rp >> 2);
+      kt[hh][m] = lds0 + uint32_t(r * 128 + 16 * ((4 * m + 2 * g + ((rp >> 1) & 1)) ^ swz_k(r)) + 8 * (rp & 1));
+    }
+  struct Unit {
+    const uint8_t *k, *v;
+    int key0;
+  };
+  const uint32_t kstep = uint32_t(a.k_token) * 2, vstep = uint32_t(a.v_token) * 2;
+  auto unit_of = [&](int u) {
+    Unit x;
+    x.key0 = (u < range.sink ? u : u - range.sink + range.from) * kKeyUnit;
+    x.k = reinterpret_cast<const uint8_t*>(a.k + int64_t(b) * a.k_batch + int64_t(x.key0) * a.k_token + int64_t(h) * a.k_head);
+    x.v = reinterpret_cast<const uint8_t*>(a.v + int64_t(b) * a.v_batch + int64_t(x.key0) * a.v_token + int64_t(h) * a.v_head);
+    return x;
+  };
+  const uint32_t chunk = uint32_t(16 * ((lane & 7) ^ swz_k(8 * (wave & 1) + (lane >> 3))));
+  struct Offsets {
+    uint32_t k[2], v[2];
+  };
+  auto offsets = [&](const Unit& u) {
+    Offsets o;
+    const bool sink = u.key0 < range.from * kKeyUnit;
+    const int top = sink ? min(63, a.sinks - 1 - u.key0) : min(63, last - u.key0);
+    const int low = sink ? 0 : range.low - u.key0, srel = a.sinks - u.key0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      int r = 8 * (wave + 4 * t) + (lane >> 3);
+      r = min(r < srel ? r : max(r, low), top);
+      o.k[t] = uint32_t(r) * kstep + chunk;
+      o.v[t] = uint32_t(r) * vstep + chunk;
+    }
+    return o;
+  };
+  auto issue = [&](const Unit& u, const Offsets& o, uint32_t buf, int k) {
+    const int t = k & 3;
+    const uint32_t to = lds0 + buf * kUnitBytes + uint32_t(wave) * 1024u + uint32_t(t) * 4096u;
+    if (k < 4)
+      dma16(u.k + (t >> 1) * 128, o.k[t & 1], to);
+    else
+      dma16(u.v + (t >> 1) * 128, o.v[t & 1], to + 16384u);
+  };
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+
+  f32x16 dqt[4];                                       // [4 dim blocks][32 dims x 32 rows]
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) dqt[mb] = f32x16{};
+
+  // Products of a unit: S0, dP0, S1, dP1, dQ0, dQ1 (eight each, per 32-key block).
+  constexpr int kSP = 32, kReads = 4;
+  auto load = [&](int k) -> bf16x8 {
+    if (k < kSP) {
+      const int n = k >> 4, ks = k & 7;
+      return lds_row(kr[ks & 3] + uint32_t(n * 4096 + (ks >> 2) * 8192 + ((k & 8) ? 16384 : 0)));
+    }
+    const int m = k - kSP, n = m >> 3, kk = (m >> 2) & 1, mb = m & 3;
+    const uint32_t at = uint32_t(n * 4096 + kk * 2048 + (mb >> 1) * 8192);
+    return lds_tr2(kt[0][mb & 1] + at, kt[1][mb & 1] + at);
+  };
+  auto body = [&](const Unit& cur, const Unit& next, uint32_t nbuf) {
+    f32x16 sv[2], dp[2];
+    bf16x8 op[2][2], x[48];
+    const Offsets no = offsets(next);
+    const bool full = cur.key0 + 63 <= pmin &&
+                      (a.window == 0 || cur.key0 >= pmax - a.window + 1 || cur.key0 + 63 < a.sinks);
+    uint64_t see = 0;
+    if (!full) see = seen_bits(pos, cur.key0, a.window, a.sinks) >> (4 * hl);
+    auto mask = [&](int n) {
+      if (full) return;
+      const uint32_t w = uint32_t(see >> (32 * n));
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (!((w >> (8 * (r >> 2) + (r & 3))) & 1u)) sv[n][r] = -INFINITY;
+    };
+    auto weight = [&](int n, int r) { sv[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[n][r], c2, nl)); };
+    auto ds = [&](int n, int e) {
+      op[n][e >> 2][2 * (e & 3)] = (__bf16)(sv[n][2 * e] * dp[n][2 * e]);
+      op[n][e >> 2][2 * (e & 3) + 1] = (__bf16)(sv[n][2 * e + 1] * dp[n][2 * e + 1]);
+    };
+#pragma unroll
+    for (int k = 0; k < kReads; ++k) x[k] = load(k);
+    fence();
+    auto eight = [&](auto from) {                      // products from .. from + 7
+      constexpr int k0 = decltype(from)::value;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int k = k0 + j;
+        if constexpr (k0 < kSP) {
+          const int n = k0 >> 4;
+          if constexpr ((k0 & 8) == 0)
+            sv[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[k], qf[j], j ? sv[n] : f32x16{}, 0, 0, 0);
+          else
+            dp[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[k], of[j], j ? dp[n] : negd, 0, 0, 0);
+        } else {
+          dqt[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[k], op[(k0 - kSP) >> 3][j >> 2], dqt[j & 3], 0, 0, 0);
+        }
+        if (k + kReads < 48) x[k + kReads] = load(k + kReads);
+        if constexpr (k0 < kSP && (k0 & 8) != 0) {     // beside dP of a block: its weights
+          weight(k0 >> 4, 2 * j);
+          weight(k0 >> 4, 2 * j + 1);
+        }
+        if constexpr (k0 == 16) ds(0, j);              // beside S of block 1
+        if constexpr (k0 == 32) ds(1, j);              // beside dQ of block 0
+        if (k % 2 == 1 && k < 16) issue(next, no, nbuf, k >> 1);
+        fence();
+      }
+      if constexpr (k0 < kSP && (k0 & 8) != 0) asm volatile("" : "+v"(sv[k0 >> 4]));
+      if constexpr (k0 == 16) asm volatile("" : "+v"(op[0][0]), "+v"(op[0][1]));
+    };
+    eight(std::integral_constant<int, 0>{});
+    mask(0);
+    eight(std::integral_constant<int, 8>{});
+    eight(std::integral_constant<int, 16>{});
+    mask(1);
+    eight(std::integral_constant<int, 24>{});
+    eight(std::integral_constant<int, 32>{});
+    eight(std::integral_constant<int, 40>{});
+  };
+  auto unseen = [&](const Unit& u) {
+    return idle || u.key0 > pmax || (a.window > 0 && u.key0 + 63 < pmin - a.window + 1 && u.key0 >= a.sinks);
+  };
+  const int U = range.count;
+  Unit cur = unit_of(0), next = unit_of(min(1, U - 1));
+  {
+    const Offsets co = offsets(cur);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) issue(cur, co, 0, k);
+  }
+  for (int u = 0; u < U; ++u) {
+    meet<0>();                                         // unit u has landed; the other buffer is free
+    const uint32_t nbuf = uint32_t(u + 1) & 1u;
+    if (!unseen(cur)) {
+      body(cur, next, nbuf);
+    } else {
+      const Offsets no = offsets(next);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) issue(next, no, nbuf, k);
+    }
+    const uint32_t d = (u & 1) ? uint32_t(-int(kUnitBytes)) : kUnitBytes;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) kr[k] += d;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) kt[k >> 1][k & 1] += d;
+    cur = next;
+    next = unit_of(min(u + 2, U - 1));
+  }
+  meet<0>();                                           // no copy outlives the workgroup
+  if (!stored) return;
+  const float f = row < rows ? a.scale : 0.f;          // (padding accumulated zeros)
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint2 u;
+      u.x = pack_bf16x2(dqt[mb][4 * k] * f, dqt[mb][4 * k + 1] * f);
+      u.y = pack_bf16x2(dqt[mb][4 * k + 2] * f, dqt[mb][4 * k + 3] * f);
+      *reinterpret_cast<uint2*>(dst + mb * 32 + 8 * k) = u;
+    }
+}
+
+// The sinks' key tiles are cut into parts of about a window tile's units, so that none
+// outlasts the launch: a tile of the window is seen by (window + 127) G / 64 units, the
+// sinks' by every unit behind them.
+Cut cut_of(const BwdArgs& a) {
+  Cut c{};
+  c.tiles = (a.tokens + kT - 1) / kT;
+  c.parts = 1;
+  if (a.window == 0 || a.sinks == 0) return c;
+  int first, end;
+  unit_range(a.tokens, a.group, 0, a.window, a.sinks, &first, &end);
+  const int64_t near = (int64_t(a.window) + kT) * a.group / 64 + 1;
+  if (end - first <= 2 * near) return c;
+  c.split = (a.sinks + kT - 1) / kT < c.tiles ? (a.sinks + kT - 1) / kT : c.tiles;
+  const int64_t least = (end - first + 63) / 64;       // 64 parts at most
+  c.part_units = int(near > least ? near : least);
+  c.parts = (end - first + c.part_units - 1) / c.part_units;
+  return c;
+}
+size_t record_bytes(const BwdArgs& a) { return size_t(a.batch) * a.kv_heads * a.tiles * kRecord; }
+
+}  // namespace
+
+size_t bwd_work_bytes(const BwdArgs& a) {
+  const Cut c = cut_of(a);
+  return record_bytes(a) + size_t(a.batch) * a.kv_heads * c.split * c.parts * kPartial;
+}
+
+hipError_t launch_window_bwd(const BwdArgs& a, hipStream_t stream) {
+  const Cut c = cut_of(a);
+  const unsigned BH = unsigned(a.batch) * unsigned(a.kv_heads);
+  float* partials = reinterpret_cast<float*>(a.work + record_bytes(a));
+  prep_kernel<<<BH * unsigned(a.tiles), 256, 0, stream>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  dkdv_kernel<<<BH * unsigned(c.split * c.parts + c.tiles - c.split), 512, 0, stream>>>(a, c, partials);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (c.split > 0) {
+    sum_kernel<<<BH * unsigned(c.split) * 32u, 256, 0, stream>>>(a, c, partials);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  dq_kernel<<<BH * unsigned(a.tiles), 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace tok
+}  // namespace uf

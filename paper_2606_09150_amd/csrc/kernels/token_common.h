@@ -1,0 +1,69 @@
+// Device helpers shared by the token attention kernels (gfx950).
+#pragma once
+
+#include "../launch_tokens.h"
+#include "attn_common.h"
+
+namespace uf {
+namespace tok {
+
+using attn::bf16x2;
+using attn::bf16x8;
+using attn::f32x16;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+
+__device__ inline bf16x8 lds_row(uint32_t at) {            // 16 bytes of a row
+  return __builtin_bit_cast(bf16x8, *(const lds_u32x4*)(uintptr_t)at);
+}
+__device__ inline v4i16 lds_tr(uint32_t at) {              // transposing read
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(uintptr_t)at);
+}
+__device__ inline bf16x8 lds_tr2(uint32_t lo, uint32_t hi) {
+  const v4i16 v[2] = {lds_tr(lo), lds_tr(hi)};
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+// Rows of 64 dimensions in LDS: 128 bytes, 16-byte chunk c of row r at c ^ swz_k(r % 16).
+// Row reads (sixteen consecutive rows, one chunk) and transposing reads (four
+// consecutive rows, 64 bytes of each) touch every bank once.
+__device__ inline int swz_k(int r) { return ((r & 2) << 1) | (((r >> 1) ^ (r << 1)) & 2) | ((r >> 3) & 1); }
+
+// Bits of the 64 keys from `key0` on that a query at position `pos` sees.
+__device__ inline uint64_t bits_upto(int n) {              // bits 0 .. n-1
+  return n >= 64 ? ~uint64_t(0) : (n <= 0 ? 0 : (uint64_t(1) << n) - 1);
+}
+__device__ inline uint64_t seen_bits(int pos, int key0, int window, int sinks) {
+  uint64_t see = bits_upto(pos - key0 + 1);
+  if (window > 0) see &= ~bits_upto(pos - window + 1 - key0) | bits_upto(sinks - key0);
+  return see;
+}
+// The same for a node of a tree over `held` tokens.
+__device__ inline uint64_t seen_bits_tree(int pos, int key0, int window, int sinks, int held, uint64_t node) {
+  uint64_t see = window > 0 ? ~bits_upto(pos - window + 1 - key0) | bits_upto(sinks - key0) : ~uint64_t(0);
+  const int d = held - key0;                               // the first node's bit
+  see &= bits_upto(d);
+  if (d >= 0) return see | (d < 64 ? node << d : 0);
+  return see | (d > -64 ? node >> -d : 0);
+}
+
+// A sequence's part in a launch over the cache's step.
+struct Part {
+  int seq, at, count, held;    // new tokens `count` from token `at` of the step on, over `held` earlier ones
+};
+__device__ inline Part step_part(const AttnArgs& a, int e) {
+  typedef const attn::const_i32* words;
+  const words w = (words)(a.step + kHeader + kEntry * e);
+  Part p;
+  p.seq = w[0];
+  p.at = w[1];
+  p.count = min(w[2], a.total - w[1]);
+  p.held = w[3] - w[2];
+  return p;
+}
+
+}  // namespace tok
+}  // namespace uf

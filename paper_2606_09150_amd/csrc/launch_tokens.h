@@ -1,0 +1,156 @@
+// Launch interface of the token operators (internal to libuf.so).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "uft.h"
+
+namespace uf {
+namespace tok {
+
+constexpr int kD = 128;
+constexpr int kMaxTree = 64;      // nodes of a tree: bits of a node's word
+constexpr int kInPlace = 16;      // rows that uft_keep moves in place
+
+// Words of host metadata that ride in a launch's arguments.
+constexpr int kWords = 880;
+
+// The device tables: the step (kHeader words, of which the first is its number of
+// sequences, then kEntry words for each: sequence, first token of the step, tokens,
+// length with them), then the page of each page_tokens tokens, [max_seqs][row].
+constexpr int kHeader = 4;
+constexpr int kEntry = 4;
+
+// words[0 .. dense) go to table[dense_at ..]; then n_runs runs: (at, count, first
+// word) triples from words[runs] on.
+struct PokeArgs {
+  int32_t* table;
+  int32_t dense_at, dense, runs, n_runs;
+  int32_t words[kWords];
+};
+hipError_t launch_poke(const PokeArgs& a, hipStream_t stream);
+
+// table rows: (source offset, target offset, count) triples
+struct RowsArgs {
+  int32_t* table;
+  int32_t n;
+  int32_t words[kWords];
+};
+hipError_t launch_rows(const RowsArgs& a, hipStream_t stream);
+
+struct Pool {
+  uint8_t* base;            // of the layer, or of layer 0
+  size_t layer_bytes;
+  int32_t layers, n_pages, kv_heads, page_tokens;
+};
+
+// (source page, target page, rows) triples, every layer
+struct CopyArgs {
+  Pool pool;
+  int32_t n;
+  int32_t words[kWords];
+};
+hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t stream);
+
+// uft_keep.  In place: kKeepWords words a sequence: table offset, length, start,
+// count, first index.  Into fresh pages: the same words, the first page written and
+// how many of the launch's pages came before; then the pages from words[pages] on.
+constexpr int kKeepWords = 7;
+struct KeepArgs {
+  Pool pool;
+  const int32_t* table;     // page table of all sequences
+  const int32_t* index;
+  int32_t n, pages, n_pages, row;
+  int32_t words[kWords];
+};
+hipError_t launch_keep_in_place(const KeepArgs& a, hipStream_t stream);
+hipError_t launch_keep_fresh(const KeepArgs& a, hipStream_t stream);
+
+struct WriteArgs {
+  const uint16_t* k;
+  const uint16_t* v;
+  int64_t k_token, k_head, v_token, v_head;   // elements
+  Pool pool;                                  // base: the layer's
+  const int32_t* step;
+  const int32_t* table;
+  int32_t n, longest, total, row;             // row: pages of a table row
+};
+hipError_t launch_write(const WriteArgs& a, hipStream_t stream);
+
+// Attention forward, from the cache or from plain tensors.
+struct AttnArgs {
+  const uint16_t* q;
+  int64_t q_batch, q_token, q_head;           // elements
+  uint16_t* o;
+  float* lse;
+  const int64_t* tree;
+  // from the cache
+  Pool pool;                                  // base: the layer's
+  const int32_t* step;
+  const int32_t* table;
+  int32_t row;
+  // from plain tensors
+  const uint16_t* k;
+  const uint16_t* v;
+  int64_t k_batch, k_token, k_head, v_batch, v_token, v_head;
+  const int32_t* lengths;
+  int32_t tokens;
+  int32_t n, total;                           // sequences; tokens of the step
+  int32_t q_heads, kv_heads, group, window, sinks;
+  float scale_log2;
+  int32_t tiles;                              // row tiles of the longest sequence
+  int32_t least_rows, most_rows;              // sequences with other numbers of rows are not this launch's
+  int32_t slice;                              // units of keys of a slice at least
+  int32_t n_split;                            // slices at most
+  float* work;                                // partials: O [row][D], then (offset, sum) [row]
+};
+constexpr int kRowTile = 128, kKeyUnit = 64;          // prompts: rows and keys of a tile
+constexpr int kFewRows = 32, kFewUnit = 32;           // few rows: rows of a workgroup, keys of a unit
+// rows (token, head of the group) of partial results of a launch
+inline size_t work_rows(const AttnArgs& a, int tile_rows) {
+  return size_t(a.n) * a.kv_heads * a.n_split * a.tiles * tile_rows;
+}
+hipError_t launch_attn_rows(const AttnArgs& a, bool paged, hipStream_t stream);
+hipError_t launch_attn_few(const AttnArgs& a, hipStream_t stream);
+
+// The range of keys of a tile of queries at positions first .. last, in units of
+// `unit` keys: units 0 .. sink-1 hold sinks that lie before the window's first unit
+// `from`, then come units from .. to.  Unit u of the range is
+// u < sink ? u : u - sink + from.
+struct Range {
+  int32_t sink, from, count, low;             // low: first key of the window of `first`
+};
+__host__ __device__ inline Range key_range(int first, int last, int window, int sinks, int unit) {
+  Range r;
+  r.low = (window > 0 && first - window + 1 > 0) ? first - window + 1 : 0;
+  r.from = r.low / unit;
+  const int s = (sinks + unit - 1) / unit;    // sinks <= 2^30
+  r.sink = s < r.from ? s : r.from;
+  r.count = r.sink + last / unit - r.from + 1;
+  return r;
+}
+// Units of a slice of a range: `slice`, unless the range has more than n_split of them.
+__host__ __device__ inline int slice_units(int count, int slice, int n_split) {
+  const int least = (count + n_split - 1) / n_split;
+  return slice > least ? slice : least;
+}
+
+// Backward.
+struct BwdArgs {
+  const uint16_t *q, *k, *v, *o, *dout;
+  const float* lse;
+  const int32_t* lengths;
+  int64_t q_batch, q_token, q_head, k_batch, k_token, k_head, v_batch, v_token, v_head;
+  uint16_t *dq, *dk, *dv;
+  uint8_t* work;
+  int32_t batch, tokens, q_heads, kv_heads, group, window, sinks;
+  int32_t tiles;                              // row tiles of a sequence
+  float scale, scale_log2;
+};
+size_t bwd_work_bytes(const BwdArgs& a);
+hipError_t launch_window_bwd(const BwdArgs& a, hipStream_t stream);
+
+}  // namespace tok
+}  // namespace uf

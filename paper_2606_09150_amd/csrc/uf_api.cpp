@@ -19,10 +19,15 @@
 
 #include "launch.h"
 #include "launch_bwd.h"
+#include "status.h"
 
 namespace {
 
 thread_local char g_last_error[512] = "";
+
+}  // namespace
+
+namespace uf {
 
 int fail(int status, const char* fmt, ...) {
   va_list ap;
@@ -36,6 +41,13 @@ int ok() {
   g_last_error[0] = '\0';
   return UF_OK;
 }
+
+}  // namespace uf
+
+namespace {
+
+using uf::fail;
+using uf::ok;
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
