@@ -66,7 +66,10 @@ def grads(q, k, v, do, see, scale):
     d_dp = (np.abs(do) @ np.abs(v).T + np.abs(delta)) * (do.shape[1] + 8) * FP32
     e_ds = np.abs(ds) * (2 * BF16 + BF16 ** 2 + off) + p * (d_delta + d_dp) * (1 + 2 * BF16)
     e_p = p * (BF16 + off)
-    b_dq, b_dk, b_dv = scale * e_ds @ np.abs(k), scale * e_ds.T @ np.abs(q), e_p.T @ np.abs(do)
+    # for dK the weights pass through fp16, 2^15 times as large: where that is subnormal (spacing 2^-24, weights below
+    # 2^-14 / 2^15) they are off by half a spacing, 2^-25 / 2^15, whatever their own size
+    e_dsk = e_ds + 2.0 ** -40 * np.abs(dp - delta) * see * (1 + BF16)
+    b_dq, b_dk, b_dv = scale * e_ds @ np.abs(k), scale * e_dsk.T @ np.abs(q), e_p.T @ np.abs(do)
     sums = (2 * max(k.shape[0], q.shape[0]) + 64) * FP32
     return [(g, b + s * sums + (np.abs(g) + b) * BF16 + 1e-30)
             for g, b, s in ((dq, b_dq, scale * np.abs(ds) @ np.abs(k)), (dk, b_dk, scale * np.abs(ds).T @ np.abs(q)),

@@ -1,6 +1,7 @@
 """ctypes binding of the token operators of libuf.so (include/uft.h): argument marshalling only."""
 
 import ctypes
+import operator
 
 from . import _lib as L
 
@@ -76,7 +77,12 @@ def load():
 
 
 def _ints(values):
-    return (_I * len(values))(*values)
+    if hasattr(values, "data_ptr"):
+        raise TypeError("sequences, counts and starts are host integers, not a tensor")
+    try:
+        return (_I * len(values))(*values)
+    except TypeError:                        # other integers (numpy's)
+        return (_I * len(values))(*[operator.index(v) for v in values])
 
 
 def _same(a, b, names):

@@ -650,10 +650,10 @@ template <int TILE, int UNIT>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
   const int H = a.kv_heads, G = a.group;
   const int lane = threadIdx.x & 63;
-  const int64_t item = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int per = a.tiles * TILE;
-  const int row = int(item % per);
-  const int eh = int(item / per);
+  const uint32_t fours = uint32_t(a.longest_rows + 3) / 4;
+  const int eh = int(blockIdx.x / fours);
+  const int row = int(blockIdx.x % fours) * 4 + (threadIdx.x >> 6);
   const int h = eh % H, e = eh / H;
   if (e >= a.n || e >= a.step[0]) return;
   const Part p = step_part(a, e);
@@ -702,8 +702,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
 
 template <int TILE, int UNIT>
 hipError_t launch_join(const AttnArgs& a, hipStream_t stream) {
-  const int64_t rows = int64_t(a.n) * a.kv_heads * a.tiles * TILE;
-  join_kernel<TILE, UNIT><<<unsigned((rows + 3) / 4), 256, 0, stream>>>(a);
+  join_kernel<TILE, UNIT><<<unsigned(a.longest_rows + 3) / 4 * unsigned(a.n) * unsigned(a.kv_heads), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -37,6 +37,7 @@ constexpr uint32_t kTile = 32768;              // [128][128] bf16
 constexpr size_t kRecord = 2 * kTile + 1024;
 constexpr size_t kPartial = size_t(2) * kT * kD * 4;   // dV, dK of a part, fp32
 
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 
@@ -232,7 +233,10 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb) acc[mb] = f32x16{};
   const float c2 = a.scale_log2;
-  const float pad = key_ok ? 0.f : -INFINITY;  // keys that are none weigh nothing
+  // P (at most 1) is formed 2^15 times too large, and dV and dK are scaled back at the end, so that it can be handed
+  // over in fp16: off by 2^-11 of itself, below weights of 2^-29 by 2^-40 at most, where bf16's 2^-8 put 20 % on dK's
+  // error
+  const float pad = key_ok ? 15.f : -INFINITY; // keys that are none weigh nothing
   uint4* const pslot = &sP[0][kw][0][lane];
   constexpr uint32_t kPStep = sizeof(sP[0]) / 16;
   // Operand addresses within the current ring slots, advanced once per phase: tr,
@@ -314,10 +318,14 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) x[i] = load(i);
+    f16x8 hand;
     auto weights = [&](int qb, int e) {
-      put(op[qb], e, __builtin_amdgcn_exp2f(__builtin_fmaf(sv[qb][2 * e], c2, pad)),
-          __builtin_amdgcn_exp2f(__builtin_fmaf(sv[qb][2 * e + 1], c2, pad)));
-      if ((e & 3) == 3) pslot[par * kPStep + (qb * 2 + (e >> 2)) * 64] = __builtin_bit_cast(uint4, op[qb][e >> 2]);
+      const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[qb][2 * e], c2, pad));
+      const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[qb][2 * e + 1], c2, pad));
+      put(op[qb], e, w0, w1);
+      hand[2 * (e & 3)] = (_Float16)w0;
+      hand[2 * (e & 3) + 1] = (_Float16)w1;
+      if ((e & 3) == 3) pslot[par * kPStep + (qb * 2 + (e >> 2)) * 64] = __builtin_bit_cast(uint4, hand);
     };
     fence();
 #pragma unroll
@@ -338,13 +346,14 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
                    const Source& next) {
     constexpr bool kDp = decltype(dp)::value, kDk = decltype(dk)::value;
     constexpr int i0 = kDp ? 0 : kRows, i1 = kDk ? kAll : kRows;
-    bf16x8 pk[NB][2], op[NB][2], x[kAll];
+    f16x8 pk[NB][2];
+    bf16x8 op[NB][2], x[kAll];
     if (kDk) {
 #pragma unroll
       for (int qb = 0; qb < NB; ++qb)
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk)
-          pk[qb][kk] = __builtin_bit_cast(bf16x8, pslot[par * kPStep + (qb * 2 + kk) * 64]);
+          pk[qb][kk] = __builtin_bit_cast(f16x8, pslot[par * kPStep + (qb * 2 + kk) * 64]);
     }
     if (kDp) seed(ld, nv);
 #pragma unroll
@@ -422,7 +431,7 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
   }
   if (key < a.tokens) {
     uint16_t* dst = (grp ? a.dk : a.dv) + ((size_t(b) * a.tokens + key) * H + h) * kD + 4 * hl;
-    const float f = grp ? a.scale : 1.0f;
+    const float f = grp ? a.scale * 0x1p-15f : 0x1p-15f;
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
@@ -464,7 +473,7 @@ __global__ __launch_bounds__(256) void sum_kernel(BwdArgs a, Cut cut, const floa
       s.w = __builtin_fmaf(v[i].w, on, s.w);
     }
   }
-  const float f = key < len ? (grp ? a.scale : 1.0f) : 0.f;
+  const float f = key < len ? (grp ? a.scale * 0x1p-15f : 0x1p-15f) : 0.f;
   uint2 u;
   u.x = pack_bf16x2(s.x * f, s.y * f);
   u.y = pack_bf16x2(s.z * f, s.w * f);
@@ -489,13 +498,16 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, hl = lane >> 5, ln = lane & 31, rp = lane & 15, g = (lane >> 4) & 1;
   const int q = wave * 32 + ln, row = row0 + q;
-  const int token = int(uint32_t(row) / uint32_t(G)), head = h * G + row - token * G;
-  const bool stored = row < a.tokens * G;
-  uint16_t* const dst = a.dq + ((size_t(b) * a.tokens + token) * a.q_heads + head) * kD + 4 * hl;
+  auto target = [&](int r) {                           // of row r's gradient
+    const int t = int(uint32_t(r) / uint32_t(G));
+    return a.dq + ((size_t(b) * a.tokens + t) * a.q_heads + h * G + r - t * G) * kD + 4 * hl;
+  };
   if (row0 >= rows) {                                  // padding
-    if (stored)
+    if (row < a.tokens * G) {
+      uint16_t* const dst = target(row);
 #pragma unroll
       for (int i = 0; i < 16; ++i) *reinterpret_cast<uint2*>(dst + 8 * i) = make_uint2(0, 0);
+    }
     return;
   }
   const int first = row0 / G, last = (min(row0 + kT, rows) - 1) / G;
@@ -503,7 +515,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
   const int w0 = row0 + wave * 32;
   const bool idle = w0 >= rows;
   const int pmin = w0 / G, pmax = (min(w0 + 32, rows) - 1) / G;
-  const int pos = min(token, pmax);
+  const int pos = min(int(uint32_t(row) / uint32_t(G)), pmax);
 
   const uint8_t* rec = a.work + (size_t(bh) * a.tiles + tile) * kRecord;
   bf16x8 qf[8], of[8];
@@ -515,9 +527,6 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
   const float c2 = a.scale_log2;
   const float nl = reinterpret_cast<const float*>(rec + 2 * kTile)[q] * c2;
   const float nd = reinterpret_cast<const float*>(rec + 2 * kTile)[kT + q];
-  f32x16 negd;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) negd[r] = nd;
 
   const uint32_t lds0 = lds_addr(&sbuf[0][0]);
   uint32_t kr[4], kt[2][2];                            // K rows (V rows 16 KB behind); K transposed
@@ -602,8 +611,8 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
     };
     auto weight = [&](int n, int r) { sv[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[n][r], c2, nl)); };
     auto ds = [&](int n, int e) {
-      op[n][e >> 2][2 * (e & 3)] = (__bf16)(sv[n][2 * e] * dp[n][2 * e]);
-      op[n][e >> 2][2 * (e & 3) + 1] = (__bf16)(sv[n][2 * e + 1] * dp[n][2 * e + 1]);
+      op[n][e >> 2][2 * (e & 3)] = (__bf16)(sv[n][2 * e] * (dp[n][2 * e] + nd));
+      op[n][e >> 2][2 * (e & 3) + 1] = (__bf16)(sv[n][2 * e + 1] * (dp[n][2 * e + 1] + nd));
     };
 #pragma unroll
     for (int k = 0; k < kReads; ++k) x[k] = load(k);
@@ -618,7 +627,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
           if constexpr ((k0 & 8) == 0)
             sv[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[k], qf[j], j ? sv[n] : f32x16{}, 0, 0, 0);
           else
-            dp[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[k], of[j], j ? dp[n] : negd, 0, 0, 0);
+            dp[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[k], of[j], j ? dp[n] : f32x16{}, 0, 0, 0);
         } else {
           dqt[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[k], op[(k0 - kSP) >> 3][j >> 2], dqt[j & 3], 0, 0, 0);
         }
@@ -673,8 +682,11 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
     next = unit_of(min(u + 2, U - 1));
   }
   meet<0>();                                           // no copy outlives the workgroup
-  if (!stored) return;
-  const float f = row < rows ? a.scale : 0.f;          // (padding accumulated zeros)
+  int r_out = row;                                     // (its address is formed here, not held across the walk)
+  asm volatile("" : "+v"(r_out));
+  if (r_out >= a.tokens * G) return;
+  uint16_t* const dst = target(r_out);
+  const float f = r_out < rows ? a.scale : 0.f;        // (padding accumulated zeros)
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb)
 #pragma unroll

@@ -36,6 +36,7 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(RowsArgs a) {
 
 // One workgroup per (page, K or V, head; layer).  Loads before stores: the stores
 // could alias them as far as the compiler knows.
+template <int T>
 __global__ __launch_bounds__(kThreads) void copy_pages_kernel(CopyArgs a) {
   const int heads = 2 * a.pool.kv_heads;
   const int i = blockIdx.x / heads, kvh = blockIdx.x % heads;
@@ -44,13 +45,19 @@ __global__ __launch_bounds__(kThreads) void copy_pages_kernel(CopyArgs a) {
   const uint4* src = reinterpret_cast<const uint4*>(base + page_rows(a.pool, a.words[3 * i], 0, kvh));
   uint4* dst = reinterpret_cast<uint4*>(base + page_rows(a.pool, a.words[3 * i + 1], 0, kvh));
   const int n = rows * kRowChunks;
-  uint4 x[8];                                // 128 rows at most
+  constexpr int kPer = T * kRowChunks / kThreads;
+  uint4 x[kPer];
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    if (threadIdx.x + k * kThreads < n) x[k] = src[threadIdx.x + k * kThreads];
+  for (int k = 0; k < kPer; ++k) {
+    const int i = threadIdx.x + k * kThreads;
+    x[k] = make_uint4(0, 0, 0, 0);
+    if (i < n) x[k] = src[i];
+  }
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    if (threadIdx.x + k * kThreads < n) dst[threadIdx.x + k * kThreads] = x[k];
+  for (int k = 0; k < kPer; ++k) {
+    const int i = threadIdx.x + k * kThreads;
+    if (i < n) dst[i] = x[k];
+  }
 }
 
 // Row at position `pos` of the sequence whose pages start at table[seq_row]: null
@@ -120,41 +127,83 @@ __global__ __launch_bounds__(kThreads) void keep_fresh_kernel(KeepArgs a) {
   }
 }
 
-// New tokens: a workgroup takes 2,048 chunks at a time (8 tokens of 8 heads) of one
-// sequence.
-__global__ __launch_bounds__(kThreads) void write_kernel(WriteArgs a) {
+// New tokens of many: one workgroup per (page's worth of them, K or V, head; sequence),
+// whose rows lie side by side in the page.
+template <int T>
+__global__ __launch_bounds__(kThreads) void write_pages_kernel(WriteArgs a, int spans) {
   const int e = blockIdx.y;
-  if (e >= a.step[0]) return;
-  const int32_t* entry = a.step + kHeader + kEntry * e;
-  const int seq = entry[0], at = entry[1], count = min(entry[2], a.total - entry[1]), first = entry[3] - entry[2];
-  const int H = a.pool.kv_heads, per = 2 * H * kRowChunks;   // chunks of a token
-  const int64_t n = int64_t(count) * per;
-  constexpr int kPer = 8;
-  for (int64_t i0 = int64_t(blockIdx.x) * kPer * kThreads; i0 < n; i0 += int64_t(gridDim.x) * kPer * kThreads) {
+  typedef __attribute__((address_space(4))) int32_t uniform_i32;
+  const uniform_i32* step = (const uniform_i32*)a.step;
+  const uniform_i32* entry = step + kHeader + kEntry * e;
+  if (e >= step[0]) return;
+  const int seq = entry[0], at = entry[1], count = min(entry[2], a.total - at), first = entry[3] - entry[2];
+  const int H = a.pool.kv_heads;
+  const int kvh = blockIdx.x / spans;
+  const uniform_i32* pages = (const uniform_i32*)(a.table + size_t(seq) * a.row);
+  constexpr int kPer = T * kRowChunks / kThreads, kSlots = kThreads / kRowChunks;
+  const int c = threadIdx.x % kRowChunks, slot = threadIdx.x / kRowChunks;
+  const bool isv = kvh >= H;
+  const int64_t ts = isv ? a.v_token : a.k_token;
+  const uint16_t* src = isv ? a.v + int64_t(kvh - H) * a.v_head : a.k + int64_t(kvh) * a.k_head;
+  for (int s = blockIdx.x % spans; ; s += spans) {
+    const int64_t p0 = (int64_t(first) / T + s) * T;     // first position of the page
+    if (p0 >= int64_t(first) + count) return;
+    const int page = pages[p0 / T];
+    if (uint32_t(page) >= uint32_t(a.pool.n_pages)) continue;
+    uint4* dst = reinterpret_cast<uint4*>(a.pool.base + page_rows(a.pool, page, 0, kvh)) + c;
     uint4 x[kPer];
-    uint4* dst[kPer];
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-      const int64_t i = i0 + k * kThreads + threadIdx.x;
-      dst[k] = nullptr;
-      if (i < n) {
-        const int t = int(i / per), r = int(i % per);
-        const int kvh = r / kRowChunks, c = r % kRowChunks;
-        const bool isv = kvh >= H;
-        const int h = isv ? kvh - H : kvh;
-        const int64_t off = isv ? int64_t(at + t) * a.v_token + int64_t(h) * a.v_head
-                                : int64_t(at + t) * a.k_token + int64_t(h) * a.k_head;
-        x[k] = *reinterpret_cast<const uint4*>((isv ? a.v : a.k) + off + 8 * c);
-        const int pos = first + t;
-        const int page = a.table[size_t(seq) * a.row + pos / a.pool.page_tokens];
-        if (uint32_t(page) < uint32_t(a.pool.n_pages))
-          dst[k] = reinterpret_cast<uint4*>(a.pool.base + page_rows(a.pool, page, 0, kvh)) +
-                   (pos % a.pool.page_tokens) * kRowChunks + c;
-      }
+      const int64_t t = p0 + slot + k * kSlots - first;
+      x[k] = make_uint4(0, 0, 0, 0);
+      if (t >= 0 && t < count) x[k] = *reinterpret_cast<const uint4*>(src + (at + t) * ts + 8 * c);
     }
 #pragma unroll
-    for (int k = 0; k < kPer; ++k)
-      if (dst[k] != nullptr) *dst[k] = x[k];
+    for (int k = 0; k < kPer; ++k) {
+      const int64_t t = p0 + slot + k * kSlots - first;
+      if (t >= 0 && t < count) dst[(slot + k * kSlots) * kRowChunks] = x[k];
+    }
+  }
+}
+
+// New tokens of few: a workgroup takes `per` tokens of one sequence at a time, a row (token,
+// K or V, head) in 16 lanes, eight rows a thread before the first is stored.
+__global__ __launch_bounds__(kThreads) void write_kernel(WriteArgs a, int per) {
+  const int e = blockIdx.y;
+  typedef __attribute__((address_space(4))) int32_t uniform_i32;
+  const uniform_i32* step = (const uniform_i32*)a.step;
+  const uniform_i32* entry = step + kHeader + kEntry * e;
+  if (e >= step[0]) return;
+  const int seq = entry[0], at = entry[1], count = min(entry[2], a.total - at), first = entry[3] - entry[2];
+  const int H = a.pool.kv_heads, T = a.pool.page_tokens;
+  const int c = threadIdx.x % kRowChunks, slot = threadIdx.x / kRowChunks;
+  const int32_t* pages = a.table + size_t(seq) * a.row;
+  constexpr int kPer = 8, kSlots = kThreads / kRowChunks;
+  for (int64_t t0 = int64_t(blockIdx.x) * per; t0 < count; t0 += int64_t(gridDim.x) * per) {
+    const int rows = min(per, count - int(t0)) * 2 * H;
+    for (int r0 = 0; r0 < rows; r0 += kPer * kSlots) {
+      uint4 x[kPer];
+      uint4* dst[kPer];
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        const int r = r0 + k * kSlots + slot;
+        dst[k] = nullptr;
+        if (r < rows) {
+          const int t = int(uint32_t(r) / uint32_t(2 * H)), kvh = r - t * 2 * H;
+          const bool isv = kvh >= H;
+          const int64_t token = at + t0 + t;
+          const int64_t off = isv ? token * a.v_token + int64_t(kvh - H) * a.v_head : token * a.k_token + int64_t(kvh) * a.k_head;
+          x[k] = *reinterpret_cast<const uint4*>((isv ? a.v : a.k) + off + 8 * c);
+          const int pos = first + int(t0) + t;
+          const int page = pages[uint32_t(pos) / uint32_t(T)];
+          if (uint32_t(page) < uint32_t(a.pool.n_pages))
+            dst[k] = reinterpret_cast<uint4*>(a.pool.base + page_rows(a.pool, page, 0, kvh)) + (pos & (T - 1)) * kRowChunks + c;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+        if (dst[k] != nullptr) *dst[k] = x[k];
+    }
   }
 }
 
@@ -171,7 +220,11 @@ hipError_t launch_rows(const RowsArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t stream) {
-  copy_pages_kernel<<<dim3(unsigned(a.n) * 2 * unsigned(a.pool.kv_heads), unsigned(a.pool.layers)), kThreads, 0, stream>>>(a);
+  const dim3 grid(unsigned(a.n) * 2 * unsigned(a.pool.kv_heads), unsigned(a.pool.layers));
+  if (a.pool.page_tokens == 128)
+    copy_pages_kernel<128><<<grid, kThreads, 0, stream>>>(a);
+  else
+    copy_pages_kernel<64><<<grid, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -190,9 +243,19 @@ hipError_t launch_keep_fresh(const KeepArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_write(const WriteArgs& a, hipStream_t stream) {
-  const int64_t chunks = int64_t(a.longest) * 2 * a.pool.kv_heads * kRowChunks;
-  const unsigned blocks = unsigned((chunks + 8 * kThreads - 1) / (8 * kThreads) < 65536 ? (chunks + 8 * kThreads - 1) / (8 * kThreads) : 65536);
-  write_kernel<<<dim3(blocks, unsigned(a.n)), kThreads, 0, stream>>>(a);
+  if (a.longest >= 16) {
+    const int T = a.pool.page_tokens;
+    const int spans = (a.longest - 1 + T - 1) / T + 1;   // pages that so many tokens can touch
+    const dim3 grid(unsigned(spans) * 2 * unsigned(a.pool.kv_heads), unsigned(a.n));
+    if (T == 128)
+      write_pages_kernel<128><<<grid, kThreads, 0, stream>>>(a, spans);
+    else
+      write_pages_kernel<64><<<grid, kThreads, 0, stream>>>(a, spans);
+    return hipGetLastError();
+  }
+  const int per = a.pool.kv_heads < 64 ? 64 / a.pool.kv_heads : 1;     // 128 rows
+  const int64_t blocks = (int64_t(a.longest) + per - 1) / per;
+  write_kernel<<<dim3(unsigned(blocks), unsigned(a.n)), kThreads, 0, stream>>>(a, per);
   return hipGetLastError();
 }
 

@@ -102,6 +102,7 @@ struct AttnArgs {
   float scale_log2;
   int32_t tiles;                              // row tiles of the longest sequence
   int32_t least_rows, most_rows;              // sequences with other numbers of rows are not this launch's
+  int32_t longest_rows;                       // the most rows of one of its sequences
   int32_t slice;                              // units of keys of a slice at least
   int32_t n_split;                            // slices at most
   float* work;                                // partials: O [row][D], then (offset, sum) [row]

@@ -746,7 +746,7 @@ namespace {
 // One launch over the sequences of a step whose rows number least .. most.
 struct Launch {
   bool run = false;
-  int32_t least = 0, most = 0, tiles = 0, slice = 0, n_split = 1;
+  int32_t least = 0, most = 0, longest = 0, tiles = 0, slice = 0, n_split = 1;
   size_t work_rows = 0;
 };
 
@@ -795,10 +795,12 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
   const int32_t sinks = std::min(d->sinks, c->d.max_tokens);
   std::vector<int32_t> few, rows;
   int64_t tiles = 0;
+  int64_t few_rows = 0, many_rows = 0;
   for (const Entry& e : c->step) {
     const int64_t r = int64_t(e.count) * G;
     if (r == 0) continue;
     const int32_t first = e.tokens - e.count;
+    (r <= tok::kFewRows ? few_rows : many_rows) = std::max(r <= tok::kFewRows ? few_rows : many_rows, r);
     if (r <= tok::kFewRows) {
       few.push_back(tok::key_range(first, e.tokens - 1, d->window, sinks, tok::kFewUnit).count);
       continue;
@@ -819,6 +821,7 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
     p->few.run = true;
     p->few.least = 1;
     p->few.most = tok::kFewRows;
+    p->few.longest = int32_t(few_rows);
     p->few.tiles = 1;
     choose_slices(few, H, d->n_cu, 6, 12, &p->few);
     p->few.work_rows = p->few.n_split > 1 ? size_t(n) * H * p->few.n_split * tok::kFewRows : 0;
@@ -827,12 +830,13 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
     p->rows.run = true;
     p->rows.least = tok::kFewRows + 1;
     p->rows.most = INT32_MAX;
+    p->rows.longest = int32_t(many_rows);
     p->rows.tiles = int32_t(tiles);
     choose_slices(rows, H, int64_t(2) * d->n_cu, 4, 6, &p->rows);
     p->rows.work_rows = p->rows.n_split > 1 ? size_t(n) * H * p->rows.n_split * size_t(tiles) * tok::kRowTile : 0;
   }
   const double grid = double(n) * H * std::max(double(tiles) * p->rows.n_split, 64.0);
-  if (grid > 2147483647.0) return fail(UF_ERR_ARG, "step too large for one launch");
+  if (grid > 2147483647.0 || double(many_rows) > 2.0e9) return fail(UF_ERR_ARG, "step too large for one launch");
   p->bytes = (p->few.work_rows + p->rows.work_rows) * (tok::kD + 2) * 4;
   return UF_OK;
 }
@@ -898,6 +902,7 @@ int uft_attn(const uft_cache* c, int32_t layer, const uft_attn_desc* d, const vo
       if (!l->run) continue;
       a.least_rows = l->least;
       a.most_rows = l->most;
+      a.longest_rows = l->longest;
       a.tiles = l->tiles;
       a.slice = l->slice;
       a.n_split = l->n_split;
