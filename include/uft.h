@@ -57,8 +57,8 @@ typedef struct {
 } uft_info;
 
 /* Elements between neighbours along each axis; the head dimension is contiguous.
- * Multiples of 8, at most 2^24 from token to token; batch is not read where there
- * is none. */
+ * Multiples of 8, at most 2^24 from token to token and 2^30 from head to head; batch
+ * is not read where there is none. */
 typedef struct {
   int64_t batch, token, head;
 } uft_stride;

@@ -645,17 +645,22 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
 
 // ---------------------------------------------------------------- join slices ----
 //
-// A wave per row: the slices' offsets and sums, then their O, two dims a lane.
-template <int TILE, int UNIT>
+// Sixteen lanes hold a row's dims, eight each, and LANES / 16 such groups share its
+// slices: their offsets and sums first, then their O.  Latency bounds it (entry, range,
+// slices, store): 16 lanes a row where slices are few, so that a wave holds four rows (a
+// wave a row took 20 us for 32,768 rows of two slices, this 9), 64 where they are many
+// (32 rows of 32 slices: 8.5 us with 16).
+template <int TILE, int UNIT, int LANES>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
+  constexpr int kGroups = LANES / 16, kRows = 256 / LANES, kOwn = 64 / LANES;   // slices of a lane
   const int H = a.kv_heads, G = a.group;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & (LANES - 1), c = lane & 15, grp = lane >> 4;
   const int per = a.tiles * TILE;
-  const uint32_t fours = uint32_t(a.longest_rows + 3) / 4;
-  const int eh = int(blockIdx.x / fours);
-  const int row = int(blockIdx.x % fours) * 4 + (threadIdx.x >> 6);
+  const uint32_t blocks = uint32_t(a.longest_rows + kRows - 1) / kRows;
+  const int eh = int(blockIdx.x / blocks);
+  const int row = int(blockIdx.x % blocks) * kRows + threadIdx.x / LANES;
   const int h = eh % H, e = eh / H;
-  if (e >= a.n || e >= a.step[0]) return;
+  if (e >= ((const const_i32*)a.step)[0]) return;
   const Part p = step_part(a, e);
   const int rows = p.count * G;
   if (rows < a.least_rows || rows > a.most_rows || row >= rows) return;
@@ -669,40 +674,67 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
   const int n = (range.count + units - 1) / units;     // at most n_split <= 64
   const size_t all = size_t(a.n) * H * a.n_split * per;
   const size_t at = size_t(eh) * a.n_split * per + row;
-  float2 ml = make_float2(-INFINITY, 0.f);
-  if (lane < n) ml = reinterpret_cast<const float2*>(a.work + all * kD)[at + size_t(lane) * per];
-  float mm = ml.x;
+  const float2* mlp = reinterpret_cast<const float2*>(a.work + all * kD) + at;
+  float f[kOwn], l[kOwn], mm = -INFINITY, lt = 0.f;
 #pragma unroll
-  for (int s = 1; s < 64; s <<= 1) mm = fmaxf(mm, __shfl_xor(mm, s));
-  const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - mm);
-  float lt = ml.y * f;
+  for (int i = 0; i < kOwn; ++i) {
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane + LANES * i < n) ml = mlp[size_t(lane + LANES * i) * per];
+    f[i] = ml.x;
+    l[i] = ml.y;
+    mm = fmaxf(mm, ml.x);
+  }
 #pragma unroll
-  for (int s = 1; s < 64; s <<= 1) lt += __shfl_xor(lt, s);
-  float x = 0.f, y = 0.f;
-  const float2* op = reinterpret_cast<const float2*>(a.work + at * kD) + lane;
-  for (int s0 = 0; s0 < n; s0 += 8) {
-    float2 v[8];
+  for (int s = 1; s < LANES; s <<= 1) mm = fmaxf(mm, __shfl_xor(mm, s, LANES));
 #pragma unroll
-    for (int s = 0; s < 8; ++s) v[s] = op[size_t(min(s0 + s, n - 1)) * per * (kD / 2)];
+  for (int i = 0; i < kOwn; ++i) {
+    f[i] = f[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(f[i] - mm);
+    lt += l[i] * f[i];
+  }
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      const float w = s0 + s < n ? __shfl(f, s0 + s) : 0.f;
-      if (w > 0.f) {                                   // (nothing was seen: its O is zero)
-        x += v[s].x * w;
-        y += v[s].y * w;
+  for (int s = 1; s < LANES; s <<= 1) lt += __shfl_xor(lt, s, LANES);
+  float x[8] = {};
+  const float4* op = reinterpret_cast<const float4*>(a.work + at * kD) + 2 * c;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i)
+    for (int s0 = LANES * i; s0 < min(n, LANES * (i + 1)); s0 += 4 * kGroups) {
+      float4 v[4][2];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const float4* vp = op + size_t(min(s0 + s * kGroups + grp, n - 1)) * per * (kD / 4);
+        v[s][0] = vp[0];
+        v[s][1] = vp[1];
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const float w = __shfl(f[i], (s0 + s * kGroups + grp) & (LANES - 1), LANES);   // 0 past the end
+        if (w > 0.f) {
+          x[0] += v[s][0].x * w, x[1] += v[s][0].y * w, x[2] += v[s][0].z * w, x[3] += v[s][0].w * w;
+          x[4] += v[s][1].x * w, x[5] += v[s][1].y * w, x[6] += v[s][1].z * w, x[7] += v[s][1].w * w;
+        }
       }
     }
-  }
+#pragma unroll
+  for (int s = 16; s < LANES; s <<= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] += __shfl_xor(x[i], s, LANES);
+  if (grp != 0) return;
   const float inv = lt > 0.f ? 1.f / lt : 0.f;
   const int token = row / G, head = h * G + row - token * G;
   const size_t out = (size_t(p.at) + token) * a.q_heads + head;
-  reinterpret_cast<uint32_t*>(a.o)[out * (kD / 2) + lane] = pack_bf16x2(x * inv, y * inv);
-  if (a.lse != nullptr && lane == 0) a.lse[out] = lt > 0.f ? (mm + log2f(lt)) * 0.69314718055994531f : -INFINITY;
+  reinterpret_cast<uint4*>(a.o)[out * (kD / 8) + c] =
+      make_uint4(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv),
+                 pack_bf16x2(x[4] * inv, x[5] * inv), pack_bf16x2(x[6] * inv, x[7] * inv));
+  if (a.lse != nullptr && c == 0) a.lse[out] = lt > 0.f ? (mm + log2f(lt)) * 0.69314718055994531f : -INFINITY;
 }
 
 template <int TILE, int UNIT>
 hipError_t launch_join(const AttnArgs& a, hipStream_t stream) {
-  join_kernel<TILE, UNIT><<<unsigned(a.longest_rows + 3) / 4 * unsigned(a.n) * unsigned(a.kv_heads), 256, 0, stream>>>(a);
+  const unsigned pairs = unsigned(a.n) * unsigned(a.kv_heads);
+  if (a.n_split <= 4)
+    join_kernel<TILE, UNIT, 16><<<unsigned(a.longest_rows + 15) / 16 * pairs, 256, 0, stream>>>(a);
+  else
+    join_kernel<TILE, UNIT, 64><<<unsigned(a.longest_rows + 3) / 4 * pairs, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -9,20 +9,22 @@
 // themselves.
 //
 // Kernels, all with 32x32x16 bf16 MFMA and fp32 accumulation:
-//  * prep: records of 128 rows, Q and dO (zero where there is no row), then
-//    -LSE/scale (-inf there, so that their weights vanish) and -delta, which seed the
-//    S and dP accumulators;
+//  * dq: one workgroup of four waves per 128 rows, two per CU: delta from the rows' dO and
+//    O, then per 32 keys S^T = K Q^T, dP^T = V dO^T, dS^T and dQ^T += K^T dS^T.  It leaves
+//    -LSE/scale (-inf where there is no row, so that its weights vanish) and -delta in
+//    the workspace, the seeds of dkdv's S and dP accumulators;
 //  * dkdv: one workgroup of eight waves per 128 keys of a head.  Waves w and w + 4
 //    share 32 keys: wave w computes S = Q K^T and P, hands P to wave w + 4 through LDS
 //    and accumulates dV^T += dO^T P, while wave w + 4 computes dP = dO V^T and, one unit
 //    of 64 rows later, dS = P dP and dK^T += Q^T dS;
-//  * dq: one workgroup of four waves per record, two per CU: per 32 keys S^T = K Q^T,
-//    dP^T = V dO^T, dS^T, then dQ^T += K^T dS^T;
 //  * sum: where a key tile's rows were cut into parts (the sinks', which every later row
 //    sees), the parts' dK and dV in fp32, added in order.
+// (A pass that copied Q and dO into records of 128 rows and formed delta took 123 us of
+// 2,660 at 16,384 tokens, 32 heads, window 2,048, and 66 KB of workspace a record.)
 // The transposed operands come from row-major LDS tiles through transposing reads.
 // Every output row is owned by one workgroup and sums have one order: no atomics.
 #include <type_traits>
+#include <utility>
 
 #include "token_common.h"
 
@@ -32,71 +34,28 @@ namespace {
 
 using namespace attn;
 
-constexpr int kT = 128;                        // rows of a record, keys of a dkdv tile
-constexpr uint32_t kTile = 32768;              // [128][128] bf16
-constexpr size_t kRecord = 2 * kTile + 1024;
+constexpr int kT = 128;                        // rows of a dq tile, keys of a dkdv tile
+constexpr size_t kSeeds = 1024;                // of 128 rows: -LSE/scale, then -delta, fp32
 constexpr size_t kPartial = size_t(2) * kT * kD * 4;   // dV, dK of a part, fp32
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 
+// f(from), .., f(to - 1), each index a constant.
+template <int FROM, class F, int... I>
+__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, FROM + I>{}), ...);
+}
+template <int FROM, int TO, class F>
+__device__ __forceinline__ void each(F f) {
+  each_of<FROM>(f, std::make_integer_sequence<int, TO - FROM>{});
+}
+
 __device__ inline float bf16f(uint32_t x) { return __uint_as_float(x << 16); }
 
 __device__ inline int length_of(const BwdArgs& a, int b) {
   return a.lengths != nullptr ? min(max(((const const_i32*)a.lengths)[b], 0), a.tokens) : a.tokens;
-}
-
-// ---------------------------------------------------------------- prep ----
-//
-// HBM-bound: Q, dO and O are read once and a record written; 16 lanes hold a row's
-// chunks, so delta is formed from the chunks of the copy and added over them.
-__global__ __launch_bounds__(256) void prep_kernel(BwdArgs a) {
-  const int H = a.kv_heads, G = a.group;
-  const int tile = blockIdx.x % a.tiles;
-  const int bh = blockIdx.x / a.tiles;
-  const int h = bh % H, b = bh / H;
-  const int rows = length_of(a, b) * G;
-  uint8_t* rec = a.work + (size_t(bh) * a.tiles + tile) * kRecord;
-  float* nlse = reinterpret_cast<float*>(rec + 2 * kTile);
-  const int cc = threadIdx.x & 15, r0 = threadIdx.x >> 4;
-  uint4 vq[8], vg[8], vo[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {                // every load before the first store
-    const int row = tile * kT + r0 + 16 * k;
-    vq[k] = vg[k] = vo[k] = make_uint4(0, 0, 0, 0);
-    if (row < rows) {
-      const int t = int(uint32_t(row) / uint32_t(G)), head = h * G + row - t * G;
-      const size_t off = ((size_t(b) * a.tokens + t) * a.q_heads + head) * kD + cc * 8;
-      vq[k] = *reinterpret_cast<const uint4*>(a.q + int64_t(b) * a.q_batch + int64_t(t) * a.q_token +
-                                              int64_t(head) * a.q_head + cc * 8);
-      vg[k] = *reinterpret_cast<const uint4*>(a.dout + off);
-      vo[k] = *reinterpret_cast<const uint4*>(a.o + off);
-    }
-  }
-  if (threadIdx.x < kT) {
-    const int row = tile * kT + threadIdx.x;
-    float nl = -INFINITY;
-    if (row < rows) {
-      const int t = int(uint32_t(row) / uint32_t(G)), head = h * G + row - t * G;
-      nl = -a.lse[(size_t(b) * a.q_heads + head) * a.tokens + t] / a.scale;
-    }
-    nlse[threadIdx.x] = nl;
-  }
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int r = r0 + 16 * k, c = r * 16 + cc;
-    reinterpret_cast<uint4*>(rec)[c] = vq[k];
-    reinterpret_cast<uint4*>(rec + kTile)[c] = vg[k];
-    const uint32_t g[4] = {vg[k].x, vg[k].y, vg[k].z, vg[k].w}, o[4] = {vo[k].x, vo[k].y, vo[k].z, vo[k].w};
-    float dl = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      dl += bf16f(o[e] & 0xffffu) * bf16f(g[e] & 0xffffu) + bf16f(o[e] >> 16) * bf16f(g[e] >> 16);
-#pragma unroll
-    for (int s = 1; s < 16; s <<= 1) dl += __shfl_xor(dl, s, 16);
-    if (cc == 0) nlse[kT + r] = -dl;
-  }
 }
 
 // ---------------------------------------------------------------- dkdv ----
@@ -108,6 +67,11 @@ __device__ inline int swz_perm(int c) { return (c & ~10) | ((c & 2) << 2) | ((c 
 __device__ inline int swz_f(int r) { return (r & 8) | ((r & 3) << 1) | (((r >> 2) ^ (r >> 3)) & 1); }
 __device__ inline uint32_t swz_elem(int r, int c) {
   return uint32_t(r * 256 + ((swz_perm(c >> 3) ^ swz_f(r & 15)) << 4) + (c & 7) * 2);
+}
+
+// dma16 with an address of its own for every lane.
+__device__ inline void dma16_at(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
 }
 
 // dma16 of the lanes in `mask` only (the whole wave is active around it).
@@ -144,7 +108,7 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
   __shared__ uint4 sQ[kQRing][UQ * 16];
   __shared__ uint4 sO[kORing][UQ * 16];
   __shared__ uint4 sP[2][kKW][NB * 2][64];     // P operands of a unit: [parity][wave pair][block, kk][lane]
-  __shared__ float sLD[kLRing][2 * kT];        // the record's -LSE/scale, then -delta, per unit
+  __shared__ float sLD[kLRing][2 * kT];        // the seeds of the unit's 128 rows, per unit
 
   const int H = a.kv_heads, G = a.group, BH = a.batch * H;
   const int bh = blockIdx.x % BH;
@@ -173,7 +137,7 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
   const int lane = tid & 63, hl = lane >> 5, ln = lane & 31, rp = lane & 15, gg = (lane >> 4) & 1;
   const int key = t * kT + kw * 32 + ln;       // this lane's key (result column)
   const bool key_ok = key < len;
-  const uint8_t* qbase = a.work + size_t(bh) * a.tiles * kRecord;
+  const uint8_t* seeds = a.work + size_t(bh) * a.tiles * kSeeds;
 
   bf16x8 bop[8];                               // B operands of the wave's keys: K (group 0) or V rows
   {
@@ -194,39 +158,67 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
   const int64_t all_lo = int64_t(k_first + 31) * G;
   const int64_t all_hi = a.window == 0 || k_first + 31 < a.sinks ? INT64_MAX : (int64_t(k_first) + a.window) * G;
 
-  // Copies of a unit: Q and dO rows, and the record's per-row values.  Copy i of wave w
-  // fills LDS chunks [64*(W i + w), +64), rows 4(W i + w) + lane/16, whose low four
-  // bits do not depend on i.
-  uint32_t voff;
-  {
-    const int r = 4 * wave + (lane >> 4);
-    voff = uint32_t(r * 256 + swz_perm((lane & 15) ^ swz_f(r & 15)) * 16);
-  }
+  // Copies of a unit: Q and dO rows, and the seeds.  Copy i of wave w fills LDS chunks
+  // [64*(8 i + w), +64), rows 32 i + 4 w + lane/16, whose low four bits do not depend
+  // on i.  A row is found from the unit's first token and that token's rows before the
+  // unit, which advance with the units; rows past the last give way to it.
+  const int lr = 4 * wave + (lane >> 4);
+  const uint32_t chunk = uint32_t(swz_perm((lane & 15) ^ swz_f(lr & 15)) * 16);
   const uint32_t lq0 = lds_addr(&sQ[0][0]), lo0 = lds_addr(&sO[0][0]), ll0 = lds_addr(&sLD[0][0]);
+  const uint8_t* const qb = reinterpret_cast<const uint8_t*>(a.q + int64_t(b) * a.q_batch + int64_t(h) * G * a.q_head);
+  const uint8_t* const ob = reinterpret_cast<const uint8_t*>(a.dout + (size_t(b) * a.tokens * a.q_heads + size_t(h) * G) * kD);
+  const float per_g = 1.f / float(G);
+  const uint32_t qt2 = uint32_t(a.q_token) * 2, qh2 = uint32_t(a.q_head) * 2, ot2 = uint32_t(a.q_heads) * (kD * 2);
+  int nu = first, nt = int(int64_t(first) * UQ / G), nr = int(int64_t(first) * UQ - int64_t(nt) * G);
   struct Source {
-    const uint8_t* rec;
-    uint32_t half, qslot, oslot;
+    const uint8_t *qbase, *obase, *seeds;
+    uint32_t qslot, oslot;
+    int r0, top;
   };
-  // Past the end the last unit is copied again, into a slot that nothing reads any more.
-  auto source = [&](int s, uint32_t qslot, uint32_t oslot) {
-    const uint32_t u = uint32_t(first + min(s, U - 1));
-    return Source{qbase + size_t(u >> 1) * kRecord, (u & 1) * UB, qslot, oslot};
+  struct Place {                               // the lane's row of a copy
+    const uint8_t* q;
+    uint32_t o;
+  };
+  // The next unit's; past the end the last one is copied again, into a slot that nothing reads any more.
+  auto source = [&](uint32_t qslot, uint32_t oslot) {
+    Source s;
+    s.qbase = qb + int64_t(nt) * a.q_token * 2;
+    s.obase = ob + int64_t(nt) * ot2;
+    s.seeds = seeds + size_t(nu >> 1) * kSeeds;
+    s.qslot = qslot;
+    s.oslot = oslot;
+    s.r0 = nr;
+    s.top = len * G - 1 - nt * G;
+    if (nu + 1 < first + U) {
+      ++nu;
+      nr += UQ % G;
+      nt += UQ / G;
+      if (nr >= G) nr -= G, ++nt;
+    }
+    return s;
+  };
+  auto locate = [&](const Source& s, int i) {
+    const int rel = min(s.r0 + 32 * i + lr, s.top);   // below 64 + G <= 2^17: the quotient is exact in fp32
+    const uint32_t tok = uint32_t((float(rel) + 0.5f) * per_g), g = uint32_t(rel) - tok * uint32_t(G);
+    return Place{s.qbase + (uint64_t(tok) * qt2 + (uint64_t(g) * qh2 + chunk)), tok * ot2 + g * (kD * 2) + chunk};
   };
   constexpr int kIssue = 2 * kCopies + 1;      // copies of a wave per unit
-  auto issue = [&](const Source& c, int k) {
+  auto issue = [&](const Source& c, const Place& p, int k) {
     if (k == 2 * kCopies) {
       constexpr uint32_t share = 2 * kT * 4 / W;
-      dma16_low(c.rec + 2 * kTile + uint32_t(wave) * share, uint32_t(lane) * 16u,
+      dma16_low(c.seeds + uint32_t(wave) * share, uint32_t(lane) * 16u,
                 ll0 + c.qslot * uint32_t(sizeof(sLD[0])) + uint32_t(wave) * share, (uint64_t(1) << (share / 16)) - 1);
       return;
     }
-    const uint32_t at = uint32_t(k >> 1) * W * 1024u;
-    dma16(c.rec + (k & 1) * kTile + c.half + at, voff,
-          ((k & 1) ? lo0 + c.oslot * UB : lq0 + c.qslot * UB) + uint32_t(wave) * 1024u + at);
+    const uint32_t at = uint32_t(wave) * 1024u + uint32_t(k >> 1) * W * 1024u;
+    if (k & 1)
+      dma16(c.obase, p.o, lo0 + c.oslot * UB + at);
+    else
+      dma16_at(p.q, lq0 + c.qslot * UB + at);
   };
   auto issue_all = [&](const Source& c) {
 #pragma unroll
-    for (int k = 0; k < kIssue; ++k) issue(c, k);
+    for (int k = 0; k < kIssue; ++k) issue(c, locate(c, k >> 1 < kCopies ? k >> 1 : 0), k);
   };
 
   f32x16 acc[4];                               // dV^T (group 0) or dK^T (group 1): [dim block][32 dims x 32 keys]
@@ -305,6 +297,7 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
   auto unit0 = [&](int row, uint32_t ld, uint32_t par, const Source& next) {
     f32x16 sv[NB];
     bf16x8 op[NB][2], x[kAll];
+    Place at{};
     seed(ld, sv);
     const bool full = row >= all_lo && row + UQ <= all_hi;
     uint64_t see = 0;
@@ -328,17 +321,19 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
       if ((e & 3) == 3) pslot[par * kPStep + (qb * 2 + (e >> 2)) * 64] = __builtin_bit_cast(uint4, hand);
     };
     fence();
-#pragma unroll
-    for (int i = 0; i < kAll; ++i) {
-      if (i == 8) mask(0);
-      if (i == 16) mask(1);
-      if (i < kRows) row_product(i, x[i], sv);
+    each<0, kAll>([&](auto ic) __attribute__((always_inline)) {
+      constexpr int i = decltype(ic)::value;
+      if constexpr (i == 8) mask(0);
+      if constexpr (i == 16) mask(1);
+      if constexpr (i < kRows) row_product(i, x[i], sv);
       else tr_product(i, x[i], op);
-      if (i + kAhead < kAll) x[i + kAhead] = load(i + kAhead);
-      if (i >= 8 && i < kAll - 8) weights((i - 8) >> 3, i & 7);
-      if (i % kGap == kGap - 1 && i / kGap < kIssue) issue(next, i / kGap);
+      if constexpr (i + kAhead < kAll) x[i + kAhead] = load(i + kAhead);
+      if constexpr (i >= 8 && i < kAll - 8) weights((i - 8) >> 3, i & 7);
+      if constexpr (i == 2) at = locate(next, 0);
+      if constexpr (i == 2 + 2 * kGap) at = locate(next, 1);
+      if constexpr (i % kGap == kGap - 1 && i / kGap < kIssue) issue(next, at, i / kGap);
       fence();
-    }
+    });
   };
   // Group 1: dP - delta of a unit (kDp) into nv, and dS (from the P slot and the dP of
   // the unit before, ov) and dK of that unit (kDk).
@@ -348,6 +343,7 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     constexpr int i0 = kDp ? 0 : kRows, i1 = kDk ? kAll : kRows;
     f16x8 pk[NB][2];
     bf16x8 op[NB][2], x[kAll];
+    Place at{};
     if (kDk) {
 #pragma unroll
       for (int qb = 0; qb < NB; ++qb)
@@ -367,15 +363,17 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
 #pragma unroll
       for (int k = 0; k < kRows; ++k) ds(k >> 3, k & 7);
     }
-#pragma unroll
-    for (int i = i0; i < i1; ++i) {
-      if (i < kRows) row_product(i, x[i], nv);
+    each<i0, i1>([&](auto ic) __attribute__((always_inline)) {
+      constexpr int i = decltype(ic)::value;
+      if constexpr (i < kRows) row_product(i, x[i], nv);
       else tr_product(i, x[i], op);
-      if (i + kAhead < i1) x[i + kAhead] = load(i + kAhead);
-      if (kDk && i < kRows) ds(i >> 3, i & 7);
-      if (kDp && kDk && i % kGap == kGap - 1 && i / kGap < kIssue) issue(next, i / kGap);
+      if constexpr (i + kAhead < i1) x[i + kAhead] = load(i + kAhead);
+      if constexpr (kDk && i < kRows) ds(i >> 3, i & 7);
+      if constexpr (kDp && kDk && i == 2) at = locate(next, 0);
+      if constexpr (kDp && kDk && i == 2 + 2 * kGap) at = locate(next, 1);
+      if constexpr (kDp && kDk && i % kGap == kGap - 1 && i / kGap < kIssue) issue(next, at, i / kGap);
       fence();
-    }
+    });
   };
   auto run = [&](auto group) {
     constexpr int G0 = decltype(group)::value;
@@ -384,7 +382,7 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     auto phase = [&](int s, auto start) {
       constexpr bool kFirst = decltype(start)::value;
       // unit s has landed; the slots of unit s+2 are free
-      const Source next = source(s + 2, uint32_t(s + 2) & 3u, om == 0 ? 2u : om - 1u);
+      const Source next = source(uint32_t(s + 2) & 3u, om == 0 ? 2u : om - 1u);
       const uint32_t ld = ld0 + (uint32_t(s) & 3u) * uint32_t(sizeof(sLD[0])) + uint32_t((first + s) & 1) * uint32_t(4 * UQ);
       if constexpr (G0 == 0) {
         unit0((first + s) * UQ, ld, uint32_t(s) & 1u, next);
@@ -412,8 +410,8 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0)); // no copy outlives the workgroup
   };
   if (U > 0) {
-    issue_all(source(0, 0, 0));
-    issue_all(source(1, 1, 1));
+    issue_all(source(0, 0));
+    issue_all(source(1, 1));
     if (grp == 0) run(std::integral_constant<int, 0>{});
     else run(std::integral_constant<int, 1>{});
   }
@@ -517,16 +515,37 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
   const int pmin = w0 / G, pmax = (min(w0 + 32, rows) - 1) / G;
   const int pos = min(int(uint32_t(row) / uint32_t(G)), pmax);
 
-  const uint8_t* rec = a.work + (size_t(bh) * a.tiles + tile) * kRecord;
+  // Q^T and dO^T: lane holds row ln, dims 16 ks + 8 hl ..; delta from the chunks of dO and O
   bf16x8 qf[8], of[8];
+  float nl = -INFINITY, nd = 0.f;
+  {
+    const int t = min(int(uint32_t(row) / uint32_t(G)), len - 1), head = h * G + (row < rows ? row - t * G : 0);
+    const uint16_t* qp = a.q + int64_t(b) * a.q_batch + int64_t(t) * a.q_token + int64_t(head) * a.q_head + 8 * hl;
+    const size_t off = ((size_t(b) * a.tokens + t) * a.q_heads + head) * kD + 8 * hl;
+    uint4 vo[8];
 #pragma unroll
-  for (int ks = 0; ks < 8; ++ks) {
-    qf[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(rec + size_t(q) * 256 + (2 * ks + hl) * 16));
-    of[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(rec + kTile + size_t(q) * 256 + (2 * ks + hl) * 16));
+    for (int ks = 0; ks < 8; ++ks) {
+      qf[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qp + 16 * ks));
+      of[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(a.dout + off + 16 * ks));
+      vo[ks] = *reinterpret_cast<const uint4*>(a.o + off + 16 * ks);
+    }
+    if (row < rows) nl = -a.lse[(size_t(b) * a.q_heads + head) * a.tokens + t] / a.scale;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      const uint32_t o[4] = {vo[ks].x, vo[ks].y, vo[ks].z, vo[ks].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        nd -= bf16f(o[e] & 0xffffu) * float(of[ks][2 * e]) + bf16f(o[e] >> 16) * float(of[ks][2 * e + 1]);
+    }
+    nd = pair_sum(nd);
+    if (hl == 0) {
+      float* seeds = reinterpret_cast<float*>(a.work + (size_t(bh) * a.tiles + tile) * kSeeds);
+      seeds[q] = nl;
+      seeds[kT + q] = nd;
+    }
   }
   const float c2 = a.scale_log2;
-  const float nl = reinterpret_cast<const float*>(rec + 2 * kTile)[q] * c2;
-  const float nd = reinterpret_cast<const float*>(rec + 2 * kTile)[kT + q];
+  nl *= c2;
 
   const uint32_t lds0 = lds_addr(&sbuf[0][0]);
   uint32_t kr[4], kt[2][2];                            // K rows (V rows 16 KB behind); K transposed
@@ -584,7 +603,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
   for (int mb = 0; mb < 4; ++mb) dqt[mb] = f32x16{};
 
   // Products of a unit: S0, dP0, S1, dP1, dQ0, dQ1 (eight each, per 32-key block).
-  constexpr int kSP = 32, kReads = 4;
+  constexpr int kSP = 32, kReads = 2;
   auto load = [&](int k) -> bf16x8 {
     if (k < kSP) {
       const int n = k >> 4, ks = k & 7;
@@ -716,29 +735,26 @@ Cut cut_of(const BwdArgs& a) {
   c.parts = (end - first + c.part_units - 1) / c.part_units;
   return c;
 }
-size_t record_bytes(const BwdArgs& a) { return size_t(a.batch) * a.kv_heads * a.tiles * kRecord; }
+size_t seed_bytes(const BwdArgs& a) { return size_t(a.batch) * a.kv_heads * a.tiles * kSeeds; }
 
 }  // namespace
 
 size_t bwd_work_bytes(const BwdArgs& a) {
   const Cut c = cut_of(a);
-  return record_bytes(a) + size_t(a.batch) * a.kv_heads * c.split * c.parts * kPartial;
+  return seed_bytes(a) + size_t(a.batch) * a.kv_heads * c.split * c.parts * kPartial;
 }
 
 hipError_t launch_window_bwd(const BwdArgs& a, hipStream_t stream) {
   const Cut c = cut_of(a);
   const unsigned BH = unsigned(a.batch) * unsigned(a.kv_heads);
-  float* partials = reinterpret_cast<float*>(a.work + record_bytes(a));
-  prep_kernel<<<BH * unsigned(a.tiles), 256, 0, stream>>>(a);
+  float* partials = reinterpret_cast<float*>(a.work + seed_bytes(a));
+  dq_kernel<<<BH * unsigned(a.tiles), 256, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   dkdv_kernel<<<BH * unsigned(c.split * c.parts + c.tiles - c.split), 512, 0, stream>>>(a, c, partials);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (c.split > 0) {
-    sum_kernel<<<BH * unsigned(c.split) * 32u, 256, 0, stream>>>(a, c, partials);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  dq_kernel<<<BH * unsigned(a.tiles), 256, 0, stream>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess || c.split == 0) return e;
+  sum_kernel<<<BH * unsigned(c.split) * 32u, 256, 0, stream>>>(a, c, partials);
   return hipGetLastError();
 }
 

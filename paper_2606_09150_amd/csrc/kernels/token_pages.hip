@@ -5,6 +5,8 @@
 // page tables name; nothing is computed.  What bounds the larger calls is HBM, the
 // smaller ones launch latency.  Page numbers and positions come from device memory
 // and are checked before they are used: what lies outside is skipped, or read as zeros.
+#include <cstring>
+
 #include "../launch_tokens.h"
 
 namespace uf {
@@ -19,16 +21,18 @@ __device__ inline size_t page_rows(const Pool& p, int page, int kv, int h) {
   return ((size_t(page) * 2 + kv) * p.kv_heads + h) * size_t(p.page_tokens) * (kD * 2);
 }
 
-__global__ __launch_bounds__(1024) void poke_kernel(PokeArgs a) {
+template <int N>
+__global__ __launch_bounds__(1024) void poke_kernel(Worded<PokeHead, N> a) {
   for (int i = threadIdx.x; i < a.dense; i += 1024) a.table[a.dense_at + i] = a.words[i];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   for (int r = wave; r < a.n_runs; r += 16) {
-    const int at = a.words[a.runs + 3 * r], n = a.words[a.runs + 3 * r + 1], from = a.words[a.runs + 3 * r + 2];
-    for (int i = lane; i < n; i += 64) a.table[at + i] = a.words[from + i];
+    const int at = a.words[a.runs + 3 * r], n = a.words[a.runs + 3 * r + 1], value = a.words[a.runs + 3 * r + 2];
+    for (int i = lane; i < n; i += 64) a.table[at + i] = value < 0 ? value : value + i;
   }
 }
 
-__global__ __launch_bounds__(kThreads) void rows_kernel(RowsArgs a) {
+template <int N>
+__global__ __launch_bounds__(kThreads) void rows_kernel(Worded<RowsHead, N> a) {
   const int b = blockIdx.x;
   const int from = a.words[3 * b], to = a.words[3 * b + 1], n = a.words[3 * b + 2];
   for (int i = threadIdx.x; i < n; i += kThreads) a.table[to + i] = a.table[from + i];
@@ -36,8 +40,8 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(RowsArgs a) {
 
 // One workgroup per (page, K or V, head; layer).  Loads before stores: the stores
 // could alias them as far as the compiler knows.
-template <int T>
-__global__ __launch_bounds__(kThreads) void copy_pages_kernel(CopyArgs a) {
+template <int T, int N>
+__global__ __launch_bounds__(kThreads) void copy_pages_kernel(Worded<CopyHead, N> a) {
   const int heads = 2 * a.pool.kv_heads;
   const int i = blockIdx.x / heads, kvh = blockIdx.x % heads;
   const int rows = a.words[3 * i + 2];
@@ -62,7 +66,7 @@ __global__ __launch_bounds__(kThreads) void copy_pages_kernel(CopyArgs a) {
 
 // Row at position `pos` of the sequence whose pages start at table[seq_row]: null
 // where there is none.
-__device__ inline const uint4* row_at(const KeepArgs& a, const uint8_t* base, int seq_row, int length, int pos, int kvh) {
+__device__ inline const uint4* row_at(const KeepHead& a, const uint8_t* base, int seq_row, int length, int pos, int kvh) {
   if (pos < 0 || pos >= length) return nullptr;
   const int page = a.table[size_t(seq_row) + pos / a.pool.page_tokens];
   if (uint32_t(page) >= uint32_t(a.pool.n_pages)) return nullptr;
@@ -71,7 +75,8 @@ __device__ inline const uint4* row_at(const KeepArgs& a, const uint8_t* base, in
 
 // Up to kInPlace rows of a sequence: one workgroup per (sequence, K or V, head; layer)
 // holds them all before it stores any.
-__global__ __launch_bounds__(kThreads) void keep_in_place_kernel(KeepArgs a) {
+template <int N>
+__global__ __launch_bounds__(kThreads) void keep_in_place_kernel(Worded<KeepHead, N> a) {
   static_assert(kInPlace * kRowChunks == kThreads, "a chunk each");
   const int heads = 2 * a.pool.kv_heads;
   const int32_t* w = a.words + kKeepWords * (blockIdx.x / heads);
@@ -90,11 +95,11 @@ __global__ __launch_bounds__(kThreads) void keep_in_place_kernel(KeepArgs a) {
 }
 
 // Rows into fresh pages: one workgroup per (page, K or V, head; layer).
-template <int T>
-__global__ __launch_bounds__(kThreads) void keep_fresh_kernel(KeepArgs a) {
+template <int T, int N>
+__global__ __launch_bounds__(kThreads) void keep_fresh_kernel(Worded<KeepHead, N> a) {
   const int heads = 2 * a.pool.kv_heads;
   const int i = blockIdx.x / heads, kvh = blockIdx.x % heads;
-  int lo = 0, hi = a.n - 1;                  // the last sequence whose pages start at or before page i
+  int lo = 0, hi = a.n - 1;                  // the last run whose pages start at or before page i
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (a.words[kKeepWords * mid + 6] <= i) lo = mid;
@@ -103,7 +108,7 @@ __global__ __launch_bounds__(kThreads) void keep_fresh_kernel(KeepArgs a) {
   const int32_t* w = a.words + kKeepWords * lo;
   const int page = w[5] + i - w[6];          // of the sequence
   uint8_t* base = a.pool.base + size_t(blockIdx.y) * a.pool.layer_bytes;
-  uint4* dst = reinterpret_cast<uint4*>(base + page_rows(a.pool, a.words[a.pages + i], 0, kvh));
+  uint4* dst = reinterpret_cast<uint4*>(base + page_rows(a.pool, w[7] + i - w[6], 0, kvh));
   const int start = w[2], end = start + w[3];
   const int c = threadIdx.x % kRowChunks, r0 = threadIdx.x / kRowChunks;
   constexpr int kPer = T * kRowChunks / kThreads;
@@ -209,36 +214,66 @@ __global__ __launch_bounds__(kThreads) void write_kernel(WriteArgs a, int per) {
 
 }  // namespace
 
-hipError_t launch_poke(const PokeArgs& a, hipStream_t stream) {
-  poke_kernel<<<1, 1024, 0, stream>>>(a);
+namespace {
+
+template <class Head>
+Worded<Head, kFew> few(const Worded<Head, kWords>& a) {
+  Worded<Head, kFew> f;
+  static_cast<Head&>(f) = a;
+  std::memcpy(f.words, a.words, sizeof(f.words));
+  return f;
+}
+
+}  // namespace
+
+hipError_t launch_poke(const PokeArgs& a, int used, hipStream_t stream) {
+  if (used <= kFew)
+    poke_kernel<kFew><<<1, 1024, 0, stream>>>(few(a));
+  else
+    poke_kernel<kWords><<<1, 1024, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_rows(const RowsArgs& a, hipStream_t stream) {
-  rows_kernel<<<unsigned(a.n), kThreads, 0, stream>>>(a);
+  if (3 * a.n <= kFew)
+    rows_kernel<kFew><<<unsigned(a.n), kThreads, 0, stream>>>(few(a));
+  else
+    rows_kernel<kWords><<<unsigned(a.n), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t stream) {
   const dim3 grid(unsigned(a.n) * 2 * unsigned(a.pool.kv_heads), unsigned(a.pool.layers));
-  if (a.pool.page_tokens == 128)
-    copy_pages_kernel<128><<<grid, kThreads, 0, stream>>>(a);
-  else
-    copy_pages_kernel<64><<<grid, kThreads, 0, stream>>>(a);
+  const bool wide = a.pool.page_tokens == 128;
+  if (3 * a.n <= kFew) {
+    if (wide) copy_pages_kernel<128, kFew><<<grid, kThreads, 0, stream>>>(few(a));
+    else copy_pages_kernel<64, kFew><<<grid, kThreads, 0, stream>>>(few(a));
+  } else {
+    if (wide) copy_pages_kernel<128, kWords><<<grid, kThreads, 0, stream>>>(a);
+    else copy_pages_kernel<64, kWords><<<grid, kThreads, 0, stream>>>(a);
+  }
   return hipGetLastError();
 }
 
 hipError_t launch_keep_in_place(const KeepArgs& a, hipStream_t stream) {
-  keep_in_place_kernel<<<dim3(unsigned(a.n) * 2 * unsigned(a.pool.kv_heads), unsigned(a.pool.layers)), kThreads, 0, stream>>>(a);
+  const dim3 grid(unsigned(a.n) * 2 * unsigned(a.pool.kv_heads), unsigned(a.pool.layers));
+  if (kKeepWords * a.n <= kFew)
+    keep_in_place_kernel<kFew><<<grid, kThreads, 0, stream>>>(few(a));
+  else
+    keep_in_place_kernel<kWords><<<grid, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_keep_fresh(const KeepArgs& a, hipStream_t stream) {
   const dim3 grid(unsigned(a.n_pages) * 2 * unsigned(a.pool.kv_heads), unsigned(a.pool.layers));
-  if (a.pool.page_tokens == 128)
-    keep_fresh_kernel<128><<<grid, kThreads, 0, stream>>>(a);
-  else
-    keep_fresh_kernel<64><<<grid, kThreads, 0, stream>>>(a);
+  const bool wide = a.pool.page_tokens == 128;
+  if (kKeepWords * a.n <= kFew) {
+    if (wide) keep_fresh_kernel<128, kFew><<<grid, kThreads, 0, stream>>>(few(a));
+    else keep_fresh_kernel<64, kFew><<<grid, kThreads, 0, stream>>>(few(a));
+  } else {
+    if (wide) keep_fresh_kernel<128, kWords><<<grid, kThreads, 0, stream>>>(a);
+    else keep_fresh_kernel<64, kWords><<<grid, kThreads, 0, stream>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -14,8 +14,9 @@ constexpr int kD = 128;
 constexpr int kMaxTree = 64;      // nodes of a tree: bits of a node's word
 constexpr int kInPlace = 16;      // rows that uft_keep moves in place
 
-// Words of host metadata that ride in a launch's arguments.
-constexpr int kWords = 880;
+// Words of host metadata that ride in a launch's arguments: kWords at most, and where
+// kFew do, a launch with arguments of that size (a host copy of 3.5 KB less).
+constexpr int kWords = 880, kFew = 64;
 
 // The device tables: the step (kHeader words, of which the first is its number of
 // sequences, then kEntry words for each: sequence, first token of the step, tokens,
@@ -23,48 +24,51 @@ constexpr int kWords = 880;
 constexpr int kHeader = 4;
 constexpr int kEntry = 4;
 
-// words[0 .. dense) go to table[dense_at ..]; then n_runs runs: (at, count, first
-// word) triples from words[runs] on.
-struct PokeArgs {
-  int32_t* table;
-  int32_t dense_at, dense, runs, n_runs;
-  int32_t words[kWords];
-};
-hipError_t launch_poke(const PokeArgs& a, hipStream_t stream);
-
-// table rows: (source offset, target offset, count) triples
-struct RowsArgs {
-  int32_t* table;
-  int32_t n;
-  int32_t words[kWords];
-};
-hipError_t launch_rows(const RowsArgs& a, hipStream_t stream);
-
 struct Pool {
   uint8_t* base;            // of the layer, or of layer 0
   size_t layer_bytes;
   int32_t layers, n_pages, kv_heads, page_tokens;
 };
 
+// words[0 .. dense) go to table[dense_at ..]; then n_runs runs from words[runs] on:
+// (at, count, value), of ascending values from `value` on.
+struct PokeHead {
+  int32_t* table;
+  int32_t dense_at, dense, runs, n_runs;
+};
+// table rows: (source offset, target offset, count) triples
+struct RowsHead {
+  int32_t* table;
+  int32_t n;
+};
 // (source page, target page, rows) triples, every layer
-struct CopyArgs {
+struct CopyHead {
   Pool pool;
   int32_t n;
-  int32_t words[kWords];
 };
-hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t stream);
-
-// uft_keep.  In place: kKeepWords words a sequence: table offset, length, start,
-// count, first index.  Into fresh pages: the same words, the first page written and
-// how many of the launch's pages came before; then the pages from words[pages] on.
-constexpr int kKeepWords = 7;
-struct KeepArgs {
+// uft_keep.  In place: kKeepWords words a sequence: table offset, length, start, count,
+// first index.  Into fresh pages: the same for a run of pages that follow one another,
+// then the sequence's page that the run begins with, how many of the launch's pages
+// came before, and the run's first page.
+constexpr int kKeepWords = 8;
+struct KeepHead {
   Pool pool;
   const int32_t* table;     // page table of all sequences
   const int32_t* index;
-  int32_t n, pages, n_pages, row;
-  int32_t words[kWords];
+  int32_t n, n_pages, row;
 };
+template <class Head, int N>
+struct Worded : Head {
+  int32_t words[N];
+};
+using PokeArgs = Worded<PokeHead, kWords>;
+using RowsArgs = Worded<RowsHead, kWords>;
+using CopyArgs = Worded<CopyHead, kWords>;
+using KeepArgs = Worded<KeepHead, kWords>;
+// `used`: words of a that hold something
+hipError_t launch_poke(const PokeArgs& a, int used, hipStream_t stream);
+hipError_t launch_rows(const RowsArgs& a, hipStream_t stream);
+hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t stream);
 hipError_t launch_keep_in_place(const KeepArgs& a, hipStream_t stream);
 hipError_t launch_keep_fresh(const KeepArgs& a, hipStream_t stream);
 

@@ -161,65 +161,41 @@ class Poke {
  public:
   explicit Poke(const uft_cache* c) : c_(c) {}
   std::vector<int32_t> dense;   // from word 0 of the table on
+  // values for table words at ..: runs of ascending pages, or of -1
   void run(int32_t at, const int32_t* values, int32_t n) {
-    runs_.push_back({at, n, int32_t(values_.size())});
-    values_.insert(values_.end(), values, values + n);
+    for (int32_t i = 0; i < n;) {
+      int32_t e = i + 1;
+      while (e < n && values[e] == (values[i] < 0 ? values[i] : values[i] + e - i)) ++e;
+      runs_.insert(runs_.end(), {at + i, e - i, values[i]});
+      i = e;
+    }
   }
   int send(hipStream_t stream) {
     if (c_->dry()) return UF_OK;
-    size_t di = 0, ri = 0;
-    int32_t done = 0;           // words of run ri that were sent
-    while (di < dense.size() || ri < runs_.size()) {
-      tok::PokeArgs a{};
+    for (size_t di = 0, ri = 0; di < dense.size() || ri < runs_.size();) {
+      tok::PokeArgs a;
       a.table = c_->table;
       a.dense_at = int32_t(di);
-      a.dense = int32_t(std::min(dense.size() - di, size_t(tok::kWords)));
+      a.dense = a.runs = int32_t(std::min(dense.size() - di, size_t(tok::kWords)));
       std::copy_n(dense.begin() + di, a.dense, a.words);
       di += size_t(a.dense);
-      // the runs' triples first, their words behind them
-      int32_t room = tok::kWords - a.dense, n = 0;
-      size_t r = ri;
-      int32_t off = done;
-      struct Piece { int32_t at, n, from; } pieces[tok::kWords / 4];
-      while (r < runs_.size() && room >= 4) {
-        const int32_t take = std::min(runs_[r].n - off, room - 3);
-        pieces[n++] = {runs_[r].at + off, take, runs_[r].from + off};
-        room -= 3 + take;
-        if (off + take == runs_[r].n) {
-          ++r;
-          off = 0;
-        } else {
-          off += take;
-        }
-      }
-      a.runs = a.dense;
-      a.n_runs = n;
-      int32_t at = a.runs + 3 * n;
-      for (int32_t k = 0; k < n; ++k) {
-        a.words[a.runs + 3 * k] = pieces[k].at;
-        a.words[a.runs + 3 * k + 1] = pieces[k].n;
-        a.words[a.runs + 3 * k + 2] = at;
-        std::copy_n(values_.begin() + pieces[k].from, pieces[k].n, a.words + at);
-        at += pieces[k].n;
-      }
-      ri = r;
-      done = off;
-      if (int s = check_hip(tok::launch_poke(a, stream), "table")) return s;
+      a.n_runs = int32_t(std::min((runs_.size() - ri) / 3, size_t(tok::kWords - a.dense) / 3));
+      std::copy_n(runs_.begin() + ri, 3 * a.n_runs, a.words + a.runs);
+      ri += size_t(3 * a.n_runs);
+      if (int s = check_hip(tok::launch_poke(a, a.dense + 3 * a.n_runs, stream), "table")) return s;
     }
     return UF_OK;
   }
 
  private:
-  struct Run { int32_t at, n, from; };
   const uft_cache* c_;
-  std::vector<Run> runs_;
-  std::vector<int32_t> values_;
+  std::vector<int32_t> runs_;   // (at, count, first value)
 };
 
 int copy_pages(const uft_cache* c, const std::vector<int32_t>& triples, hipStream_t stream) {
   if (c->dry()) return UF_OK;
   for (size_t i = 0; i < triples.size();) {
-    tok::CopyArgs a{};
+    tok::CopyArgs a;
     a.pool = c->pool_of(0);
     const size_t n = std::min(triples.size() - i, size_t(tok::kWords / 3 * 3));
     std::copy_n(triples.begin() + i, n, a.words);
@@ -246,8 +222,9 @@ int check_stride(const uft_stride* s, const char* name) {
   if (s == nullptr) return fail(UF_ERR_ARG, "%s is null", name);
   if (s->token < 0 || s->head < 0 || s->batch < 0) return fail(UF_ERR_ARG, "%s must not be negative", name);
   if (s->token % 8 || s->head % 8 || s->batch % 8) return fail(UF_ERR_ARG, "%s must be multiples of 8", name);
-  // a tile's offsets are 32-bit: 127 tokens' strides in bytes
-  if (s->token > (int64_t(1) << 23) * 2) return fail(UF_ERR_ARG, "%s.token must be at most 2^24", name);
+  // a tile's offsets are 32-bit: 64 tokens' strides in bytes
+  if (s->token > (int64_t(1) << 24)) return fail(UF_ERR_ARG, "%s.token must be at most 2^24", name);
+  if (s->head > (int64_t(1) << 30)) return fail(UF_ERR_ARG, "%s.head must be at most 2^30", name);
   return UF_OK;
 }
 
@@ -453,8 +430,9 @@ int uft_fork(uft_cache* c, int32_t n, const int32_t* src, const int32_t* dst, vo
     for (int32_t i = 0; i < n; ++i) c->seqs[size_t(dst[i])].pages.reserve(c->seqs[size_t(src[i])].pages.size());
     if (!c->dry())
       for (int32_t i = 0; i < n;) {
-        tok::RowsArgs a{};
+        tok::RowsArgs a;
         a.table = c->table;
+        a.n = 0;
         for (; i < n && a.n < tok::kWords / 3; ++i, ++a.n) {
           a.words[3 * a.n] = c->row_at(src[i]);
           a.words[3 * a.n + 1] = c->row_at(dst[i]);
@@ -558,7 +536,7 @@ int uft_keep(uft_cache* c, int32_t n, const int32_t* seqs, const int32_t* starts
     }
     if (!c->dry() && any) {
       hipStream_t st = static_cast<hipStream_t>(stream);
-      tok::KeepArgs a{};
+      tok::KeepArgs a;
       a.pool = c->pool_of(0);
       a.table = c->table + c->rows_at();
       a.index = d_index;
@@ -580,31 +558,27 @@ int uft_keep(uft_cache* c, int32_t n, const int32_t* seqs, const int32_t* starts
         if (a.n > 0)
           if (int s = check_hip(tok::launch_keep_in_place(a, st), "keep")) return s;
       }
-      // fresh pages: sequences' words from the front, their pages from the back
-      int32_t done = 0;            // pages of sequence i that were sent
-      for (int32_t i = 0; i < n;) {
-        a.n = a.n_pages = 0;
-        std::vector<int32_t> pages;
-        for (; i < n; ++i) {
-          const Move& m = moves[size_t(i)];
-          if (!m.fresh) continue;
-          const int32_t room = tok::kWords - tok::kKeepWords * (a.n + 1) - int32_t(pages.size());
-          if (room < 1) break;
-          const int32_t take = std::min(room, int32_t(m.pages.size()) - done);
+      // fresh pages, run by run
+      a.n = a.n_pages = 0;
+      for (int32_t i = 0; i < n; ++i) {
+        const Move& m = moves[size_t(i)];
+        for (size_t k = 0; k < m.pages.size();) {
+          size_t e = k + 1;
+          while (e < m.pages.size() && m.pages[e] == m.pages[k] + int32_t(e - k)) ++e;
           int32_t* w = words(i);
-          w[5] = m.first + done;
-          w[6] = int32_t(pages.size());
-          pages.insert(pages.end(), m.pages.begin() + done, m.pages.begin() + done + take);
-          done += take;
-          if (done < int32_t(m.pages.size())) break;
-          done = 0;
+          w[5] = m.first + int32_t(k);
+          w[6] = a.n_pages;
+          w[7] = m.pages[k];
+          a.n_pages += int32_t(e - k);
+          k = e;
+          if (a.n == tok::kWords / tok::kKeepWords) {
+            if (int s = check_hip(tok::launch_keep_fresh(a, st), "keep")) return s;
+            a.n = a.n_pages = 0;
+          }
         }
-        if (a.n == 0) continue;
-        a.pages = tok::kKeepWords * a.n;
-        a.n_pages = int32_t(pages.size());
-        std::copy(pages.begin(), pages.end(), a.words + a.pages);
-        if (int s = check_hip(tok::launch_keep_fresh(a, st), "keep")) return s;
       }
+      if (a.n > 0)
+        if (int s = check_hip(tok::launch_keep_fresh(a, st), "keep")) return s;
       if (int s = poke.send(st)) return s;
     }
     if (in_step(c, n, seqs)) end_step(c);
@@ -750,27 +724,35 @@ struct Launch {
   size_t work_rows = 0;
 };
 
+// How a launch's time goes with its workgroups, in units of keys, measured.
+struct Cost {
+  int64_t slots;      // workgroups that run side by side
+  double alone;       // time of a unit where a compute unit has one workgroup, of its time where it has all it holds
+  double fixed;       // a workgroup's loads of queries, tables and its stores
+  double join;        // the joining launch
+  double partial;     // a slice's partial results, written and read, per slice
+};
+
 // Slices: the launch takes rounds of `slots` workgroups, each as long as a slice and
-// its fixed cost (`fixed` units: the queries' loads, the merge of waves, the stores);
-// split launches add the joining launch (`join` units).
-void choose_slices(const std::vector<int32_t>& counts, int32_t heads, int64_t slots, int32_t fixed, int32_t join,
-                   Launch* l) {
+// its fixed cost; split launches add the joining launch and their partial results.
+void choose_slices(const std::vector<int32_t>& counts, int32_t heads, int64_t n_cu, const Cost& cost, Launch* l) {
   int32_t most = 1;
   for (int32_t u : counts) most = std::max(most, u);
   l->slice = most;
   l->n_split = 1;
-  if (slots <= 0 || int64_t(counts.size()) * heads >= 8 * slots) return;
+  if (n_cu <= 0 || int64_t(counts.size()) * heads >= 8 * cost.slots) return;
   static const int32_t kTry[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
-  int64_t best = INT64_MAX;
+  double best = 1e300;
   for (int32_t m : kTry) {
     const int32_t slice = (most + m - 1) / m;
     if (m > 1 && slice < 4) break;
     int64_t groups = 0;
     for (int32_t u : counts) groups += (u + slice - 1) / slice;
-    const int64_t rounds = (groups * heads + slots - 1) / slots;
-    const int64_t cost = rounds * (slice + fixed) + (m > 1 ? join : 0);
-    if (cost < best) {
-      best = cost;
+    groups *= heads;
+    const double rounds = groups <= n_cu ? cost.alone : double((groups + cost.slots - 1) / cost.slots);
+    const double time = rounds * (slice + cost.fixed) + (m > 1 ? cost.join + cost.partial * double(groups) : 0.0);
+    if (time < best) {
+      best = time;
       l->slice = slice;
       l->n_split = (most + slice - 1) / slice;
     }
@@ -823,7 +805,7 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
     p->few.most = tok::kFewRows;
     p->few.longest = int32_t(few_rows);
     p->few.tiles = 1;
-    choose_slices(few, H, d->n_cu, 6, 12, &p->few);
+    choose_slices(few, H, d->n_cu, Cost{d->n_cu, 1.0, 6.0, 8.0, 0.004}, &p->few);
     p->few.work_rows = p->few.n_split > 1 ? size_t(n) * H * p->few.n_split * tok::kFewRows : 0;
   }
   if (!rows.empty()) {
@@ -832,7 +814,7 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
     p->rows.most = INT32_MAX;
     p->rows.longest = int32_t(many_rows);
     p->rows.tiles = int32_t(tiles);
-    choose_slices(rows, H, int64_t(2) * d->n_cu, 4, 6, &p->rows);
+    choose_slices(rows, H, d->n_cu, Cost{int64_t(2) * d->n_cu, 0.72, 4.0, 2.0, 0.014}, &p->rows);
     p->rows.work_rows = p->rows.n_split > 1 ? size_t(n) * H * p->rows.n_split * size_t(tiles) * tok::kRowTile : 0;
   }
   const double grid = double(n) * H * std::max(double(tiles) * p->rows.n_split, 64.0);

@@ -39,19 +39,22 @@ def _dense(t, name, shape, dtype=torch.bfloat16, device=None):
         raise ValueError(f"{name} must be contiguous")
 
 
-def _strides(t, name):
-    """Strides (batch, token, head) in elements of a tensor [.., tokens, heads, 128]."""
+def _strides(t, name, dense=None):
+    """Strides (batch, token, head) in elements of a tensor [.., tokens, heads, 128]; ``dense`` if it is contiguous."""
+    contiguous = t.is_contiguous()
+    if contiguous and dense is not None and t.data_ptr() % 16 == 0:
+        return dense
     st = t.stride()
     if st[-1] != 1:
         raise ValueError(f"{name} must be contiguous along its last dimension")
-    if not t.is_contiguous():                            # an axis of one element is never stepped along
+    if not contiguous:                                   # an axis of one element is never stepped along
         st = [0 if n == 1 else s for n, s in zip(t.shape, st)]
     if t.data_ptr() % 16 or st[-2] % 8 or st[-3] % 8 or st[0] % 8:
         raise ValueError(f"{name} must be 16-byte aligned, with strides that are multiples of 8 elements")
     return T.uft_stride(st[0] if len(st) == 4 else 0, st[-3], st[-2])
 
 
-_current_device = torch.cuda.current_device
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (a Stream object costs more than a small call)
 
 
@@ -91,6 +94,7 @@ class TokenCache:
             self.n_cu = torch.cuda.get_device_properties(self.device).multi_processor_count
         self.handle = T.uft_create(self.desc, self.pool, self.table)
         self._step = None
+        self._dense = T.uft_stride(0, kv_heads * D, D)
 
     def close(self):
         if getattr(self, "handle", None) is not None:
@@ -132,7 +136,7 @@ class TokenCache:
     def extend(self, seqs, counts, stream=None):
         """Begin a step: sequence seqs[i] grows by counts[i] tokens."""
         self._run(stream, lambda s: T.uft_extend(self.handle, seqs, counts, s))
-        self._step = None
+        self._step = sum(counts)
 
     def write(self, layer, k, v, stream=None):
         """The step's keys and values of a layer, [step tokens, kv_heads, 128] (strided views too)."""
@@ -141,7 +145,7 @@ class TokenCache:
         shape = (self.step_tokens(), self.desc.kv_heads, D)
         _check(k, "k", shape, device=self.device)
         _check(v, "v", shape, device=self.device)
-        ks, vs = _strides(k, "k"), _strides(v, "v")
+        ks, vs = _strides(k, "k", self._dense), _strides(v, "v", self._dense)
         _enqueue(self.device, stream, lambda s: T.uft_write(self.handle, layer, k, ks, v, vs, s))
 
     def fork(self, src, dst, stream=None):
