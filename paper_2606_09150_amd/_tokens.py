@@ -1,7 +1,7 @@
 """ctypes binding of the token operators of libuf.so (include/uft.h): argument marshalling only."""
 
+import array
 import ctypes
-import operator
 
 from . import _lib as L
 
@@ -42,13 +42,13 @@ _SIGNATURES = {
     "uft_table_bytes": [ctypes.POINTER(uft_desc), _ZP],
     "uft_create": [ctypes.POINTER(uft_desc), _P, _Z, _P, _Z, ctypes.POINTER(_P)],
     "uft_destroy": [_P],
-    "uft_extend": [_P, _I, _IP, _IP, _P],
+    "uft_extend": [_P, _I, _P, _P, _P],
     "uft_write": [_P, _I, _P, ctypes.POINTER(uft_stride), _P, ctypes.POINTER(uft_stride), _P],
-    "uft_fork": [_P, _I, _IP, _IP, _P],
-    "uft_copy": [_P, _I, _IP, _IP, _P],
-    "uft_keep": [_P, _I, _IP, _IP, _IP, _P, _P],
-    "uft_trim": [_P, _I, _IP, _I, _I, _P],
-    "uft_free": [_P, _I, _IP],
+    "uft_fork": [_P, _I, _P, _P, _P],
+    "uft_copy": [_P, _I, _P, _P, _P],
+    "uft_keep": [_P, _I, _P, _P, _P, _P, _P],
+    "uft_trim": [_P, _I, _P, _I, _I, _P],
+    "uft_free": [_P, _I, _P],
     "uft_pack": [_P, _IP, _P],
     "uft_get_info": [_P, ctypes.POINTER(uft_info)],
     "uft_seq_tokens": [_P, _I, _IP],
@@ -77,12 +77,14 @@ def load():
 
 
 def _ints(values):
+    """Host integers as an array (which the caller holds during the call)."""
     if hasattr(values, "data_ptr"):
         raise TypeError("sequences, counts and starts are host integers, not a tensor")
-    try:
-        return (_I * len(values))(*values)
-    except TypeError:                        # other integers (numpy's)
-        return (_I * len(values))(*[operator.index(v) for v in values])
+    return array.array("i", values)
+
+
+def _at(ints):
+    return ints.buffer_info()[0]
 
 
 def _same(a, b, names):
@@ -121,7 +123,8 @@ def uft_destroy(handle) -> None:
 
 def uft_extend(handle, seqs, counts, stream=None) -> None:
     _same(seqs, counts, "seqs and counts")
-    L._check(load().uft_extend(handle, len(seqs), _ints(seqs), _ints(counts), stream))
+    s, c = _ints(seqs), _ints(counts)
+    L._check(load().uft_extend(handle, len(s), _at(s), _at(c), stream))
 
 
 def uft_write(handle, layer, k, k_stride, v, v_stride, stream=None) -> None:
@@ -130,26 +133,31 @@ def uft_write(handle, layer, k, k_stride, v, v_stride, stream=None) -> None:
 
 def uft_fork(handle, src, dst, stream=None) -> None:
     _same(src, dst, "src and dst")
-    L._check(load().uft_fork(handle, len(src), _ints(src), _ints(dst), stream))
+    s, d = _ints(src), _ints(dst)
+    L._check(load().uft_fork(handle, len(s), _at(s), _at(d), stream))
 
 
 def uft_copy(handle, src, dst, stream=None) -> None:
     _same(src, dst, "src and dst")
-    L._check(load().uft_copy(handle, len(src), _ints(src), _ints(dst), stream))
+    s, d = _ints(src), _ints(dst)
+    L._check(load().uft_copy(handle, len(s), _at(s), _at(d), stream))
 
 
 def uft_keep(handle, seqs, starts, counts, index=None, stream=None) -> None:
     _same(seqs, starts, "seqs and starts")
     _same(seqs, counts, "seqs and counts")
-    L._check(load().uft_keep(handle, len(seqs), _ints(seqs), _ints(starts), _ints(counts), L._ptr(index), stream))
+    s, a, c = _ints(seqs), _ints(starts), _ints(counts)
+    L._check(load().uft_keep(handle, len(s), _at(s), _at(a), _at(c), L._ptr(index), stream))
 
 
 def uft_trim(handle, seqs, window, sinks, stream=None) -> None:
-    L._check(load().uft_trim(handle, len(seqs), _ints(seqs), window, sinks, stream))
+    s = _ints(seqs)
+    L._check(load().uft_trim(handle, len(s), _at(s), window, sinks, stream))
 
 
 def uft_free(handle, seqs) -> None:
-    L._check(load().uft_free(handle, len(seqs), _ints(seqs)))
+    s = _ints(seqs)
+    L._check(load().uft_free(handle, len(s), _at(s)))
 
 
 def uft_pack(handle, stream=None) -> int:

@@ -98,7 +98,6 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
 
   // this wave's positions, and the lane's
   const int w0 = row0 + wave * 32;
-  const bool idle = w0 >= min(rows_all, p.count * G);  // no row of it sees anything
   const int pmin = tree ? p.held - 1 : p.held + w0 / G;
   const int pmax = tree ? last : p.held + min(min(w0 + 31, rows_all - 1) / G, p.count - 1);
   uint64_t node = 0;
@@ -275,29 +274,34 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
       fence();
     }
   };
-  // Whether no row of this wave sees a key of the unit.
-  auto unseen = [&](const Unit& u) {
-    return idle || u.key0 > pmax || (a.window > 0 && u.key0 + 63 < pmin - a.window + 1 && u.key0 >= a.sinks);
+  // A wave without a row only copies: in a loop of its own, since a branch around the body would have the compiler
+  // keep two sets of accumulators and move one into the other (64 registers a unit: 2 % of a long prompt).
+  const bool idle = row0 + wave * 32 >= min(rows_all, p.count * G);
+  auto walk_idle = [&](int U, auto&& entry) {
+    Unit cur = entry(0);
+    for (int u = 0; u <= U; ++u) {
+      const Offsets co = offsets(cur);
+      if (u > 0) meet<0>();
+#pragma unroll
+      for (int k = 0; k < 8; ++k) issue(cur, co, uint32_t(u) & 1u, k);
+      cur = entry(min(u + 1, U - 1));
+    }
+    meet<0>();
   };
   auto walk = [&](int U, auto&& entry) {
+    if (idle) return walk_idle(U, entry);
     Unit cur = entry(0), next = entry(U > 1 ? 1 : 0);
     {
       const Offsets co = offsets(cur);
 #pragma unroll
       for (int k = 0; k < 8; ++k) issue(cur, co, 0, k);
     }
-    for (int u = 0; u < U; ++u) {
+    int u = 0;
+    do {
       meet<0>();                                       // unit u has landed; the other buffer is free
       const uint32_t nbuf = uint32_t(u + 1) & 1u;
-      if (!unseen(cur)) {
-        body(cur, next, nbuf);                         // past the end the last unit is copied again, and not read
-        if (u == kExact - 1) bound = kSumBound;
-      } else {
-        const Offsets no = offsets(next);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) issue(next, no, nbuf, k);
-        if (u >= kExact - 1) bound = kSumBound;
-      }
+      body(cur, next, nbuf);                           // past the end the last unit is copied again, and not read
+      if (u == kExact - 1) bound = kSumBound;
       const uint32_t d = (u & 1) ? uint32_t(-int(kUnitBytes)) : kUnitBytes;
 #pragma unroll
       for (int k = 0; k < 4; ++k) kr[k] += d;
@@ -305,7 +309,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
       for (int k = 0; k < 4; ++k) vt[k >> 1][k & 1] += d;
       cur = next;
       next = entry(min(u + 2, U - 1));
-    }
+    } while (++u < U);
     if (U & 1) {                                       // the next units start in buffer 0 again
 #pragma unroll
       for (int k = 0; k < 4; ++k) kr[k] -= kUnitBytes;

@@ -511,7 +511,6 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
   const int first = row0 / G, last = (min(row0 + kT, rows) - 1) / G;
   const Range range = key_range(first, last, a.window, a.sinks, kKeyUnit);
   const int w0 = row0 + wave * 32;
-  const bool idle = w0 >= rows;
   const int pmin = w0 / G, pmax = (min(w0 + 32, rows) - 1) / G;
   const int pos = min(int(uint32_t(row) / uint32_t(G)), pmax);
 
@@ -672,9 +671,6 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
     eight(std::integral_constant<int, 32>{});
     eight(std::integral_constant<int, 40>{});
   };
-  auto unseen = [&](const Unit& u) {
-    return idle || u.key0 > pmax || (a.window > 0 && u.key0 + 63 < pmin - a.window + 1 && u.key0 >= a.sinks);
-  };
   const int U = range.count;
   Unit cur = unit_of(0), next = unit_of(min(1, U - 1));
   {
@@ -682,16 +678,11 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) issue(cur, co, 0, k);
   }
-  for (int u = 0; u < U; ++u) {
+  int u = 0;
+  do {
     meet<0>();                                         // unit u has landed; the other buffer is free
     const uint32_t nbuf = uint32_t(u + 1) & 1u;
-    if (!unseen(cur)) {
-      body(cur, next, nbuf);
-    } else {
-      const Offsets no = offsets(next);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) issue(next, no, nbuf, k);
-    }
+    body(cur, next, nbuf);                             // past the end the last unit is copied again, and not read
     const uint32_t d = (u & 1) ? uint32_t(-int(kUnitBytes)) : kUnitBytes;
 #pragma unroll
     for (int k = 0; k < 4; ++k) kr[k] += d;
@@ -699,8 +690,8 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
     for (int k = 0; k < 4; ++k) kt[k >> 1][k & 1] += d;
     cur = next;
     next = unit_of(min(u + 2, U - 1));
-  }
-  meet<0>();                                           // no copy outlives the workgroup
+  } while (++u < U);
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));           // no copy outlives the workgroup
   int r_out = row;                                     // (its address is formed here, not held across the walk)
   asm volatile("" : "+v"(r_out));
   if (r_out >= a.tokens * G) return;
