@@ -69,11 +69,6 @@ __device__ inline uint32_t swz_elem(int r, int c) {
   return uint32_t(r * 256 + ((swz_perm(c >> 3) ^ swz_f(r & 15)) << 4) + (c & 7) * 2);
 }
 
-// dma16 with an address of its own for every lane.
-__device__ inline void dma16_at(const void* p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
-}
-
 // dma16 of the lanes in `mask` only (the whole wave is active around it).
 __device__ inline void dma16_low(const void* base, uint32_t off, uint32_t lds, uint64_t mask) {
   asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1"
@@ -171,24 +166,26 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
   const uint32_t qt2 = uint32_t(a.q_token) * 2, qh2 = uint32_t(a.q_head) * 2, ot2 = uint32_t(a.q_heads) * (kD * 2);
   int nu = first, nt = int(int64_t(first) * UQ / G), nr = int(int64_t(first) * UQ - int64_t(nt) * G);
   struct Source {
-    const uint8_t *qbase, *obase, *seeds;
+    const uint8_t *q, *o, *seeds;
     uint32_t qslot, oslot;
-    int r0, top;
   };
-  struct Place {                               // the lane's row of a copy
-    const uint8_t* q;
-    uint32_t o;
-  };
+  uint32_t qoff[kCopies], ooff[kCopies];       // the lane's rows, from the unit's first token on
+  bool placed = false;
   // The next unit's; past the end the last one is copied again, into a slot that nothing reads any more.
   auto source = [&](uint32_t qslot, uint32_t oslot) {
-    Source s;
-    s.qbase = qb + int64_t(nt) * a.q_token * 2;
-    s.obase = ob + int64_t(nt) * ot2;
-    s.seeds = seeds + size_t(nu >> 1) * kSeeds;
-    s.qslot = qslot;
-    s.oslot = oslot;
-    s.r0 = nr;
-    s.top = len * G - 1 - nt * G;
+    const Source s{qb + int64_t(nt) * a.q_token * 2, ob + int64_t(nt) * ot2, seeds + size_t(nu >> 1) * kSeeds, qslot, oslot};
+    const int top = len * G - 1 - nt * G;
+    // the same for every whole unit where the heads of a group divide one
+    if (!placed || UQ % G != 0 || top < UQ - 1) {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) {
+        const int rel = min(nr + 32 * i + lr, top);    // below 64 + G <= 2^17: the quotient is exact in fp32
+        const uint32_t tok = uint32_t((float(rel) + 0.5f) * per_g), g = uint32_t(rel) - tok * uint32_t(G);
+        qoff[i] = tok * qt2 + g * qh2 + chunk;
+        ooff[i] = tok * ot2 + g * (kD * 2) + chunk;
+      }
+      placed = true;
+    }
     if (nu + 1 < first + U) {
       ++nu;
       nr += UQ % G;
@@ -197,13 +194,8 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     }
     return s;
   };
-  auto locate = [&](const Source& s, int i) {
-    const int rel = min(s.r0 + 32 * i + lr, s.top);   // below 64 + G <= 2^17: the quotient is exact in fp32
-    const uint32_t tok = uint32_t((float(rel) + 0.5f) * per_g), g = uint32_t(rel) - tok * uint32_t(G);
-    return Place{s.qbase + (uint64_t(tok) * qt2 + (uint64_t(g) * qh2 + chunk)), tok * ot2 + g * (kD * 2) + chunk};
-  };
   constexpr int kIssue = 2 * kCopies + 1;      // copies of a wave per unit
-  auto issue = [&](const Source& c, const Place& p, int k) {
+  auto issue = [&](const Source& c, int k) {
     if (k == 2 * kCopies) {
       constexpr uint32_t share = 2 * kT * 4 / W;
       dma16_low(c.seeds + uint32_t(wave) * share, uint32_t(lane) * 16u,
@@ -212,13 +204,13 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     }
     const uint32_t at = uint32_t(wave) * 1024u + uint32_t(k >> 1) * W * 1024u;
     if (k & 1)
-      dma16(c.obase, p.o, lo0 + c.oslot * UB + at);
+      dma16(c.o, ooff[k >> 1], lo0 + c.oslot * UB + at);
     else
-      dma16_at(p.q, lq0 + c.qslot * UB + at);
+      dma16(c.q, qoff[k >> 1], lq0 + c.qslot * UB + at);
   };
   auto issue_all = [&](const Source& c) {
 #pragma unroll
-    for (int k = 0; k < kIssue; ++k) issue(c, locate(c, k >> 1 < kCopies ? k >> 1 : 0), k);
+    for (int k = 0; k < kIssue; ++k) issue(c, k);
   };
 
   f32x16 acc[4];                               // dV^T (group 0) or dK^T (group 1): [dim block][32 dims x 32 keys]
@@ -297,7 +289,6 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
   auto unit0 = [&](int row, uint32_t ld, uint32_t par, const Source& next) {
     f32x16 sv[NB];
     bf16x8 op[NB][2], x[kAll];
-    Place at{};
     seed(ld, sv);
     const bool full = row >= all_lo && row + UQ <= all_hi;
     uint64_t see = 0;
@@ -329,9 +320,7 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
       else tr_product(i, x[i], op);
       if constexpr (i + kAhead < kAll) x[i + kAhead] = load(i + kAhead);
       if constexpr (i >= 8 && i < kAll - 8) weights((i - 8) >> 3, i & 7);
-      if constexpr (i == 2) at = locate(next, 0);
-      if constexpr (i == 2 + 2 * kGap) at = locate(next, 1);
-      if constexpr (i % kGap == kGap - 1 && i / kGap < kIssue) issue(next, at, i / kGap);
+      if constexpr (i % kGap == kGap - 1 && i / kGap < kIssue) issue(next, i / kGap);
       fence();
     });
   };
@@ -343,7 +332,6 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     constexpr int i0 = kDp ? 0 : kRows, i1 = kDk ? kAll : kRows;
     f16x8 pk[NB][2];
     bf16x8 op[NB][2], x[kAll];
-    Place at{};
     if (kDk) {
 #pragma unroll
       for (int qb = 0; qb < NB; ++qb)
@@ -369,9 +357,7 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
       else tr_product(i, x[i], op);
       if constexpr (i + kAhead < i1) x[i + kAhead] = load(i + kAhead);
       if constexpr (kDk && i < kRows) ds(i >> 3, i & 7);
-      if constexpr (kDp && kDk && i == 2) at = locate(next, 0);
-      if constexpr (kDp && kDk && i == 2 + 2 * kGap) at = locate(next, 1);
-      if constexpr (kDp && kDk && i % kGap == kGap - 1 && i / kGap < kIssue) issue(next, at, i / kGap);
+      if constexpr (kDp && kDk && i % kGap == kGap - 1 && i / kGap < kIssue) issue(next, i / kGap);
       fence();
     });
   };

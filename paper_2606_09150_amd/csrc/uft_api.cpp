@@ -917,6 +917,9 @@ int check_window(const uft_window_desc* d, float* log2) {
   if (int s = check_stride(&d->q, "q stride")) return s;
   if (int s = check_stride(&d->k, "k stride")) return s;
   if (int s = check_stride(&d->v, "v stride")) return s;
+  // the backward's offsets of a group's heads are 32-bit
+  if (d->q.head * (d->q_heads / d->kv_heads) > (int64_t(1) << 30))
+    return fail(UF_ERR_ARG, "the q stride's head times the query heads of a key head must be at most 2^30");
   return check_scale(d->scale, log2);
 }
 
