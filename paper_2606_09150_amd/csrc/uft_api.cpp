@@ -724,9 +724,14 @@ struct Launch {
   size_t work_rows = 0;
 };
 
-// How a launch's time goes with its workgroups, in units of keys, measured.
+// How a launch's time goes with its workgroups, in units of keys.  Measured (us, attention
+// alone): 16 sequences x 8 heads x 2 tiles of 65 units, whole 95, in two slices 89, in three
+// 103; 4 heads x 1 tile of 33 units, whole 44, slices of 5 units 15.7, of 2 14.6; few rows: one
+// sequence of 4,096 units and 8 heads, in 4 slices 410, 8 217, 16 120, 32 100, 48 115, 64 104;
+// 384 of 129 units, whole 154, in two slices 150, in four 159.
 struct Cost {
   int64_t slots;      // workgroups that run side by side
+  int32_t least;      // units of a slice at least
   double alone;       // time of a unit where a compute unit has one workgroup, of its time where it has all it holds
   double fixed;       // a workgroup's loads of queries, tables and its stores
   double join;        // the joining launch
@@ -745,7 +750,7 @@ void choose_slices(const std::vector<int32_t>& counts, int32_t heads, int64_t n_
   double best = 1e300;
   for (int32_t m : kTry) {
     const int32_t slice = (most + m - 1) / m;
-    if (m > 1 && slice < 4) break;
+    if (m > 1 && slice < cost.least) break;
     int64_t groups = 0;
     for (int32_t u : counts) groups += (u + slice - 1) / slice;
     groups *= heads;
@@ -805,7 +810,7 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
     p->few.most = tok::kFewRows;
     p->few.longest = int32_t(few_rows);
     p->few.tiles = 1;
-    choose_slices(few, H, d->n_cu, Cost{d->n_cu, 1.0, 6.0, 8.0, 0.004}, &p->few);
+    choose_slices(few, H, d->n_cu, Cost{d->n_cu, 4, 1.0, 6.0, 8.0, 0.004}, &p->few);
     p->few.work_rows = p->few.n_split > 1 ? size_t(n) * H * p->few.n_split * tok::kFewRows : 0;
   }
   if (!rows.empty()) {
@@ -814,7 +819,7 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
     p->rows.most = INT32_MAX;
     p->rows.longest = int32_t(many_rows);
     p->rows.tiles = int32_t(tiles);
-    choose_slices(rows, H, d->n_cu, Cost{int64_t(2) * d->n_cu, 0.72, 4.0, 2.0, 0.014}, &p->rows);
+    choose_slices(rows, H, d->n_cu, Cost{int64_t(2) * d->n_cu, 2, 0.72, 4.0, 2.0, 0.014}, &p->rows);
     p->rows.work_rows = p->rows.n_split > 1 ? size_t(n) * H * p->rows.n_split * size_t(tiles) * tok::kRowTile : 0;
   }
   const double grid = double(n) * H * std::max(double(tiles) * p->rows.n_split, 64.0);
