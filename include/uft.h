@@ -175,7 +175,7 @@ int uft_attn(const uft_cache* cache, int32_t layer, const uft_attn_desc* desc, c
  * [batch, q_heads, tokens] fp32 or NULL.  d_lengths, NULL or int32 [batch] (device):
  * tokens from d_lengths[b] on are padding: no key, not read, and their rows get
  * O = 0, LSE = -inf and zero gradients.  q.head times the query heads of a key head
- * is at most 2^30.  Errors: UF_ERR_ARG, UF_ERR_HIP.
+ * is at most 2^30; scale as for uft_attn, and at least 2^-100.  Errors: UF_ERR_ARG, UF_ERR_HIP.
  *
  * Backward: d_o and d_lse as the forward left them, d_do [batch, tokens, q_heads,
  * head_dim] bf16 contiguous; outputs d_dq (as q) and d_dk, d_dv (as k) bf16,

@@ -696,20 +696,24 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
 
 // The sinks' key tiles are cut into parts of about a window tile's units, so that none
 // outlasts the launch: a tile of the window is seen by (window + 127) G / 64 units, the
-// sinks' by every unit behind them.
+// sinks' by every unit behind them.  No more parts than give the sinks' tiles 1,024
+// workgroups: many such tiles fill the GPU as they are, and a part's results are 128 KB.
+constexpr int kMostParts = 1024;
 Cut cut_of(const BwdArgs& a) {
   Cut c{};
   c.tiles = (a.tokens + kT - 1) / kT;
   c.parts = 1;
   if (a.window == 0 || a.sinks == 0) return c;
+  const int sinks = (a.sinks + kT - 1) / kT < c.tiles ? (a.sinks + kT - 1) / kT : c.tiles;
   int first, end;
   unit_range(a.tokens, a.group, 0, a.window, a.sinks, &first, &end);
-  const int64_t near = (int64_t(a.window) + kT) * a.group / 64 + 1;
-  if (end - first <= 2 * near) return c;
-  c.split = (a.sinks + kT - 1) / kT < c.tiles ? (a.sinks + kT - 1) / kT : c.tiles;
-  const int64_t least = (end - first + 63) / 64;       // 64 parts at most
-  c.part_units = int(near > least ? near : least);
-  c.parts = (end - first + c.part_units - 1) / c.part_units;
+  const int64_t near = (int64_t(a.window) + kT) * a.group / 64 + 1, all = end - first;
+  const int64_t room = kMostParts / (int64_t(a.batch) * a.kv_heads * sinks);
+  const int64_t parts = all / near < room ? all / near : room;
+  if (parts < 2) return c;
+  c.split = sinks;
+  c.part_units = int((all + parts - 1) / parts);
+  c.parts = int((all + c.part_units - 1) / c.part_units);
   return c;
 }
 size_t seed_bytes(const BwdArgs& a) { return size_t(a.batch) * a.kv_heads * a.tiles * kSeeds; }

@@ -925,7 +925,10 @@ int check_window(const uft_window_desc* d, float* log2) {
   // the backward's offsets of a group's heads are 32-bit
   if (d->q.head * (d->q_heads / d->kv_heads) > (int64_t(1) << 30))
     return fail(UF_ERR_ARG, "the q stride's head times the query heads of a key head must be at most 2^30");
-  return check_scale(d->scale, log2);
+  if (int s = check_scale(d->scale, log2)) return s;
+  // the backward seeds its products with LSE / scale
+  if (d->scale < 0x1p-100f) return fail(UF_ERR_ARG, "scale must be at least 2^-100");
+  return UF_OK;
 }
 
 tok::BwdArgs bwd_args(const uft_window_desc* d, float log2) {

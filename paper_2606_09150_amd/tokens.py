@@ -41,14 +41,12 @@ def _dense(t, name, shape, dtype=torch.bfloat16, device=None):
 
 def _strides(t, name, dense=None):
     """Strides (batch, token, head) in elements of a tensor [.., tokens, heads, 128]; ``dense`` if it is contiguous."""
-    contiguous = t.is_contiguous()
-    if contiguous and dense is not None and t.data_ptr() % 16 == 0:
+    if dense is not None and t.is_contiguous() and t.data_ptr() % 16 == 0:
         return dense
-    st = t.stride()
+    # an axis of one element is never stepped along
+    st = [0 if n == 1 else s for n, s in zip(t.shape, t.stride())]
     if st[-1] != 1:
         raise ValueError(f"{name} must be contiguous along its last dimension")
-    if not contiguous:                                   # an axis of one element is never stepped along
-        st = [0 if n == 1 else s for n, s in zip(t.shape, st)]
     if t.data_ptr() % 16 or st[-2] % 8 or st[-3] % 8 or st[0] % 8:
         raise ValueError(f"{name} must be 16-byte aligned, with strides that are multiples of 8 elements")
     return T.uft_stride(st[0] if len(st) == 4 else 0, st[-3], st[-2])
@@ -58,8 +56,9 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (a Stream object costs more than a small call)
 
 
-def _enqueue(device, stream, call):
-    """``call`` with the stream's handle; the device is current meanwhile, and tensors that it makes belong to the stream."""
+def _enqueue(device, stream, call, *tensors):
+    """``call`` with the stream's handle; the device is current meanwhile, tensors that it makes belong to the stream, and
+    ``tensors``, which it works on, are kept from reuse until the stream is past it."""
     if stream is None and _current_device() == device.index:
         return call(_raw_stream(device.index))
     if stream is None:
@@ -69,6 +68,9 @@ def _enqueue(device, stream, call):
         raise TypeError("stream must be a torch.cuda.Stream")
     if stream.device != device:
         raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
     with torch.cuda.device(device), torch.cuda.stream(stream):
         return call(stream.cuda_stream)
 
@@ -93,7 +95,7 @@ class TokenCache:
             self.table = torch.empty(T.uft_table_bytes(self.desc), dtype=torch.uint8, device=self.device)
             self.n_cu = torch.cuda.get_device_properties(self.device).multi_processor_count
         self.handle = T.uft_create(self.desc, self.pool, self.table)
-        self._step = None
+        self._step, self._need = None, {}
         self._dense = T.uft_stride(0, kv_heads * D, D)
 
     def close(self):
@@ -107,8 +109,8 @@ class TokenCache:
         except Exception:
             pass
 
-    def _run(self, stream, call):
-        return call(None) if self.dry else _enqueue(self.device, stream, call)
+    def _run(self, stream, call, *tensors):
+        return call(None) if self.dry else _enqueue(self.device, stream, call, self.pool, self.table, *tensors)
 
     # -- state ----------------------------------------------------------------
     def info(self):
@@ -137,6 +139,7 @@ class TokenCache:
         """Begin a step: sequence seqs[i] grows by counts[i] tokens."""
         self._run(stream, lambda s: T.uft_extend(self.handle, seqs, counts, s))
         self._step = sum(counts)
+        self._need = {}
 
     def write(self, layer, k, v, stream=None):
         """The step's keys and values of a layer, [step tokens, kv_heads, 128] (strided views too)."""
@@ -146,7 +149,7 @@ class TokenCache:
         _check(k, "k", shape, device=self.device)
         _check(v, "v", shape, device=self.device)
         ks, vs = _strides(k, "k", self._dense), _strides(v, "v", self._dense)
-        _enqueue(self.device, stream, lambda s: T.uft_write(self.handle, layer, k, ks, v, vs, s))
+        self._run(stream, lambda s: T.uft_write(self.handle, layer, k, ks, v, vs, s), k, v)
 
     def fork(self, src, dst, stream=None):
         """Sequences dst[i] continue src[i] and share its pages until one of them grows."""
@@ -164,8 +167,8 @@ class TokenCache:
         if index is None and any(counts):
             raise ValueError("counts above 0 need an index")
         index = None if self.dry else index
-        self._run(stream, lambda s: T.uft_keep(self.handle, seqs, starts, counts, index, s))
-        self._step = None
+        self._run(stream, lambda s: T.uft_keep(self.handle, seqs, starts, counts, index, s), index)
+        self._step, self._need = None, {}
 
     def trim(self, seqs, window, sinks=0, stream=None):
         """Give back the pages that no later query of this window and these sinks sees."""
@@ -173,7 +176,7 @@ class TokenCache:
 
     def free(self, seqs):
         T.uft_free(self.handle, seqs)
-        self._step = None
+        self._step, self._need = None, {}
 
     def pack(self, stream=None):
         """Move pages so that those in use come first; returns their number."""
@@ -203,7 +206,10 @@ class TokenCache:
         if lse is not True and lse is not False and lse is not None:
             _dense(lse, "lse", (n, Hq), torch.float32, self.device)
         desc = T.uft_attn_desc(Hq, window, sinks, self.n_cu, scale, _strides(q, "q"))
-        need = T.uft_attn_work_bytes(self.handle, desc)
+        plan = (Hq, window, sinks, self.n_cu)            # the same for every layer of the step
+        need = self._need.get(plan)
+        if need is None:
+            need = self._need[plan] = T.uft_attn_work_bytes(self.handle, desc)
         if work is not None:
             _dense(work, "work", work.shape, torch.uint8, self.device)
             if work.numel() < need:
@@ -216,7 +222,7 @@ class TokenCache:
             T.uft_attn(self.handle, layer, desc, q, tree, o, sums, w, need, s)
             return o if sums is None else (o, sums)
 
-        return _enqueue(self.device, stream, call)
+        return self._run(stream, call, q, tree, out, work, lse if isinstance(lse, torch.Tensor) else None)
 
 
 def _window_desc(q, k, v, window, sinks, scale, lengths):
@@ -253,7 +259,7 @@ def window_attention(q, k, v, window=0, sinks=0, scale=None, lengths=None, out=N
         T.uft_window_fwd(desc, q, k, v, lengths, o, sums, s)
         return o if sums is None else (o, sums)
 
-    return _enqueue(q.device, stream, call)
+    return _enqueue(q.device, stream, call, q, k, v, lengths, out, lse if isinstance(lse, torch.Tensor) else None)
 
 
 def window_attention_bwd(q, k, v, o, lse, do, window=0, sinks=0, scale=None, lengths=None, work=None, stream=None):
@@ -277,4 +283,4 @@ def window_attention_bwd(q, k, v, o, lse, do, window=0, sinks=0, scale=None, len
         T.uft_window_bwd(desc, q, k, v, o, lse, do, lengths, dq, dk, dv, w, need, s)
         return dq, dk, dv
 
-    return _enqueue(q.device, stream, call)
+    return _enqueue(q.device, stream, call, q, k, v, o, lse, do, lengths, work)

@@ -181,6 +181,46 @@ def test_split_launches_equal_whole_ones_up_to_rounding():
         check_step(cache, 0, q, whole, 0, 0, what="whole", seqs=[0, 1], counts=new)
 
 
+@pytest.mark.parametrize("new,heads", [(1, 2), (40, 1)])
+@pytest.mark.parametrize("split", [False, True])
+def test_more_keys_than_a_table_of_units_holds(new, heads, split):
+    """70,000 tokens, a hole in their middle, whole rows and slices."""
+    P = require_gpu()
+    cache = P.TokenCache(1, 1, 1200, 1, 70100, 64)
+    poison(cache)
+    fill(cache, [0], [70000], 1)
+    cache.trim([0], 30000, 20000)                        # tokens from 20,032 up to the last 30,000 leave
+    fill(cache, [0], [new], 7)
+    q = draw((new, heads, D), 3, 2.0)
+    cache.n_cu = cache.n_cu if split else 0
+    out = cache.attention(0, q, lse=True)
+    torch.cuda.synchronize()
+    assert cache.pages(0).count(-1) > 300
+    check_step(cache, 0, q, out, 0, 0, what="long", seqs=[0], counts=[new])
+
+
+def test_pages_beyond_four_gigabytes():
+    P = require_gpu()
+    cache = P.TokenCache(2, 8, 9000, 2, 8900 * 128, 128)  # 4.7 GB a layer
+    cache.extend([0], [8890 * 128])                      # takes the low pages, and is never written
+    cache.extend([1], [0])
+    fill(cache, [1], [400], 3)
+    assert min(cache.pages(1)) >= 8890
+    for new in (1, 90):
+        fill(cache, [1], [new], 20 + new)
+        for layer in (0, 1):
+            q = draw((new, 16, D), new + layer)
+            out = cache.attention(layer, q, 300, 2, lse=True)
+            torch.cuda.synchronize()
+            check_step(cache, layer, q, out, 300, 2, what=f"layer {layer}", seqs=[1], counts=[new])
+    cache.free([0])
+    before = [read(cache, 1, layer) for layer in (0, 1)]
+    assert cache.pack() == 4 and cache.pages(1) == [0, 1, 2, 3]
+    for layer in (0, 1):
+        for a, b in zip(before[layer], read(cache, 1, layer)):
+            assert np.array_equal(a, b)
+
+
 def test_large_logits_and_values_behind_the_window():
     """Scores of hundreds, the largest at either end; NaN and infinities where nothing is seen."""
     P = require_gpu()

@@ -102,6 +102,42 @@ def test_strided_views_of_one_projection_and_large_logits():
     check_all(q, *shared, do, out, 90, 2)
 
 
+def test_more_than_two_to_the_31_elements():
+    """Queries, outputs and their gradients past 32-bit offsets: the last tokens, as a sequence of their own."""
+    P = require_gpu()
+    n, Hq, Hk, W, m = 263_000, 64, 8, 40, 150
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    q, do = (torch.randn((1, n, Hq, D), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    k, v = (torch.randn((1, n, Hk, D), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    assert q.numel() > 2 ** 31
+    o, lse, dq, dk, dv = run_all(P, q, k, v, do, W, 0)
+    tail = [t[:, -m - W:].contiguous() for t in (q, k, v, do)]
+    want = run_all(P, *tail, W, 0)
+    torch.cuda.synchronize()
+    # a row's products are the same ones, in tiles that begin elsewhere: fp32 sums in another order, then one rounding
+    for got, alone in ((o, want[0]), (dq, want[2])):
+        assert (got[:, -m:].float() - alone[:, -m:].float()).abs().max() < 2 ** -5
+    for got, alone in ((dk, want[3]), (dv, want[4])):
+        a, b = got[:, -m:].float(), alone[:, -m:].float()
+        assert (a - b).abs().max() < 2 ** -5 * b.abs().max()
+    assert (lse[:, :, -m:] - want[1][:, :, -m:]).abs().max() < 1e-4
+    check_all(*(t[:, :m] for t in (q, k, v, do)), run_all(P, *(t[:, :m].contiguous() for t in (q, k, v, do)), W, 0), W, 0)
+
+
+def test_sinks_of_many_tiles():
+    """Key tiles of sinks that fill the GPU by themselves are not cut; few of them are."""
+    P = require_gpu()
+    for tokens, kv, sinks in ((2600, 1, 2500), (2600, 8, 300)):
+        q, do = draw((1, tokens, kv, D), 1), draw((1, tokens, kv, D), 2)
+        k, v = draw((1, tokens, kv, D), 3), draw((1, tokens, kv, D), 4)
+        out = run_all(P, q, k, v, do, 30, sinks)
+        torch.cuda.synchronize()
+        h = slice(kv - 1, kv)
+        check_all(*(t[:, :, h] for t in (q, k, v, do)),
+                  (out[0][:, :, h], out[1][:, h], out[2][:, :, h], out[3][:, :, h], out[4][:, :, h]), 30, sinks)
+
+
 def test_the_same_bits_again_on_another_stream_and_from_a_graph():
     P = require_gpu()
     q, do = draw((1, 700, 4, D), 1), draw((1, 700, 4, D), 2)
