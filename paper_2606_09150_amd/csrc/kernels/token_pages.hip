@@ -21,14 +21,19 @@ __device__ inline size_t page_rows(const Pool& p, int page, int kv, int h) {
   return ((size_t(page) * 2 + kv) * p.kv_heads + h) * size_t(p.page_tokens) * (kD * 2);
 }
 
-template <int N>
-__global__ __launch_bounds__(1024) void poke_kernel(Worded<PokeHead, N> a) {
-  for (int i = threadIdx.x; i < a.dense; i += 1024) a.table[a.dense_at + i] = a.words[i];
+// By a workgroup of THREADS.
+template <int THREADS>
+__device__ inline void poke(const PokeHead& a, const int32_t* words) {
+  for (int i = threadIdx.x; i < a.dense; i += THREADS) a.table[a.dense_at + i] = words[i];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int r = wave; r < a.n_runs; r += 16) {
-    const int at = a.words[a.runs + 3 * r], n = a.words[a.runs + 3 * r + 1], value = a.words[a.runs + 3 * r + 2];
+  for (int r = wave; r < a.n_runs; r += THREADS / 64) {
+    const int at = words[a.runs + 3 * r], n = words[a.runs + 3 * r + 1], value = words[a.runs + 3 * r + 2];
     for (int i = lane; i < n; i += 64) a.table[at + i] = value < 0 ? value : value + i;
   }
+}
+template <int N>
+__global__ __launch_bounds__(1024) void poke_kernel(Worded<PokeHead, N> a) {
+  poke<1024>(a, a.words);
 }
 
 template <int N>
@@ -38,12 +43,16 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Worded<RowsHead, N> a) {
   for (int i = threadIdx.x; i < n; i += kThreads) a.table[to + i] = a.table[from + i];
 }
 
-// One workgroup per (page, K or V, head; layer).  Loads before stores: the stores
-// could alias them as far as the compiler knows.
+// One workgroup per (page, K or V, head; layer), and one for the tables.  Loads before
+// stores: the stores could alias them as far as the compiler knows.
 template <int T, int N>
 __global__ __launch_bounds__(kThreads) void copy_pages_kernel(Worded<CopyHead, N> a) {
   const int heads = 2 * a.pool.kv_heads;
   const int i = blockIdx.x / heads, kvh = blockIdx.x % heads;
+  if (i == a.n) {
+    if (blockIdx.y == 0) poke<kThreads>(a.poke, a.words + 3 * a.n);
+    return;
+  }
   const int rows = a.words[3 * i + 2];
   uint8_t* base = a.pool.base + size_t(blockIdx.y) * a.pool.layer_bytes;
   const uint4* src = reinterpret_cast<const uint4*>(base + page_rows(a.pool, a.words[3 * i], 0, kvh));
@@ -242,10 +251,10 @@ hipError_t launch_rows(const RowsArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t stream) {
-  const dim3 grid(unsigned(a.n) * 2 * unsigned(a.pool.kv_heads), unsigned(a.pool.layers));
+hipError_t launch_copy_pages(const CopyArgs& a, int used, hipStream_t stream) {
+  const dim3 grid(unsigned(a.n) * 2 * unsigned(a.pool.kv_heads) + (a.poke.table != nullptr ? 1 : 0), unsigned(a.pool.layers));
   const bool wide = a.pool.page_tokens == 128;
-  if (3 * a.n <= kFew) {
+  if (used <= kFew) {
     if (wide) copy_pages_kernel<128, kFew><<<grid, kThreads, 0, stream>>>(few(a));
     else copy_pages_kernel<64, kFew><<<grid, kThreads, 0, stream>>>(few(a));
   } else {

@@ -41,10 +41,12 @@ struct RowsHead {
   int32_t* table;
   int32_t n;
 };
-// (source page, target page, rows) triples, every layer
+// (source page, target page, rows) triples, every layer; with them, from words[3 n] on,
+// the words of a PokeHead (table null: none).
 struct CopyHead {
   Pool pool;
   int32_t n;
+  PokeHead poke;
 };
 // uft_keep.  In place: kKeepWords words a sequence: table offset, length, start, count,
 // first index.  Into fresh pages: the same for a run of pages that follow one another,
@@ -68,7 +70,7 @@ using KeepArgs = Worded<KeepHead, kWords>;
 // `used`: words of a that hold something
 hipError_t launch_poke(const PokeArgs& a, int used, hipStream_t stream);
 hipError_t launch_rows(const RowsArgs& a, hipStream_t stream);
-hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t stream);
+hipError_t launch_copy_pages(const CopyArgs& a, int used, hipStream_t stream);
 hipError_t launch_keep_in_place(const KeepArgs& a, hipStream_t stream);
 hipError_t launch_keep_fresh(const KeepArgs& a, hipStream_t stream);
 

@@ -170,6 +170,15 @@ class Poke {
       i = e;
     }
   }
+  // All of it beside `used` words of another launch: its head, the words behind them.  False where it does not fit.
+  bool join(tok::PokeHead* head, int32_t* words, int used) {
+    if (size_t(used) + dense.size() + runs_.size() > size_t(tok::kWords)) return false;
+    *head = tok::PokeHead{c_->table, 0, int32_t(dense.size()), int32_t(dense.size()), int32_t(runs_.size() / 3)};
+    std::copy(dense.begin(), dense.end(), words + used);
+    std::copy(runs_.begin(), runs_.end(), words + used + dense.size());
+    return true;
+  }
+  int words() const { return int(dense.size() + runs_.size()); }
   int send(hipStream_t stream) {
     if (c_->dry()) return UF_OK;
     for (size_t di = 0, ri = 0; di < dense.size() || ri < runs_.size();) {
@@ -192,18 +201,22 @@ class Poke {
   std::vector<int32_t> runs_;   // (at, count, first value)
 };
 
-int copy_pages(const uft_cache* c, const std::vector<int32_t>& triples, hipStream_t stream) {
+// Pages to copy and table changes: in one launch where their words fit.
+int copy_and_poke(const uft_cache* c, const std::vector<int32_t>& triples, Poke& poke, hipStream_t stream) {
   if (c->dry()) return UF_OK;
   for (size_t i = 0; i < triples.size();) {
     tok::CopyArgs a;
     a.pool = c->pool_of(0);
+    a.poke = tok::PokeHead{};
     const size_t n = std::min(triples.size() - i, size_t(tok::kWords / 3 * 3));
     std::copy_n(triples.begin() + i, n, a.words);
     a.n = int32_t(n / 3);
-    if (int s = check_hip(tok::launch_copy_pages(a, stream), "page copy")) return s;
     i += n;
+    const bool joined = i == triples.size() && poke.join(&a.poke, a.words, int(n));
+    if (int s = check_hip(tok::launch_copy_pages(a, int(n) + (joined ? poke.words() : 0), stream), "page copy")) return s;
+    if (joined) return UF_OK;
   }
-  return UF_OK;
+  return poke.send(stream);
 }
 
 bool in_step(uft_cache* c, int32_t n, const int32_t* seqs) {
@@ -373,8 +386,7 @@ int uft_extend(uft_cache* c, int32_t n, const int32_t* seqs, const int32_t* coun
     for (int32_t i = 0; i < n; ++i)
       c->seqs[size_t(seqs[i])].pages.reserve(c->seqs[size_t(seqs[i])].pages.size() + grown[size_t(i)].fresh.size());
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (int s = copy_pages(c, copies, st)) return s;
-    if (int s = poke.send(st)) return s;
+    if (int s = copy_and_poke(c, copies, poke, st)) return s;
     taken.keep();
     for (int32_t i = 0; i < n; ++i) {
       Seq& q = c->seqs[size_t(seqs[i])];
@@ -477,8 +489,7 @@ int uft_copy(uft_cache* c, int32_t n, const int32_t* src, const int32_t* dst, vo
       poke.run(c->row_at(dst[i]), to.data(), int32_t(to.size()));
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (int s = copy_pages(c, copies, st)) return s;
-    if (int s = poke.send(st)) return s;
+    if (int s = copy_and_poke(c, copies, poke, st)) return s;
     taken.keep();
     for (int32_t i = 0; i < n; ++i) {
       c->seqs[size_t(dst[i])].pages.swap(pages[size_t(i)]);
@@ -673,8 +684,7 @@ int uft_pack(uft_cache* c, int32_t* used_pages, void* stream) {
     for (int32_t p = c->d.n_pages - 1; p >= used; --p) left.push_back(p);
     decltype(c->free) free(std::greater<int32_t>(), std::move(left));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (int s = copy_pages(c, copies, st)) return s;
-    if (int s = poke.send(st)) return s;
+    if (int s = copy_and_poke(c, copies, poke, st)) return s;
     for (Seq& q : c->seqs)
       for (int32_t& p : q.pages)
         if (p >= 0) {

@@ -19,6 +19,8 @@ _NO_STRIDE = T.uft_stride(0, 0, 0)
 
 def _check(t, name, shape, dtype=torch.bfloat16, device=None):
     """A device tensor of this type, shape and device."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.shape == shape and not t.requires_grad:
+        return                                           # (device: a GPU's)
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a tensor (got {type(t).__name__})")
     if t.dtype is not dtype:
