@@ -79,6 +79,7 @@ __device__ inline void dma16_low(const void* base, uint32_t off, uint32_t lds, u
 // of `part_units` units, the others are whole.
 struct Cut {
   int32_t tiles, split, parts, part_units;
+  int32_t turn;                                // units of a tile of the window, 0 without a window
 };
 // Units (64 rows) of a sequence of `len` tokens that see keys of [k0, k0 + 128): first, end.
 __host__ __device__ inline void unit_range(int len, int G, int k0, int window, int sinks, int* first, int* end) {
@@ -125,6 +126,18 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     return;
   }
   const int U = end - first;
+  // The order of the units.  Tiles side by side see rows that lie 128 tokens apart, so that in ascending order each
+  // would read a unit when the other has long left it (32 tiles an XCD, 8 MB of Q and dO between the first and the last
+  // of them: all of it past the L2, 4.0 GB at 16,384 tokens, 32 heads, window 2,048).  So they begin at the same unit, a
+  // multiple of a tile's number of units, and take those before it at the end; without a window they begin at the
+  // last unit.
+  const int ahead = cut.turn > 0 && whole ? (first + cut.turn - 1) / cut.turn * cut.turn - first : 0;
+  const int start = ahead < U ? ahead : 0;
+  auto unit_at = [&](int s) {
+    if (cut.turn == 0) return end - 1 - s;
+    const int u = start + s;
+    return first + (u < U ? u : u - U);
+  };
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -156,7 +169,7 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
   // Copies of a unit: Q and dO rows, and the seeds.  Copy i of wave w fills LDS chunks
   // [64*(8 i + w), +64), rows 32 i + 4 w + lane/16, whose low four bits do not depend
   // on i.  A row is found from the unit's first token and that token's rows before the
-  // unit, which advance with the units; rows past the last give way to it.
+  // unit; rows past the last give way to it.
   const int lr = 4 * wave + (lane >> 4);
   const uint32_t chunk = uint32_t(swz_perm((lane & 15) ^ swz_f(lr & 15)) * 16);
   const uint32_t lq0 = lds_addr(&sQ[0][0]), lo0 = lds_addr(&sO[0][0]), ll0 = lds_addr(&sLD[0][0]);
@@ -164,19 +177,19 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
   const uint8_t* const ob = reinterpret_cast<const uint8_t*>(a.dout + (size_t(b) * a.tokens * a.q_heads + size_t(h) * G) * kD);
   const float per_g = 1.f / float(G);
   const uint32_t qt2 = uint32_t(a.q_token) * 2, qh2 = uint32_t(a.q_head) * 2, ot2 = uint32_t(a.q_heads) * (kD * 2);
-  int nu = first, nt = int(int64_t(first) * UQ / G), nr = int(int64_t(first) * UQ - int64_t(nt) * G);
   struct Source {
     const uint8_t *q, *o, *seeds;
     uint32_t qslot, oslot;
   };
   uint32_t qoff[kCopies], ooff[kCopies];       // the lane's rows, from the unit's first token on
-  bool placed = false;
-  // The next unit's; past the end the last one is copied again, into a slot that nothing reads any more.
-  auto source = [&](uint32_t qslot, uint32_t oslot) {
-    const Source s{qb + int64_t(nt) * a.q_token * 2, ob + int64_t(nt) * ot2, seeds + size_t(nu >> 1) * kSeeds, qslot, oslot};
+  bool placed = false;                         // for every whole unit
+  // Unit s; past the end the last one is copied again, into a slot that nothing reads any more.
+  auto source = [&](int s, uint32_t qslot, uint32_t oslot) {
+    const int u = unit_at(min(s, U - 1));
+    const int nt = div_nt(uint32_t(u) * UQ, a.group_div), nr = u * UQ - nt * G;
     const int top = len * G - 1 - nt * G;
-    // the same for every whole unit where the heads of a group divide one
-    if (!placed || UQ % G != 0 || top < UQ - 1) {
+    const bool same = UQ % G == 0 && top >= UQ - 1;    // the heads of a group divide a unit, and it is whole
+    if (!placed || !same) {
 #pragma unroll
       for (int i = 0; i < kCopies; ++i) {
         const int rel = min(nr + 32 * i + lr, top);    // below 64 + G <= 2^17: the quotient is exact in fp32
@@ -184,15 +197,9 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
         qoff[i] = tok * qt2 + g * qh2 + chunk;
         ooff[i] = tok * ot2 + g * (kD * 2) + chunk;
       }
-      placed = true;
+      placed = same;
     }
-    if (nu + 1 < first + U) {
-      ++nu;
-      nr += UQ % G;
-      nt += UQ / G;
-      if (nr >= G) nr -= G, ++nt;
-    }
-    return s;
+    return Source{qb + int64_t(nt) * a.q_token * 2, ob + int64_t(nt) * ot2, seeds + size_t(u >> 1) * kSeeds, qslot, oslot};
   };
   constexpr int kIssue = 2 * kCopies + 1;      // copies of a wave per unit
   auto issue = [&](const Source& c, int k) {
@@ -368,10 +375,11 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     auto phase = [&](int s, auto start) {
       constexpr bool kFirst = decltype(start)::value;
       // unit s has landed; the slots of unit s+2 are free
-      const Source next = source(uint32_t(s + 2) & 3u, om == 0 ? 2u : om - 1u);
-      const uint32_t ld = ld0 + (uint32_t(s) & 3u) * uint32_t(sizeof(sLD[0])) + uint32_t((first + s) & 1) * uint32_t(4 * UQ);
+      const Source next = source(s + 2, uint32_t(s + 2) & 3u, om == 0 ? 2u : om - 1u);
+      const int u = unit_at(s);
+      const uint32_t ld = ld0 + (uint32_t(s) & 3u) * uint32_t(sizeof(sLD[0])) + uint32_t(u & 1) * uint32_t(4 * UQ);
       if constexpr (G0 == 0) {
-        unit0((first + s) * UQ, ld, uint32_t(s) & 1u, next);
+        unit0(u * UQ, ld, uint32_t(s) & 1u, next);
         advance((s & 3) == 3, kQRing);
         advance_tr(om == 2, kORing);
       } else {
@@ -396,8 +404,8 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0)); // no copy outlives the workgroup
   };
   if (U > 0) {
-    issue_all(source(0, 0));
-    issue_all(source(1, 1));
+    issue_all(source(0, 0, 0));
+    issue_all(source(1, 1, 1));
     if (grp == 0) run(std::integral_constant<int, 0>{});
     else run(std::integral_constant<int, 1>{});
   }
@@ -703,7 +711,10 @@ Cut cut_of(const BwdArgs& a) {
   Cut c{};
   c.tiles = (a.tokens + kT - 1) / kT;
   c.parts = 1;
-  if (a.window == 0 || a.sinks == 0) return c;
+  if (a.window == 0) return c;
+  const int64_t turn = ((int64_t(a.window < a.tokens ? a.window : a.tokens) + kT - 1) * a.group + 63) / 64;
+  c.turn = int(turn);
+  if (a.sinks == 0) return c;
   const int sinks = (a.sinks + kT - 1) / kT < c.tiles ? (a.sinks + kT - 1) / kT : c.tiles;
   int first, end;
   unit_range(a.tokens, a.group, 0, a.window, a.sinks, &first, &end);

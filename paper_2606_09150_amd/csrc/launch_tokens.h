@@ -154,6 +154,7 @@ struct BwdArgs {
   uint8_t* work;
   int32_t batch, tokens, q_heads, kv_heads, group, window, sinks;
   int32_t tiles;                              // row tiles of a sequence
+  uint64_t group_div;                         // (2^64 - 1) / group: j / group == ((j + 1) * group_div) >> 64 for 0 <= j < 2^31
   float scale, scale_log2;
 };
 size_t bwd_work_bytes(const BwdArgs& a);

@@ -951,6 +951,7 @@ tok::BwdArgs bwd_args(const uft_window_desc* d, float log2) {
   a.q_heads = d->q_heads;
   a.kv_heads = d->kv_heads;
   a.group = d->q_heads / d->kv_heads;
+  a.group_div = ~uint64_t(0) / uint64_t(a.group);
   a.window = d->window;
   a.sinks = std::min(d->sinks, d->tokens);
   a.tiles = int32_t((int64_t(d->tokens) * a.group + 127) / 128);
