@@ -6,6 +6,7 @@ all computation happens in libuf.so's kernels (include/uft.h has the definitions
 """
 
 import math
+import operator
 
 import torch
 
@@ -39,6 +40,14 @@ def _dense(t, name, shape, dtype=torch.bfloat16, device=None):
     _check(t, name, shape, dtype, device)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+
+
+def _int(x, name):
+    """An integer that a C int32 holds (ctypes would cut a larger one off)."""
+    x = operator.index(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must fit in 32 bits (got {x})")
+    return x
 
 
 def _strides(t, name, dense=None):
@@ -85,7 +94,10 @@ class TokenCache:
     Every call takes its work on ``stream`` (default: the current one); calls on one cache are to be ordered."""
 
     def __init__(self, layers, kv_heads, n_pages, max_seqs, max_tokens, page_tokens=64, head_dim=D, flags=0, device=None):
-        self.desc = T.uft_desc(layers, kv_heads, head_dim, page_tokens, n_pages, max_seqs, max_tokens, flags)
+        sizes = dict(layers=layers, kv_heads=kv_heads, head_dim=head_dim, page_tokens=page_tokens, n_pages=n_pages,
+                     max_seqs=max_seqs, max_tokens=max_tokens)
+        self.desc = T.uft_desc(flags=flags, **{name: _int(x, name) for name, x in sizes.items()})
+        kv_heads = self.desc.kv_heads
         self.dry = bool(flags & L.UF_F_DRYRUN)
         self.pool_bytes = T.uft_pool_bytes(self.desc)
         self.pool = self.table = self.device = None
@@ -119,11 +131,11 @@ class TokenCache:
         return T.uft_get_info(self.handle)
 
     def tokens(self, seq):
-        return T.uft_seq_tokens(self.handle, seq)
+        return T.uft_seq_tokens(self.handle, _int(seq, "seq"))
 
     def pages(self, seq):
         """The page of each ``page_tokens`` tokens of a sequence (-1: trimmed)."""
-        return T.uft_seq_pages(self.handle, seq)
+        return T.uft_seq_pages(self.handle, _int(seq, "seq"))
 
     def pages_view(self):
         """All pages, [layers, n_pages, (K, V), kv_heads, page_tokens, head_dim] bfloat16."""
@@ -145,6 +157,7 @@ class TokenCache:
 
     def write(self, layer, k, v, stream=None):
         """The step's keys and values of a layer, [step tokens, kv_heads, 128] (strided views too)."""
+        layer = _int(layer, "layer")
         if self.dry:
             return T.uft_write(self.handle, layer, k, _NO_STRIDE, v, _NO_STRIDE)
         shape = (self.step_tokens(), self.desc.kv_heads, D)
@@ -174,6 +187,7 @@ class TokenCache:
 
     def trim(self, seqs, window, sinks=0, stream=None):
         """Give back the pages that no later query of this window and these sinks sees."""
+        window, sinks = _int(window, "window"), _int(sinks, "sinks")
         self._run(stream, lambda s: T.uft_trim(self.handle, seqs, window, sinks, s))
 
     def free(self, seqs):
@@ -187,13 +201,14 @@ class TokenCache:
     # -- attention ----------------------------------------------------------------
     def work_bytes(self, q_heads, window=0, sinks=0):
         """Scratch that ``attention`` needs for the present step."""
-        return T.uft_attn_work_bytes(self.handle, T.uft_attn_desc(q_heads, window, sinks, self.n_cu, SCALE, _NO_STRIDE))
+        return T.uft_attn_work_bytes(self.handle, T.uft_attn_desc(_int(q_heads, "q_heads"), _int(window, "window"), _int(sinks, "sinks"), self.n_cu, SCALE, _NO_STRIDE))
 
     def attention(self, layer, q, window=0, sinks=0, scale=None, tree=None, out=None, lse=False, work=None, stream=None):
         """O [step tokens, q_heads, 128] bf16 (and LSE [step tokens, q_heads] fp32 when ``lse``) of the step's tokens.
 
         ``window`` 0: all earlier tokens; else the last ``window`` and the first ``sinks`` ones.  ``tree``: int64
         [step tokens], the nodes that each new token sees, as bits.  ``work``: scratch (allocated here when None)."""
+        layer, window, sinks = _int(layer, "layer"), _int(window, "window"), _int(sinks, "sinks")
         scale = SCALE if scale is None else scale
         if self.dry:                                     # q: the number of its heads
             T.uft_attn(self.handle, layer, T.uft_attn_desc(q, window, sinks, 0, scale, _NO_STRIDE), None, tree, None, None, None)
@@ -239,7 +254,7 @@ def _window_desc(q, k, v, window, sinks, scale, lengths):
     if lengths is not None:
         _dense(lengths, "lengths", (B,), torch.int32, q.device)
     scale = SCALE if scale is None else scale
-    return T.uft_window_desc(B, n, Hq, Hk, D, window, sinks, scale, _strides(q, "q"), _strides(k, "k"), _strides(v, "v"))
+    return T.uft_window_desc(B, n, Hq, Hk, D, _int(window, "window"), _int(sinks, "sinks"), scale, _strides(q, "q"), _strides(k, "k"), _strides(v, "v"))
 
 
 def window_attention(q, k, v, window=0, sinks=0, scale=None, lengths=None, out=None, lse=True, stream=None):

@@ -413,6 +413,50 @@ def test_many_pages_in_one_call():
     check_step(cache, 0, q, out, 0, 0, what="after all", seqs=[2], counts=[1])
 
 
+def test_many_sequences_in_one_call():
+    """More sequences than a launch's arguments hold words for."""
+    P = require_gpu()
+    n = 420
+    cache, model = P.TokenCache(2, 1, 2600, 2 * n, 400, 64), O.PageModel(2600, 2 * n, 400, 64)
+    poison(cache)
+    rng = np.random.default_rng(1)
+    ids, at = list(range(n)), 1
+    for turn in range(2):
+        new = []
+        for _ in ids:
+            k = int(rng.integers(1, 130)) if turn == 0 else 1
+            new.append(list(range(at, at + k)))
+            at += k
+        assert model.extend(ids, new)
+        cache.extend(ids, [len(x) for x in new])
+        for layer, rows in enumerate(_values(sum(new, []), 1, 2)):
+            cache.write(layer, *rows)
+    q = draw((n, 3, D), 5, 0.01)
+    out = cache.attention(1, q, 60, 1, lse=True)
+    torch.cuda.synchronize()
+    check_step(cache, 1, q, out, 60, 1, what="many", seqs=ids, counts=[1] * n)
+    twins = [n + s for s in ids]
+    model.fork(ids, twins)
+    cache.fork(ids, twins)
+    new = [[at + s] for s in ids]                         # every partly filled page is copied first
+    assert model.extend(twins, new)
+    cache.extend(twins, [1] * n)
+    for layer, rows in enumerate(_values(sum(new, []), 1, 2)):
+        cache.write(layer, *rows)
+    _compare(cache, model, 1, 2)
+    for most in (16, 100):                                # in place, and into fresh pages
+        starts = [int(rng.integers(0, len(model.rows[s]) + 1)) for s in ids]
+        index = [[int(x) for x in rng.integers(0, len(model.rows[s]), rng.integers(0, min(most, len(model.rows[s]) - a) + 1))]
+                 for s, a in zip(ids, starts)]
+        assert model.keep(ids, starts, index)
+        cache.keep(ids, starts, [len(x) for x in index], torch.tensor(sum(index, []), dtype=torch.int32, device="cuda"))
+        _compare(cache, model, 1, 2)
+    model.free(twins)
+    cache.free(twins)
+    assert cache.pack() == model.pack()
+    _compare(cache, model, 1, 2)
+
+
 def test_a_speculative_run_equals_the_plain_one():
     """Prompt, draft trees, the accepted path kept, pages trimmed and packed: attention as of a sequence that
     holds only the accepted tokens, at every step."""

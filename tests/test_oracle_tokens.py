@@ -2,6 +2,9 @@
 no GPU) against the oracle's model, with every refusal that the host can force."""
 
 import math
+import os
+import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -228,6 +231,39 @@ def test_refusals(P):
         assert status(lambda: T.uft_window_bwd_work_bytes(w(**bad))) == want, bad
     assert status(lambda: T.uft_window_fwd(w(), None, None, None, None, None, None)) == ARG
     assert status(lambda: T.uft_window_bwd(w(), *[None] * 11)) == ARG
+
+
+def test_integers_that_32_bits_cannot_hold(P):
+    c = _dry(P)
+    c.extend([0], [5])
+    for f in (lambda: c.attention(0, 3, 2 ** 32), lambda: c.attention(2 ** 32, 3), lambda: c.attention(0, 3, 1, 2 ** 31),
+              lambda: c.trim([0], 2 ** 32 + 1), lambda: c.write(2 ** 32, None, None), lambda: c.tokens(2 ** 32),
+              lambda: _dry(P, max_tokens=2 ** 32 + 5), lambda: c.work_bytes(3, 2 ** 33)):
+        with pytest.raises(ValueError):
+            f()
+    with pytest.raises(OverflowError):
+        c.extend([0], [2 ** 32])
+    with pytest.raises(TypeError):
+        c.attention(0, 3, 1.5)
+    assert c.tokens(np.int64(0)) == 5
+    c.attention(np.int64(0), 3, np.int32(4))
+
+
+def test_library_exports_every_declared_symbol(P):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    names = sorted(set(re.findall(r"^\s*int\s+(uft_\w+)\s*\(", open(os.path.join(root, "include", "uft.h")).read(), re.M)))
+    out = subprocess.run(["nm", "-D", "--defined-only", P._lib.LIB_PATH], capture_output=True, text=True).stdout
+    assert len(names) == 20 and sorted(set(re.findall(r"\sT\s(uft_\w+)$", out, re.M))) == names
+    assert set(P._tokens._SIGNATURES) == set(names)
+
+
+def test_the_header_is_plain_c(tmp_path):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "a.c"
+    src.write_text('#include "uft.h"\nint main(void) { uft_window_desc d = {0}; return (int)d.batch; }\n')
+    r = subprocess.run(["gcc", "-std=c11", "-Wall", "-Werror", "-pedantic", f"-I{root}/include", "-fsyntax-only", str(src)],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
 
 
 def test_the_wrappers_refuse_host_tensors(P):
