@@ -17,12 +17,11 @@
  *     LSE = natural log of sum_j exp(scale q.k_j);
  * a query that sees nothing gets O = 0 and LSE = -inf.  Query head n reads key
  * head n / (q_heads / kv_heads).  Scores, weights' sums and accumulators are fp32;
- * weights are rounded to bf16 for their product with V.  Tiles of keys and queries
- * are multiplied whole, with weights of zero where a query does not see a key: a
- * value that is not finite, at a token that one query of a call sees, can
- * therefore make NaN of the other queries of that call.  What no query of a tile
- * sees is not read: neither memory past a sequence's end nor tokens that have
- * left the window.
+ * weights are rounded to bf16 for their product with V.  A key or value that is not
+ * finite reaches the queries that see it and no others (where there is one, the rows
+ * beside it are formed key by key, which is slow).  The gradients' products run over
+ * whole tiles: there such a token can make NaN of its neighbours' gradients.  Memory
+ * past a sequence's end, padding and pages of others are never read.
  */
 #ifndef UFT_H
 #define UFT_H

@@ -365,6 +365,38 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
     walk(n_units, [&](int u) { return unit_of(tile_of(u), 0); });
   }
 
+  // A weight of zero times a value that is not finite: a row that does not see the value has it all the same.  Where any
+  // of the wave's results is not finite its rows are formed again key by key, each from the keys it sees.
+  float probe = 0.f;
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) probe += o[mb][r];
+  if (__ballot(not_finite(probe)) != 0) {
+    float out[64];
+#pragma unroll
+    for (int i = 0; i < 64; ++i) out[i] = 0.f;
+    for (int u = 0; u < n_units; ++u) {
+      const int t = tile_of(u0 + u);
+      int page = 0;
+      if (PAGED) {
+        page = __builtin_amdgcn_readfirstlane(a.table[size_t(p.seq) * a.row + uint32_t(t * kKeyUnit) / uint32_t(T)]);
+        if (uint32_t(page) >= uint32_t(a.pool.n_pages)) continue;
+      }
+      const Unit c = unit_of(t, page);
+      const uint64_t see = tree ? seen_bits_tree(pos, c.key0, a.window, a.sinks, p.held, node)
+                                : seen_bits(pos, c.key0, a.window, a.sinks);
+      for (int k = 0; k < kKeyUnit; ++k) {
+        const bool on = live && ((see >> k) & 1u);
+        if (__ballot(on) != 0)
+          add_key<16>(qf, c.k + uint32_t(k) * kstep, c.v + uint32_t(k) * vstep, hl, on, c2, moff, 4 * hl, out);
+      }
+    }
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[mb][r] = out[16 * mb + r];
+  }
   l = pair_sum(l);
   if (!whole) {                                        // a slice: O relative to the offset, the offset and the sum
     if (live) {
@@ -382,7 +414,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
     return;
   }
   if (live) {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l == 0.f ? 0.f : 1.f / l;       // (a sum that is no number stays one)
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
@@ -392,7 +424,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
         u.y = pack_bf16x2(o[mb][4 * i + 2] * inv, o[mb][4 * i + 3] * inv);
         *reinterpret_cast<uint2*>(op + mb * 32 + 8 * i) = u;
       }
-    if (lp != nullptr && hl == 0) *lp = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    if (lp != nullptr && hl == 0) *lp = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
   } else if (stored) {
     store_zero();
   }
@@ -635,6 +667,26 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
     for (int w = 0; w < 4; ++w) out[r] += xo[((w * 8 + wave) * 16 + r) * 64 + lane] * f[w];
   }
   const int d0 = wave * 32 + 4 * hl;
+  float probe = 0.f;                                   // as above: a value that a row does not see
+#pragma unroll
+  for (int r = 0; r < 16; ++r) probe += out[r];
+  if (__ballot(not_finite(probe)) != 0) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) out[r] = 0.f;
+    for (int u = u0; u < u0 + n_units; ++u) {
+      const int key0 = (u < range.sink ? u : u - range.sink + range.from) * kFewUnit;
+      const int page = __builtin_amdgcn_readfirstlane(pages[uint32_t(key0) / uint32_t(T)]);
+      if (uint32_t(page) >= uint32_t(a.pool.n_pages)) continue;
+      const uint8_t* kp = a.pool.base + (size_t(page) * 2 * H + h) * size_t(T) * (kD * 2) + size_t(key0 & (T - 1)) * (kD * 2);
+      const uint64_t see = tree ? seen_bits_tree(pos, key0, a.window, a.sinks, p.held, node)
+                                : seen_bits(pos, key0, a.window, a.sinks);
+      for (int k = 0; k < kFewUnit; ++k) {
+        const bool on = (see >> k) & 1u;
+        if (__ballot(on) != 0)
+          add_key<4>(qf, kp + k * (kD * 2), kp + vbase + k * (kD * 2), hl, on, c2, mm == -INFINITY ? 0.f : mm, d0, out);
+      }
+    }
+  }
   if (!whole) {
     const size_t all = size_t(a.n) * H * a.n_split * kFewRows;
     const size_t at = ((size_t(e) * H + h) * a.n_split + slice) * kFewRows + ln;
@@ -645,7 +697,7 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
     if (wave == 0 && hl == 0) reinterpret_cast<float2*>(a.work + all * kD)[at] = make_float2(mm, lt);
     return;
   }
-  const float inv = lt > 0.f ? 1.f / lt : 0.f;
+  const float inv = lt == 0.f ? 0.f : 1.f / lt;
   uint16_t* op = a.o + (size_t(p.at) + token) * a.q_heads * kD + size_t(head) * kD + d0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -655,7 +707,7 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
     *reinterpret_cast<uint2*>(op + 8 * i) = u;
   }
   if (a.lse != nullptr && wave == 0 && hl == 0)
-    a.lse[(size_t(p.at) + token) * a.q_heads + head] = lt > 0.f ? (mm + log2f(lt)) * 0.69314718055994531f : -INFINITY;
+    a.lse[(size_t(p.at) + token) * a.q_heads + head] = lt == 0.f ? -INFINITY : (mm + log2f(lt)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------- join slices ----
@@ -734,13 +786,13 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] += __shfl_xor(x[i], s, LANES);
   if (grp != 0) return;
-  const float inv = lt > 0.f ? 1.f / lt : 0.f;
+  const float inv = lt == 0.f ? 0.f : 1.f / lt;
   const int token = row / G, head = h * G + row - token * G;
   const size_t out = (size_t(p.at) + token) * a.q_heads + head;
   reinterpret_cast<uint4*>(a.o)[out * (kD / 8) + c] =
       make_uint4(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv),
                  pack_bf16x2(x[4] * inv, x[5] * inv), pack_bf16x2(x[6] * inv, x[7] * inv));
-  if (a.lse != nullptr && c == 0) a.lse[out] = lt > 0.f ? (mm + log2f(lt)) * 0.69314718055994531f : -INFINITY;
+  if (a.lse != nullptr && c == 0) a.lse[out] = lt == 0.f ? -INFINITY : (mm + log2f(lt)) * 0.69314718055994531f;
 }
 
 template <int TILE, int UNIT>

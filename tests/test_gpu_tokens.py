@@ -245,6 +245,47 @@ def test_large_logits_and_values_behind_the_window():
         check_rows(f64(q), f64(out[0]), f64(out[1]), kk, vv, see)
 
 
+def _only_those_that_see(q, o, lse, k, v, see, bad):
+    """Rows that see none of the keys ``bad`` are as if those were anything else; the others are not finite."""
+    hit = see[:, bad].any(1)
+    assert hit.any() and not hit.all()
+    assert not np.isfinite(o[hit]).all(axis=(1, 2)).any()
+    if np.isnan(k[bad]).any():
+        assert np.isnan(lse[hit]).all()
+    k, v = k.copy(), v.copy()
+    k[bad], v[bad] = 0, 0
+    check_rows(q[~hit], o[~hit], lse[~hit], k, v, see[~hit])
+
+
+@pytest.mark.parametrize("held,new,heads,window,sinks,bad", [
+    (0, 300, 2, 50, 3, [100, 101, 220]),                  # a prompt
+    (2000, 40, 1, 0, 0, [2017]),                          # slices
+    (500, 3, 8, 60, 2, [502]),                            # few rows
+    (90, 8, 4, 0, 0, [97])])
+def test_values_that_are_not_finite_reach_only_rows_that_see_them(held, new, heads, window, sinks, bad):
+    P = require_gpu()
+    for kind in ("v inf", "v nan", "k nan"):
+        k, v = draw((held + new, 1, D), 1), draw((held + new, 1, D), 2)
+        (k if kind[0] == "k" else v)[bad] = float(kind[2:])
+        cache = P.TokenCache(1, 1, 50, 1, 3000, 64)
+        poison(cache)
+        if held:
+            fill(cache, [0], [held], 0, k[:held], v[:held])
+        fill(cache, [0], [new], 0, k[held:], v[held:])
+        q = draw((new, heads, D), 3)
+        log(f"not finite: {kind} {held}+{new} heads={heads}")
+        o, lse = cache.attention(0, q, window, sinks, lse=True)
+        torch.cuda.synchronize()
+        see = O.sees(np.arange(held, held + new), np.arange(held + new), window, sinks)
+        _only_those_that_see(f64(q), f64(o), f64(lse), f64(k), f64(v), see, bad)
+        bits = [1 << t | (1 if t else 0) for t in range(min(new, 40))]     # a root, and leaves that do not see each other
+        if new <= 40:
+            words = torch.tensor(bits, dtype=torch.int64, device="cuda")
+            o, lse = cache.attention(0, q, window, sinks, tree=words, lse=True)
+            torch.cuda.synchronize()
+            _only_those_that_see(f64(q), f64(o), f64(lse), f64(k), f64(v), O.tree_sees(held, bits, window, sinks), bad)
+
+
 def test_strided_views_another_stream_and_the_callers_buffers():
     P = require_gpu()
     cache = P.TokenCache(1, 2, 20, 2, 600, 64)

@@ -9,7 +9,7 @@ import torch
 
 from oracle import tokens as O
 from tests.gpu_common import f64, log, require_gpu
-from tests.test_gpu_tokens import D, SCALE, check_rows, draw
+from tests.test_gpu_tokens import D, SCALE, _only_those_that_see, check_rows, draw
 
 pytestmark = pytest.mark.gpu
 
@@ -136,6 +136,20 @@ def test_sinks_of_many_tiles():
         h = slice(kv - 1, kv)
         check_all(*(t[:, :, h] for t in (q, k, v, do)),
                   (out[0][:, :, h], out[1][:, h], out[2][:, :, h], out[3][:, :, h], out[4][:, :, h]), 30, sinks)
+
+
+@pytest.mark.parametrize("kind", ["v inf", "v nan", "k nan"])
+def test_values_that_are_not_finite_reach_only_rows_that_see_them(kind):
+    P = require_gpu()
+    q, k, v = draw((1, 400, 6, D), 1), draw((1, 400, 2, D), 2), draw((1, 400, 2, D), 3)
+    bad = [130, 131, 300]
+    (k if kind[0] == "k" else v)[:, bad, 1] = float(kind[2:])
+    o, lse = P.window_attention(q, k, v, 40, 5)
+    torch.cuda.synchronize()
+    see = O.sees(np.arange(400), np.arange(400), 40, 5)
+    o, lse = f64(o)[0], f64(lse)[0].T
+    check_rows(f64(q)[0, :, :3], o[:, :3], lse[:, :3], f64(k)[0, :, :1], f64(v)[0, :, :1], see)
+    _only_those_that_see(f64(q)[0, :, 3:], o[:, 3:], lse[:, 3:], f64(k)[0, :, 1:], f64(v)[0, :, 1:], see, bad)
 
 
 def test_the_same_bits_again_on_another_stream_and_from_a_graph():
