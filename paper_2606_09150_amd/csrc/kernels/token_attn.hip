@@ -33,6 +33,8 @@
 // changed nothing.)
 #include "token_common.h"
 
+#include <algorithm>
+
 namespace uf {
 namespace tok {
 namespace {
@@ -54,10 +56,21 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
   int idx = blockIdx.x;
   const int h = idx % H;
   idx /= H;
-  const int e = idx % a.n;
-  idx /= a.n;
-  const int tile = a.tiles - 1 - idx % a.tiles;        // long ranges first
-  const int slice = idx / a.tiles;
+  int e, tile, slice, at_tile;                         // at_tile: of the launch
+  if (PAGED && a.packed > 0) {
+    slice = idx / a.packed;
+    at_tile = a.packed - 1 - idx % a.packed;
+    const Place w = tile_place(a, at_tile, kRowTile);
+    if (w.entry < 0) return;
+    e = w.entry;
+    tile = w.tile;
+  } else {
+    e = idx % a.n;
+    idx /= a.n;
+    tile = a.tiles - 1 - idx % a.tiles;                // long ranges first
+    slice = idx / a.tiles;
+    at_tile = e * a.tiles + tile;
+  }
 
   Part p;
   int rows_all;                                        // rows with an output
@@ -400,8 +413,8 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
   l = pair_sum(l);
   if (!whole) {                                        // a slice: O relative to the offset, the offset and the sum
     if (live) {
-      const size_t rows = size_t(a.n) * H * a.n_split * a.tiles * kRowTile;
-      const size_t at = ((size_t(e) * H + h) * a.n_split + slice) * (size_t(a.tiles) * kRowTile) + row;
+      const size_t rows = work_rows(a, kRowTile);
+      const size_t at = work_at(a, at_tile, h, slice, kRowTile) + (row - row0);
       float* wp = a.work + at * kD + 4 * hl;
 #pragma unroll
       for (int mb = 0; mb < 4; ++mb)
@@ -449,8 +462,13 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
   int idx = blockIdx.x;
   const int h = idx % H;
   idx /= H;
-  const int e = idx % a.n;
-  const int slice = idx / a.n;
+  const int sequences = a.packed > 0 ? a.packed : a.n;
+  const int at_tile = idx % sequences, slice = idx / sequences;
+  int e = at_tile;
+  if (a.packed > 0) {
+    e = tile_place(a, at_tile, kFewRows).entry;
+    if (e < 0) return;
+  }
   if (e >= ((const const_i32*)a.step)[0]) return;
   const Part p = step_part(a, e);
   const int rows = p.count * G;
@@ -688,8 +706,8 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
     }
   }
   if (!whole) {
-    const size_t all = size_t(a.n) * H * a.n_split * kFewRows;
-    const size_t at = ((size_t(e) * H + h) * a.n_split + slice) * kFewRows + ln;
+    const size_t all = work_rows(a, kFewRows);
+    const size_t at = work_at(a, at_tile, h, slice, kFewRows) + ln;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       *reinterpret_cast<float4*>(a.work + at * kD + d0 + 8 * i) =
@@ -722,11 +740,20 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
   constexpr int kGroups = LANES / 16, kRows = 256 / LANES, kOwn = 64 / LANES;   // slices of a lane
   const int H = a.kv_heads, G = a.group;
   const int lane = threadIdx.x & (LANES - 1), c = lane & 15, grp = lane >> 4;
-  const int per = a.tiles * TILE;
-  const uint32_t blocks = uint32_t(a.longest_rows + kRows - 1) / kRows;
+  const uint32_t blocks = uint32_t((a.packed > 0 ? min(a.longest_rows, TILE) : a.longest_rows) + kRows - 1) / kRows;
   const int eh = int(blockIdx.x / blocks);
-  const int row = int(blockIdx.x % blocks) * kRows + threadIdx.x / LANES;
-  const int h = eh % H, e = eh / H;
+  int row = int(blockIdx.x % blocks) * kRows + threadIdx.x / LANES;
+  const int h = eh % H;
+  int e = eh / H, at_tile;                             // of the launch
+  if (a.packed > 0) {
+    at_tile = e;
+    const Place w = tile_place(a, at_tile, TILE);
+    if (w.entry < 0) return;
+    e = w.entry;
+    row += w.tile * TILE;
+  } else {
+    at_tile = e * a.tiles + row / TILE;
+  }
   if (e >= ((const const_i32*)a.step)[0]) return;
   const Part p = step_part(a, e);
   const int rows = p.count * G;
@@ -739,14 +766,13 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
   const int units = slice_units(range.count, a.slice, a.n_split);
   if (units >= range.count) return;                    // whole: written already
   const int n = (range.count + units - 1) / units;     // at most n_split <= 64
-  const size_t all = size_t(a.n) * H * a.n_split * per;
-  const size_t at = size_t(eh) * a.n_split * per + row;
+  const size_t all = work_rows(a, TILE), at = work_at(a, at_tile, h, 0, TILE) + (row - row0);
   const float2* mlp = reinterpret_cast<const float2*>(a.work + all * kD) + at;
   float f[kOwn], l[kOwn], mm = -INFINITY, lt = 0.f;
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) {
     float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane + LANES * i < n) ml = mlp[size_t(lane + LANES * i) * per];
+    if (lane + LANES * i < n) ml = mlp[(lane + LANES * i) * TILE];
     f[i] = ml.x;
     l[i] = ml.y;
     mm = fmaxf(mm, ml.x);
@@ -768,7 +794,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
       float4 v[4][2];
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const float4* vp = op + size_t(min(s0 + s * kGroups + grp, n - 1)) * per * (kD / 4);
+        const float4* vp = op + min(s0 + s * kGroups + grp, n - 1) * TILE * (kD / 4);
         v[s][0] = vp[0];
         v[s][1] = vp[1];
       }
@@ -797,18 +823,20 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
 
 template <int TILE, int UNIT>
 hipError_t launch_join(const AttnArgs& a, hipStream_t stream) {
-  const unsigned pairs = unsigned(a.n) * unsigned(a.kv_heads);
+  const unsigned pairs = unsigned(a.packed > 0 ? a.packed : a.n) * unsigned(a.kv_heads);
+  const int rows = a.packed > 0 ? std::min(a.longest_rows, TILE) : a.longest_rows;
   if (a.n_split <= 4)
-    join_kernel<TILE, UNIT, 16><<<unsigned(a.longest_rows + 15) / 16 * pairs, 256, 0, stream>>>(a);
+    join_kernel<TILE, UNIT, 16><<<unsigned(rows + 15) / 16 * pairs, 256, 0, stream>>>(a);
   else
-    join_kernel<TILE, UNIT, 64><<<unsigned(a.longest_rows + 3) / 4 * pairs, 256, 0, stream>>>(a);
+    join_kernel<TILE, UNIT, 64><<<unsigned(rows + 3) / 4 * pairs, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_attn_rows(const AttnArgs& a, bool paged, hipStream_t stream) {
-  const unsigned blocks = unsigned(a.kv_heads) * unsigned(a.n) * unsigned(a.tiles) * unsigned(a.n_split);
+  const unsigned tiles = a.packed > 0 ? unsigned(a.packed) : unsigned(a.n) * unsigned(a.tiles);
+  const unsigned blocks = unsigned(a.kv_heads) * tiles * unsigned(a.n_split);
   if (paged)
     attn_rows_kernel<true><<<blocks, 256, 0, stream>>>(a);
   else
@@ -819,7 +847,7 @@ hipError_t launch_attn_rows(const AttnArgs& a, bool paged, hipStream_t stream) {
 }
 
 hipError_t launch_attn_few(const AttnArgs& a, hipStream_t stream) {
-  const unsigned blocks = unsigned(a.kv_heads) * unsigned(a.n) * unsigned(a.n_split);
+  const unsigned blocks = unsigned(a.kv_heads) * unsigned(a.packed > 0 ? a.packed : a.n) * unsigned(a.n_split);
   attn_few_kernel<<<blocks, 256, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_split == 1) return e;

@@ -1,8 +1,8 @@
 // Device helpers shared by the token attention kernels (gfx950).
 #pragma once
 
-#include "../launch_tokens.h"
 #include "attn_common.h"
+#include "token_step.h"
 
 namespace uf {
 namespace tok {
@@ -90,6 +90,22 @@ __device__ inline Part step_part(const AttnArgs& a, int e) {
   p.count = min(w[2], a.total - w[1]);
   p.held = w[3] - w[2];
   return p;
+}
+// The sequence and tile of a launch's tile k, where it deals workgroups to the tiles there are.
+__device__ inline Place tile_place(const AttnArgs& a, int k, int tile_rows) {
+  Place w = place_of(a.step, a.n, k, [&](const int32_t* entry) {
+    const int rows = min(entry[2], a.total - entry[1]) * a.group;
+    return rows < a.least_rows || rows > a.most_rows ? 0 : min((rows + tile_rows - 1) / tile_rows, a.tiles);
+  });
+  if (uint32_t(w.tile) >= uint32_t(a.tiles)) w.entry = -1;
+  return w;
+}
+// Where a launch's partial results of a (tile, key head, slice) start, in rows, and their number.
+__device__ inline size_t work_at(const AttnArgs& a, int tile, int h, int slice, int tile_rows) {
+  return ((size_t(tile) * a.kv_heads + h) * a.n_split + slice) * tile_rows;
+}
+__device__ inline size_t work_rows(const AttnArgs& a, int tile_rows) {
+  return work_at(a, a.packed > 0 ? a.packed : a.n * a.tiles, 0, 0, tile_rows);
 }
 
 }  // namespace tok

@@ -7,7 +7,7 @@
 // and are checked before they are used: what lies outside is skipped, or read as zeros.
 #include <cstring>
 
-#include "../launch_tokens.h"
+#include "token_step.h"
 
 namespace uf {
 namespace tok {
@@ -149,21 +149,28 @@ __global__ __launch_bounds__(kThreads) void keep_fresh_kernel(Worded<KeepHead, N
 // workgroups would find nothing: write_kernel.
 template <int T>
 __global__ __launch_bounds__(kThreads) void write_pages_kernel(WriteArgs a, int spans) {
-  const int e = blockIdx.y;
+  const int H = a.pool.kv_heads;
+  int e = blockIdx.y, kvh = blockIdx.x / spans, s = blockIdx.x % spans;
+  if (a.packed > 0) {                        // spans: of all sequences
+    const Place w = place_of(a.step, a.n, s, [&](const int32_t* entry) {
+      return write_spans(min(entry[2], a.total - entry[1]), T);
+    });
+    if (w.entry < 0) return;
+    e = w.entry;
+    s = w.tile;
+  }
   typedef __attribute__((address_space(4))) int32_t uniform_i32;
   const uniform_i32* step = (const uniform_i32*)a.step;
   const uniform_i32* entry = step + kHeader + kEntry * e;
   if (e >= step[0]) return;
   const int seq = entry[0], at = entry[1], count = min(entry[2], a.total - at), first = entry[3] - entry[2];
-  const int H = a.pool.kv_heads;
-  const int kvh = blockIdx.x / spans;
   const uniform_i32* pages = (const uniform_i32*)(a.table + size_t(seq) * a.row);
   constexpr int kPer = T * kRowChunks / kThreads, kSlots = kThreads / kRowChunks;
   const int c = threadIdx.x % kRowChunks, slot = threadIdx.x / kRowChunks;
   const bool isv = kvh >= H;
   const int64_t ts = isv ? a.v_token : a.k_token;
   const uint16_t* src = isv ? a.v + int64_t(kvh - H) * a.v_head : a.k + int64_t(kvh) * a.k_head;
-  for (int s = blockIdx.x % spans; ; s += spans) {
+  for (; ; s += spans) {
     const int64_t p0 = (int64_t(first) / T + s) * T;     // first position of the page
     if (p0 >= int64_t(first) + count) return;
     const int page = pages[p0 / T];
@@ -293,8 +300,8 @@ hipError_t launch_keep_fresh(const KeepArgs& a, hipStream_t stream) {
 hipError_t launch_write(const WriteArgs& a, hipStream_t stream) {
   if (a.longest >= 16) {
     const int T = a.pool.page_tokens;
-    const int spans = (a.longest - 1 + T - 1) / T + 1;   // pages that so many tokens can touch
-    const dim3 grid(unsigned(spans) * 2 * unsigned(a.pool.kv_heads), unsigned(a.n));
+    const int spans = a.packed > 0 ? a.packed : write_spans(a.longest, T);
+    const dim3 grid(unsigned(spans) * 2 * unsigned(a.pool.kv_heads), a.packed > 0 ? 1 : unsigned(a.n));
     if (T == 128)
       write_pages_kernel<128><<<grid, kThreads, 0, stream>>>(a, spans);
     else

@@ -82,7 +82,12 @@ struct WriteArgs {
   const int32_t* step;
   const int32_t* table;
   int32_t n, longest, total, row;             // row: pages of a table row
+  int32_t packed;                             // pages of all sequences, where workgroups are dealt to those; or 0
 };
+// Pages that so many new tokens of a sequence touch at most.
+__host__ __device__ inline int write_spans(int count, int page_tokens) {
+  return count > 0 ? (count - 1 + page_tokens - 1) / page_tokens + 1 : 0;
+}
 hipError_t launch_write(const WriteArgs& a, hipStream_t stream);
 
 // Attention forward, from the cache or from plain tensors.
@@ -107,18 +112,15 @@ struct AttnArgs {
   int32_t q_heads, kv_heads, group, window, sinks;
   float scale_log2;
   int32_t tiles;                              // row tiles of the longest sequence
+  int32_t packed;                             // row tiles of all sequences, where workgroups are dealt to those; 0: `tiles` each
   int32_t least_rows, most_rows;              // sequences with other numbers of rows are not this launch's
   int32_t longest_rows;                       // the most rows of one of its sequences
   int32_t slice;                              // units of keys of a slice at least
   int32_t n_split;                            // slices at most
-  float* work;                                // partials: O [row][D], then (offset, sum) [row]
+  float* work;                                // partials: O [tile][kv head][slice][row][D], then (offset, sum) of the same
 };
 constexpr int kRowTile = 128, kKeyUnit = 64;          // prompts: rows and keys of a tile
 constexpr int kFewRows = 32, kFewUnit = 32;           // few rows: rows of a workgroup, keys of a unit
-// rows (token, head of the group) of partial results of a launch
-inline size_t work_rows(const AttnArgs& a, int tile_rows) {
-  return size_t(a.n) * a.kv_heads * a.n_split * a.tiles * tile_rows;
-}
 hipError_t launch_attn_rows(const AttnArgs& a, bool paged, hipStream_t stream);
 hipError_t launch_attn_few(const AttnArgs& a, hipStream_t stream);
 

@@ -248,6 +248,13 @@ int check_scale(float scale, float* log2) {
   return UF_OK;
 }
 
+// Workgroups go to the tiles that sequences have (`tiles`; their waves look up whose theirs is), not to as many for each
+// sequence as the longest has (`each`), where most of those would find nothing; 0: for each.  Measured (us, for each / to
+// what there is): 255 single tokens and a piece of 512 over 1,000 earlier ones, 8 key heads, attention 408 / 237, write 32 /
+// 11, and 4,160 / 16 MiB of scratch; 7 x 64 and 512 tokens 58 / 36.5; near to even, 3 x 256 and 512 tokens, 45.6 / 44.4; 1,023
+// of 1,024 sequences with few rows 304 / 420: looking up costs a round of 64 sequences after the other.
+int32_t deal_packed(int64_t each, int64_t tiles) { return each > 2 * tiles && tiles <= INT32_MAX ? int32_t(tiles) : 0; }
+
 int check_fork(uft_cache* c, int32_t n, const int32_t* src, const int32_t* dst) {
   if (int s = check_seqs(c, n, dst, "dst")) return s;
   if (src == nullptr) return fail(UF_ERR_ARG, "src is null");
@@ -359,18 +366,18 @@ int uft_extend(uft_cache* c, int32_t n, const int32_t* seqs, const int32_t* coun
     step.reserve(size_t(n));
     copies.reserve(3 * shared.size());
     poke.dense = {n, int32_t(total), 0, 0};
-    std::vector<int32_t> gone;         // one entry per use given up so far
-    gone.reserve(shared.size());
+    std::vector<int32_t> gone(shared.size(), 0);   // uses given up so far, at a page's first place in `shared`
     int32_t at = 0;
     for (int32_t i = 0; i < n; ++i) {
       const Seq& q = c->seqs[size_t(seqs[i])];
       Grown& g = grown[size_t(i)];
       if (counts[i] > 0 && q.tokens % T != 0) {
         const int32_t last = q.pages.back();
-        if (c->uses[size_t(last)] - int32_t(std::count(gone.begin(), gone.end(), last)) > 1) {
+        const size_t at = size_t(std::lower_bound(shared.begin(), shared.end(), last) - shared.begin());
+        if (c->uses[size_t(last)] > 1 && c->uses[size_t(last)] - gone[at] > 1) {
           g.old = last;
           g.own = taken.take();
-          gone.push_back(last);
+          ++gone[at];
           copies.insert(copies.end(), {last, g.own, q.tokens % T});
           poke.run(c->row_at(seqs[i]) + int32_t(q.pages.size()) - 1, &g.own, 1);
         }
@@ -430,6 +437,9 @@ int uft_write(const uft_cache* c, int32_t layer, const void* d_k, const uft_stri
     a.longest = c->step_longest;
     a.total = c->step_tokens;
     a.row = c->row;
+    int64_t spans = 0;
+    for (const Entry& e : c->step) spans += tok::write_spans(e.count, c->d.page_tokens);
+    a.packed = deal_packed(int64_t(a.n) * tok::write_spans(a.longest, c->d.page_tokens), spans);
     if (int s = check_hip(tok::launch_write(a, static_cast<hipStream_t>(stream)), "token write")) return s;
     return ok();
   });
@@ -727,10 +737,12 @@ int uft_seq_pages(const uft_cache* c, int32_t seq, int32_t* pages, int32_t cap, 
 
 namespace {
 
+constexpr double kMostGroups = 16777215.0;   // workgroups of a launch: 2^32 - 1 threads
+
 // One launch over the sequences of a step whose rows number least .. most.
 struct Launch {
   bool run = false;
-  int32_t least = 0, most = 0, longest = 0, tiles = 0, slice = 0, n_split = 1;
+  int32_t least = 0, most = 0, longest = 0, tiles = 0, packed = 0, slice = 0, n_split = 1;
   size_t work_rows = 0;
 };
 
@@ -791,7 +803,7 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
   const int32_t H = c->d.kv_heads, G = d->q_heads / H, n = int32_t(c->step.size());
   const int32_t sinks = std::min(d->sinks, c->d.max_tokens);
   std::vector<int32_t> few, rows;
-  int64_t tiles = 0;
+  int64_t tiles = 0, all_tiles = 0;
   int64_t few_rows = 0, many_rows = 0;
   for (const Entry& e : c->step) {
     const int64_t r = int64_t(e.count) * G;
@@ -804,6 +816,7 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
     }
     const int64_t t = (r + tok::kRowTile - 1) / tok::kRowTile;
     tiles = std::max(tiles, t);
+    all_tiles += t;
     for (int64_t k = 0; k < t && rows.size() < size_t(8) * 65536; ++k) {
       const int32_t a = int32_t(k * tok::kRowTile / G);
       const int32_t b = int32_t(std::min(r, (k + 1) * tok::kRowTile) - 1) / G;
@@ -821,7 +834,7 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
     p->few.longest = int32_t(few_rows);
     p->few.tiles = 1;
     choose_slices(few, H, d->n_cu, Cost{d->n_cu, 4, 1.0, 6.0, 8.0, 0.004}, &p->few);
-    p->few.work_rows = p->few.n_split > 1 ? size_t(n) * H * p->few.n_split * tok::kFewRows : 0;
+    p->few.packed = deal_packed(n, int64_t(few.size()));
   }
   if (!rows.empty()) {
     p->rows.run = true;
@@ -830,10 +843,16 @@ int plan_attn(const uft_cache* c, const uft_attn_desc* d, Plan* p) {
     p->rows.longest = int32_t(many_rows);
     p->rows.tiles = int32_t(tiles);
     choose_slices(rows, H, d->n_cu, Cost{int64_t(2) * d->n_cu, 2, 0.72, 4.0, 2.0, 0.014}, &p->rows);
-    p->rows.work_rows = p->rows.n_split > 1 ? size_t(n) * H * p->rows.n_split * size_t(tiles) * tok::kRowTile : 0;
+    p->rows.packed = deal_packed(n * tiles, all_tiles);
   }
-  const double grid = double(n) * H * std::max(double(tiles) * p->rows.n_split, 64.0);
-  if (grid > 2147483647.0 || double(many_rows) > 2.0e9) return fail(UF_ERR_ARG, "step too large for one launch");
+  for (Launch* l : {&p->few, &p->rows}) {
+    const int32_t rows = l == &p->few ? tok::kFewRows : tok::kRowTile;
+    const double groups = (l->packed > 0 ? double(l->packed) : double(n) * l->tiles) * H * l->n_split;
+    // (a join takes a workgroup per four rows at least)
+    if (groups > kMostGroups || (l->n_split > 1 && groups / l->n_split * (rows / 4) > kMostGroups) || double(many_rows) > 2.0e9)
+      return fail(UF_ERR_ARG, "step too large for one launch");
+    if (l->n_split > 1) l->work_rows = size_t(groups) * size_t(rows);
+  }
   p->bytes = (p->few.work_rows + p->rows.work_rows) * (tok::kD + 2) * 4;
   return UF_OK;
 }
@@ -901,6 +920,7 @@ int uft_attn(const uft_cache* c, int32_t layer, const uft_attn_desc* d, const vo
       a.most_rows = l->most;
       a.longest_rows = l->longest;
       a.tiles = l->tiles;
+      a.packed = l->packed;
       a.slice = l->slice;
       a.n_split = l->n_split;
       const hipError_t e = l == &p.few ? tok::launch_attn_few(a, st) : tok::launch_attn_rows(a, true, st);
@@ -926,7 +946,7 @@ int check_window(const uft_window_desc* d, float* log2) {
   if (d->tokens > (1 << 30)) return fail(UF_ERR_ARG, "tokens must be at most 2^30");
   if (d->window < 0 || d->sinks < 0) return fail(UF_ERR_ARG, "window and sinks must be >= 0");
   const double group = d->q_heads / d->kv_heads;
-  if (double(d->batch) * d->kv_heads * (std::ceil(d->tokens * group / 128.0) + 2.0) > 5.0e8 ||
+  if (double(d->batch) * d->kv_heads * (std::ceil(d->tokens * group / 128.0) + 2.0) > kMostGroups ||
       d->tokens * group > 2.0e9)
     return fail(UF_ERR_ARG, "shape too large: batch * q_heads * tokens");
   if (int s = check_stride(&d->q, "q stride")) return s;

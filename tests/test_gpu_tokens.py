@@ -498,6 +498,68 @@ def test_many_sequences_in_one_call():
     _compare(cache, model, 1, 2)
 
 
+@pytest.mark.parametrize("kv,group,n,usual,others,held,window,sinks", [
+    (2, 4, 150, 1, {70: 200, 140: 37}, 300, 0, 0),       # single tokens with two pieces of prompts, cut into slices
+    (1, 3, 66, 1, {65: 500}, 20, 64, 5),
+    (1, 40, 130, 0, {129: 4}, 150, 0, 0),                # tiles of one sequence at the end, the others do not grow
+    (1, 2, 90, 17, {64: 1, 89: 3}, 2000, 0, 0),          # few rows beside many, over long ones
+    (2, 1, 70, 20, {3: 700}, 65, 50, 2)])                # 33 rows and more only in one sequence
+def test_steps_whose_sequences_grow_unequally(kv, group, n, usual, others, held, window, sinks):
+    """A step of more than 64 sequences most of which bring other numbers of tokens than the longest, and a captured layer
+    of such a step."""
+    P = require_gpu()
+    counts = [others.get(i, usual) for i in range(n)]
+    lengths = [held if i in others or held < 1000 else 5 + i for i in range(n)]
+    pages = sum(-(-(a + 4 * b) // 64) for a, b in zip(lengths, counts)) + 2
+    cache = P.TokenCache(1, kv, pages, n, max(lengths) + 4 * max(counts), 64)
+    poison(cache)
+    seqs = [int(s) for s in np.random.default_rng(n).permutation(n)]
+    fill(cache, seqs, lengths, 1)
+    fill(cache, seqs, counts, 30)
+    total = sum(counts)
+    q = draw((total, kv * group, D), 7)
+    log(f"unequal: kv={kv} group={group} n={n} usual={usual} others={others}")
+    need = cache.work_bytes(kv * group, window, sinks)
+    work = torch.full((need + 256,), 0x5A, dtype=torch.uint8, device="cuda")
+    out = cache.attention(0, q, window, sinks, lse=True, work=work[:need] if need else None)
+    torch.cuda.synchronize()
+    assert (work[need:] == 0x5A).all()
+    check_step(cache, 0, q, out, window, sinks, what="unequal", seqs=seqs, counts=counts)
+
+    k, v = draw((total, kv, D), 8), draw((total, kv, D), 9)
+    o, lse = torch.empty_like(q), torch.empty((total, kv * group), device="cuda")
+    cache.extend(seqs, counts)
+    work = torch.empty(cache.work_bytes(kv * group, window, sinks) + 16, dtype=torch.uint8, device="cuda")
+
+    def layer():
+        cache.write(0, k, v)
+        cache.attention(0, q, window, sinks, out=o, lse=lse, work=work)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        layer()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer()
+    for turn in range(3):
+        order = list(seqs)
+        if turn == 1:                                    # the same counts in the same places, other sequences
+            same = [i for i in range(n) if i not in others]
+            for i, j in zip(same, same[1:] + same[:1]):
+                order[i] = seqs[j]
+        if turn:
+            cache.extend(order, counts)
+        for t, seed in ((k, 10), (v, 11), (q, 12)):
+            t.copy_(draw(t.shape, 100 * turn + seed))
+        o.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_step(cache, 0, q, (o, lse), window, sinks, what=f"replay {turn}", seqs=order, counts=counts)
+
+
 def test_a_speculative_run_equals_the_plain_one():
     """Prompt, draft trees, the accepted path kept, pages trimmed and packed: attention as of a sequence that
     holds only the accepted tokens, at every step."""

@@ -233,6 +233,21 @@ def test_refusals(P):
     assert status(lambda: T.uft_window_bwd(w(), *[None] * 11)) == ARG
 
 
+@pytest.mark.parametrize("held,new,one,one_held", [(4000, 1, 512, 4000), (10, 16, 1, 100000), (900, 1, 700, 0), (300, 9, 8, 5000)])
+def test_scratch_follows_the_sequences_that_are_cut(P, held, new, one, one_held):
+    """A sequence beside 200 others that bring other numbers of rows: the step's scratch is at most twice that of the two
+    kinds in steps of their own."""
+    c = _dry(P, 60000, 201, 200000, kv_heads=8)
+    c.n_cu = 256
+    c.extend(list(range(201)), [one_held] + [held] * 200)
+    need = []
+    for seqs, counts in (([0], [one]), (list(range(1, 201)), [new] * 200), (list(range(201)), [one] + [new] * 200)):
+        c.extend(seqs, counts)
+        need.append(c.work_bytes(32))
+        c.keep(seqs, [c.tokens(s) - n for s, n in zip(seqs, counts)], [0] * len(seqs))
+    assert need[2] <= 2 * (need[0] + need[1]), need
+
+
 def test_integers_that_32_bits_cannot_hold(P):
     c = _dry(P)
     c.extend([0], [5])
