@@ -696,14 +696,14 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
   asm volatile("" : "+v"(r_out));
   if (r_out >= a.tokens * G) return;
   uint16_t* const dst = target(r_out);
-  const float f = r_out < rows ? a.scale : 0.f;        // (padding accumulated zeros)
+  const bool on = r_out < rows;                        // padding gets zeros
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       uint2 u;
-      u.x = pack_bf16x2(dqt[mb][4 * k] * f, dqt[mb][4 * k + 1] * f);
-      u.y = pack_bf16x2(dqt[mb][4 * k + 2] * f, dqt[mb][4 * k + 3] * f);
+      u.x = on ? pack_bf16x2(dqt[mb][4 * k] * a.scale, dqt[mb][4 * k + 1] * a.scale) : 0;
+      u.y = on ? pack_bf16x2(dqt[mb][4 * k + 2] * a.scale, dqt[mb][4 * k + 3] * a.scale) : 0;
       *reinterpret_cast<uint2*>(dst + mb * 32 + 8 * k) = u;
     }
 }

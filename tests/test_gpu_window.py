@@ -152,6 +152,22 @@ def test_values_that_are_not_finite_reach_only_rows_that_see_them(kind):
     _only_those_that_see(f64(q)[0, :, 3:], o[:, 3:], lse[:, 3:], f64(k)[0, :, 1:], f64(v)[0, :, 1:], see, bad)
 
 
+def test_padding_has_zero_gradients_beside_values_that_are_not_finite():
+    P = require_gpu()
+    lengths = torch.tensor([70, 200, 1], dtype=torch.int32, device="cuda")
+    q, k, v, do = (draw((3, 300, h, D), i) for i, h in enumerate((6, 2, 2, 6)))
+    for t in (k, v):
+        t[:, [0, 60, 190]] = float("nan")
+    o, lse = P.window_attention(q, k, v, 30, 3, lengths=lengths)
+    grads = P.window_attention_bwd(q, k, v, o, lse, do, 30, 3, lengths=lengths)
+    torch.cuda.synchronize()
+    for g in (o, *grads):
+        for b, n in enumerate((70, 200, 1)):
+            assert not g[b, n:].any()
+            assert g[b, :n].isnan().any()
+    assert (lse.transpose(1, 2)[1, 200:] == -float("inf")).all()
+
+
 def test_the_same_bits_again_on_another_stream_and_from_a_graph():
     P = require_gpu()
     q, do = draw((1, 700, 4, D), 1), draw((1, 700, 4, D), 2)
