@@ -10,9 +10,9 @@
 //
 // Kernels, all with 32x32x16 bf16 MFMA and fp32 accumulation:
 //  * dq: one workgroup of four waves per 128 rows, two per CU: delta from the rows' dO and
-//    O, then per 32 keys S^T = K Q^T, dP^T = V dO^T, dS^T and dQ^T += K^T dS^T.  It leaves
-//    -LSE/scale (-inf where there is no row, so that its weights vanish) and -delta in
-//    the workspace, the seeds of dkdv's S and dP accumulators;
+//    O, then per 32 keys S^T = K Q^T, dP^T = V dO^T, dS^T and dQ^T += K^T dS^T (dS in two
+//    parts).  It leaves -LSE/scale (-inf where there is no row, so that its weights vanish)
+//    and -delta in the workspace, the seeds of dkdv's S and dP accumulators;
 //  * dkdv: one workgroup of eight waves per 128 keys of a head.  Waves w and w + 4
 //    share 32 keys: wave w computes S = Q K^T and P, hands P to wave w + 4 through LDS
 //    and accumulates dV^T += dO^T P, while wave w + 4 computes dP = dO V^T and, one unit
@@ -477,11 +477,13 @@ __global__ __launch_bounds__(256) void sum_kernel(BwdArgs a, Cut cut, const floa
 // ------------------------------------------------------------------ dq ----
 //
 // The walk, the unit's layout and its copies are the forward's (token_attn.hip).  What
-// bounds it: three products per pair on the matrix cores, busy 63 % of the cycles at 1.7
-// GHz: 1,060 TFLOP/s at 16,384 tokens, 32 heads over 8, window 2,048 (730 us).  Two
+// bounds it: four products per pair on the matrix cores, busy 66 % of the cycles at 1.75
+// GHz: 1,135 TFLOP/s at 16,384 tokens, 32 heads over 8, window 2,048 (908 us).  Two
 // operands are read ahead: three to six, which the registers hold too, changed nothing.
-// dS is rounded to bf16 for its product, which with delta from the rounded O is what dQ
-// is off by beyond its own rounding.
+// dS goes to its product in two bf16 parts, its rounding and the remainder: rounded once it
+// is the largest part of dQ's error (2.8e-3 of dQ, now 2.1e-3, of which 1.7e-3 are dQ's own
+// rounding and the rest delta from the rounded O).  The remainder's product costs 200 us of
+// a backward of 1,950 at that size, in whichever order the two are issued.
 constexpr uint32_t kUnitBytes = 32768;
 
 __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
@@ -614,7 +616,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
   };
   auto body = [&](const Unit& cur, const Unit& next, uint32_t nbuf) {
     f32x16 sv[2], dp[2];
-    bf16x8 op[2][2], x[48];
+    bf16x8 op[2][2], rest[2][2], x[48];   // dS and what its rounding leaves
     const Offsets no = offsets(next);
     const bool full = cur.key0 + 63 <= pmin &&
                       (a.window == 0 || cur.key0 >= pmax - a.window + 1 || cur.key0 + 63 < a.sinks);
@@ -629,8 +631,13 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
     };
     auto weight = [&](int n, int r) { sv[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[n][r], c2, nl)); };
     auto ds = [&](int n, int e) {
-      op[n][e >> 2][2 * (e & 3)] = (__bf16)(sv[n][2 * e] * (dp[n][2 * e] + nd));
-      op[n][e >> 2][2 * (e & 3) + 1] = (__bf16)(sv[n][2 * e + 1] * (dp[n][2 * e + 1] + nd));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int at = 2 * (e & 3) + i;
+        const float d = sv[n][2 * e + i] * (dp[n][2 * e + i] + nd);
+        op[n][e >> 2][at] = (__bf16)d;
+        rest[n][e >> 2][at] = (__bf16)(d - float(op[n][e >> 2][at]));
+      }
     };
 #pragma unroll
     for (int k = 0; k < kReads; ++k) x[k] = load(k);
@@ -648,6 +655,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
             dp[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[k], of[j], j ? dp[n] : f32x16{}, 0, 0, 0);
         } else {
           dqt[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[k], op[(k0 - kSP) >> 3][j >> 2], dqt[j & 3], 0, 0, 0);
+          dqt[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[k], rest[(k0 - kSP) >> 3][j >> 2], dqt[j & 3], 0, 0, 0);
         }
         if (k + kReads < 48) x[k + kReads] = load(k + kReads);
         if constexpr (k0 < kSP && (k0 & 8) != 0) {     // beside dP of a block: its weights
@@ -660,7 +668,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
         fence();
       }
       if constexpr (k0 < kSP && (k0 & 8) != 0) asm volatile("" : "+v"(sv[k0 >> 4]));
-      if constexpr (k0 == 16) asm volatile("" : "+v"(op[0][0]), "+v"(op[0][1]));
+      if constexpr (k0 == 16) asm volatile("" : "+v"(op[0][0]), "+v"(op[0][1]), "+v"(rest[0][0]), "+v"(rest[0][1]));
     };
     eight(std::integral_constant<int, 0>{});
     mask(0);
