@@ -76,8 +76,10 @@ def load():
     return _lib
 
 
-def _ints(values):
-    """Host integers as an array (which the caller holds during the call)."""
+def ints(values):
+    """Host integers as the library reads them, an array of int32 (which the caller holds during the call)."""
+    if isinstance(values, array.array) and values.typecode == "i":
+        return values
     if hasattr(values, "data_ptr"):
         raise TypeError("sequences, counts and starts are host integers, not a tensor")
     return array.array("i", values)
@@ -123,7 +125,7 @@ def uft_destroy(handle) -> None:
 
 def uft_extend(handle, seqs, counts, stream=None) -> None:
     _same(seqs, counts, "seqs and counts")
-    s, c = _ints(seqs), _ints(counts)
+    s, c = ints(seqs), ints(counts)
     L._check(load().uft_extend(handle, len(s), _at(s), _at(c), stream))
 
 
@@ -133,30 +135,30 @@ def uft_write(handle, layer, k, k_stride, v, v_stride, stream=None) -> None:
 
 def uft_fork(handle, src, dst, stream=None) -> None:
     _same(src, dst, "src and dst")
-    s, d = _ints(src), _ints(dst)
+    s, d = ints(src), ints(dst)
     L._check(load().uft_fork(handle, len(s), _at(s), _at(d), stream))
 
 
 def uft_copy(handle, src, dst, stream=None) -> None:
     _same(src, dst, "src and dst")
-    s, d = _ints(src), _ints(dst)
+    s, d = ints(src), ints(dst)
     L._check(load().uft_copy(handle, len(s), _at(s), _at(d), stream))
 
 
 def uft_keep(handle, seqs, starts, counts, index=None, stream=None) -> None:
     _same(seqs, starts, "seqs and starts")
     _same(seqs, counts, "seqs and counts")
-    s, a, c = _ints(seqs), _ints(starts), _ints(counts)
+    s, a, c = ints(seqs), ints(starts), ints(counts)
     L._check(load().uft_keep(handle, len(s), _at(s), _at(a), _at(c), L._ptr(index), stream))
 
 
 def uft_trim(handle, seqs, window, sinks, stream=None) -> None:
-    s = _ints(seqs)
+    s = ints(seqs)
     L._check(load().uft_trim(handle, len(s), _at(s), window, sinks, stream))
 
 
 def uft_free(handle, seqs) -> None:
-    s = _ints(seqs)
+    s = ints(seqs)
     L._check(load().uft_free(handle, len(s), _at(s)))
 
 

@@ -151,6 +151,7 @@ class TokenCache:
     # -- pages ------------------------------------------------------------------
     def extend(self, seqs, counts, stream=None):
         """Begin a step: sequence seqs[i] grows by counts[i] tokens."""
+        counts = T.ints(counts)
         self._run(stream, lambda s: T.uft_extend(self.handle, seqs, counts, s))
         self._step = sum(counts)
         self._need = {}
@@ -177,6 +178,7 @@ class TokenCache:
     def keep(self, seqs, starts, counts, index=None, stream=None):
         """Sequence seqs[i] keeps its first starts[i] tokens, then the tokens at the next counts[i] positions of ``index``
         (int32, on the device), moved up behind them."""
+        counts = T.ints(counts)
         if index is not None and not self.dry:
             _dense(index, "index", (sum(counts),), torch.int32, self.device)
         if index is None and any(counts):

@@ -1,0 +1,29 @@
+"""Calls of the token operators that need no GPU: what the wrappers hand on, and when a step ends."""
+
+import array
+
+import numpy as np
+import pytest
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2606_09150_amd as pkg
+    pkg.load()
+    return pkg
+
+
+def _dry(P, n_pages=40, max_seqs=6, max_tokens=700, page=64, layers=2, kv_heads=3):
+    return P.TokenCache(layers, kv_heads, n_pages, max_seqs, max_tokens, page, flags=P._lib.UF_F_DRYRUN)
+
+
+@pytest.mark.parametrize("kind", [np.uint8, np.int16, np.int32, np.int64])
+def test_counts_of_any_integer_type_add_up(P, kind):
+    """The step's tokens are what the library counts, also where the counts' own type cannot hold their sum."""
+    c = _dry(P, n_pages=1200, max_seqs=2, max_tokens=40000)
+    counts = np.array([200, 100] if kind is np.uint8 else [20000, 20000], kind)
+    c.extend(np.arange(2), counts)
+    assert c.step_tokens() == c.info().step_tokens == sum(counts.tolist())
+    c.extend([0], array.array("H", [7]))
+    assert c.step_tokens() == 7
+
