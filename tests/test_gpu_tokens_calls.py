@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from tests.gpu_common import f64, require_gpu
 from tests.test_gpu_tokens import D, check_step, draw, poison, read
 
 pytestmark = pytest.mark.gpu
