@@ -80,8 +80,8 @@ def ints(values):
     """Host integers as the library reads them, an array of int32 (which the caller holds during the call)."""
     if isinstance(values, array.array) and values.typecode == "i":
         return values
-    if hasattr(values, "data_ptr"):
-        raise TypeError("sequences, counts and starts are host integers, not a tensor")
+    if hasattr(values, "data_ptr") or isinstance(values, (bytes, bytearray)):   # (an array would take those as its memory)
+        raise TypeError(f"sequences, counts and starts are host integers, not {type(values).__name__}")
     return array.array("i", values)
 
 
@@ -124,8 +124,8 @@ def uft_destroy(handle) -> None:
 
 
 def uft_extend(handle, seqs, counts, stream=None) -> None:
-    _same(seqs, counts, "seqs and counts")
     s, c = ints(seqs), ints(counts)
+    _same(s, c, "seqs and counts")
     L._check(load().uft_extend(handle, len(s), _at(s), _at(c), stream))
 
 
@@ -134,21 +134,21 @@ def uft_write(handle, layer, k, k_stride, v, v_stride, stream=None) -> None:
 
 
 def uft_fork(handle, src, dst, stream=None) -> None:
-    _same(src, dst, "src and dst")
     s, d = ints(src), ints(dst)
+    _same(s, d, "src and dst")
     L._check(load().uft_fork(handle, len(s), _at(s), _at(d), stream))
 
 
 def uft_copy(handle, src, dst, stream=None) -> None:
-    _same(src, dst, "src and dst")
     s, d = ints(src), ints(dst)
+    _same(s, d, "src and dst")
     L._check(load().uft_copy(handle, len(s), _at(s), _at(d), stream))
 
 
 def uft_keep(handle, seqs, starts, counts, index=None, stream=None) -> None:
-    _same(seqs, starts, "seqs and starts")
-    _same(seqs, counts, "seqs and counts")
     s, a, c = ints(seqs), ints(starts), ints(counts)
+    _same(s, a, "seqs and starts")
+    _same(s, c, "seqs and counts")
     L._check(load().uft_keep(handle, len(s), _at(s), _at(a), _at(c), L._ptr(index), stream))
 
 

@@ -27,3 +27,15 @@ def test_counts_of_any_integer_type_add_up(P, kind):
     c.extend([0], array.array("H", [7]))
     assert c.step_tokens() == 7
 
+
+
+def test_host_integers_are_counted_as_they_are_handed_on(P):
+    c = _dry(P)
+    for seqs, counts in (([0, 1, 2, 3], b"\1\0\0\0"), (b"\0\0\0\0", [1]), (bytearray(4), bytearray(4))):
+        with pytest.raises((TypeError, ValueError)):
+            c.extend(seqs, counts)
+        with pytest.raises((TypeError, ValueError)):
+            c.keep(seqs, counts, counts, np.zeros(1))
+        with pytest.raises((TypeError, ValueError)):
+            c.fork(seqs, counts)
+    assert c.info().step_seqs == 0 and c.tokens(0) == 0
