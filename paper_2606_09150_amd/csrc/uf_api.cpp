@@ -192,7 +192,7 @@ int uf_kv_create(const uf_kv_desc* desc, void* d_pool, size_t pool_bytes, uf_kv*
 
 int uf_kv_destroy(uf_kv* kv) {
   delete kv;
-  return ok();
+  return UF_OK;   // (the last error's text stays: a garbage collector may call this between an error and its reader)
 }
 
 namespace {

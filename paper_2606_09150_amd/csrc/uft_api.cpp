@@ -321,7 +321,7 @@ int uft_create(const uft_desc* desc, void* d_pool, size_t pool_bytes, void* d_ta
 
 int uft_destroy(uft_cache* cache) {
   delete cache;
-  return ok();
+  return UF_OK;   // (the last error's text stays, as in uf_kv_destroy)
 }
 
 int uft_extend(uft_cache* c, int32_t n, const int32_t* seqs, const int32_t* counts, void* stream) {

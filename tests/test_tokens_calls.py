@@ -39,3 +39,17 @@ def test_host_integers_are_counted_as_they_are_handed_on(P):
         with pytest.raises((TypeError, ValueError)):
             c.fork(seqs, counts)
     assert c.info().step_seqs == 0 and c.tokens(0) == 0
+
+
+def test_a_handle_that_goes_leaves_the_last_errors_text(P):
+    """Handles are closed whenever Python collects them: also between a failed call and the reader of its text."""
+    L = P._lib
+    window = P.KVWindow(1, 1, 300, 128, 2, flags=L.UF_F_DRYRUN)
+    cache, other = _dry(P), _dry(P)
+    for close in (cache.close, window.close):
+        with pytest.raises(P.UfError):
+            other.extend([77], [1])
+        text = L.uf_last_error()
+        assert "77" in text
+        close()
+        assert L.uf_last_error() == text
