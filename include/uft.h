@@ -80,9 +80,10 @@ int uft_destroy(uft_cache* cache); /* NULL is accepted */
  * own first (all layers).  The new tokens' rows are written by uft_write and
  * attended by uft_attn, layer by layer; both act on the last step, in whose order
  * tokens are counted: sequence by sequence.  A step no longer holds once one of
- * its sequences is kept or freed.  A sequence appears once.  A captured graph of
- * uft_write and uft_attn reads the step from the tables when it is replayed: it may
- * be replayed after any later step of as many sequences with the same counts.
+ * its sequences is kept or freed, or trimmed of the step's own tokens.  A sequence
+ * appears once.  A captured graph of uft_write and uft_attn reads the step from the
+ * tables when it is replayed: it may be replayed after any later step of as many
+ * sequences with the same counts.
  * Errors: UF_ERR_ARG, UF_ERR_CAPACITY (no free pages, or longer than max_tokens),
  * UF_ERR_HIP. */
 int uft_extend(uft_cache* cache, int32_t n, const int32_t* seqs, const int32_t* counts, void* stream);
@@ -116,10 +117,12 @@ int uft_copy(uft_cache* cache, int32_t n, const int32_t* src, const int32_t* dst
 int uft_keep(uft_cache* cache, int32_t n, const int32_t* seqs, const int32_t* starts, const int32_t* counts,
              const int32_t* d_index, void* stream);
 
-/* Give back the pages of sequences that no later query sees under this window
- * (>= 1) and these sinks: whole pages of positions j with sinks <= j <= length -
- * window.  Later queries, of a wider window too, see nothing there; positions do
- * not change.  Errors: UF_ERR_ARG, UF_ERR_HIP. */
+/* Give back the pages of sequences that no query of a later step sees under this
+ * window (>= 1) and these sinks: whole pages of positions j with sinks <= j <=
+ * length - window.  Queries attended after the call, of a wider window and of the
+ * present step too, see nothing there; positions do not change.  So it belongs
+ * behind a step's last layer; a step some of whose own tokens lie in those pages
+ * no longer holds.  Errors: UF_ERR_ARG, UF_ERR_HIP. */
 int uft_trim(uft_cache* cache, int32_t n, const int32_t* seqs, int32_t window, int32_t sinks, void* stream);
 
 /* Empty the sequences; pages that no other sequence shares become free (their

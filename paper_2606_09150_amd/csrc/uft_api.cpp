@@ -639,7 +639,15 @@ int uft_trim(uft_cache* c, int32_t n, const int32_t* seqs, int32_t window, int32
       holes.push_back(Hole{seqs[i], int32_t(from), int32_t(to)});
       poke.run(c->row_at(seqs[i]) + int32_t(from), none.data(), int32_t(to - from));
     }
+    // a step some of whose own tokens lose their place is over
+    bool ends = false;
+    if (!holes.empty()) {
+      std::vector<int64_t> gone(size_t(c->d.max_seqs), 0);   // tokens before the hole's end
+      for (const Hole& h : holes) gone[size_t(h.seq)] = h.to * T;
+      for (const Entry& e : c->step) ends = ends || (e.count > 0 && gone[size_t(e.seq)] > e.tokens - e.count);
+    }
     if (int s = poke.send(static_cast<hipStream_t>(stream))) return s;
+    if (ends) end_step(c);
     for (const Hole& h : holes) {
       Seq& q = c->seqs[size_t(h.seq)];
       for (int32_t p = h.from; p < h.to; ++p) {

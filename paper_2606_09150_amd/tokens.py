@@ -188,9 +188,12 @@ class TokenCache:
         self._step, self._need = None, {}
 
     def trim(self, seqs, window, sinks=0, stream=None):
-        """Give back the pages that no later query of this window and these sinks sees."""
+        """Give back the pages that no query of a later step sees under this window and these sinks.  Call it behind the last
+        layer of a step: queries of the step itself see nothing in those pages either, and where they hold tokens of the
+        step, it ends."""
         window, sinks = _int(window, "window"), _int(sinks, "sinks")
         self._run(stream, lambda s: T.uft_trim(self.handle, seqs, window, sinks, s))
+        self._step, self._need = None, {}
 
     def free(self, seqs):
         T.uft_free(self.handle, seqs)

@@ -53,3 +53,43 @@ def test_a_handle_that_goes_leaves_the_last_errors_text(P):
         assert "77" in text
         close()
         assert L.uf_last_error() == text
+
+
+def _empty(P, *calls):
+    for call in calls:
+        with pytest.raises(P.UfError) as e:
+            call()
+        assert e.value.status == P._lib.UF_ERR_EMPTY
+
+
+def test_a_trim_that_takes_pages_of_the_steps_tokens_ends_the_step(P):
+    """The pages go as the window says; what would write or attend tokens without a place is refused then."""
+    c = _dry(P, max_tokens=2000)
+    c.extend([0, 1], [800, 3])
+    c.trim([1], 1)
+    c.trim([0], 800)                                   # nothing to give back
+    c.write(1, None, None)
+    c.attention(1, 6)
+    c.trim([0], 737)                                   # page 0, tokens 0 .. 63: all new
+    assert c.pages(0) == [-1] + list(range(1, 13)) and c.info().step_seqs == 0 and c.step_tokens() == 0
+    _empty(P, lambda: c.write(1, None, None), lambda: c.attention(1, 6), lambda: c.work_bytes(6))
+    c.extend([0], [1])
+    c.trim([0], 100)                                   # pages of earlier tokens: the step's own are there
+    assert c.info().step_seqs == 1 and c.pages(0)[:10] == [-1] * 10 and c.pages(0)[10] >= 0
+    c.attention(0, 6)
+    # the last page trimmed holds an earlier token and new ones
+    c.extend([1], [61])
+    c.trim([1], 2)
+    assert c.info().step_seqs == 1                     # position 63 of 0 .. 63 is still seen
+    c.trim([1], 1)
+    assert c.pages(1) == [-1] and c.info().step_seqs == 0
+    # a step of sequences that do not grow, and one whose other sequence is trimmed
+    c.extend([0], [0])
+    c.trim([0], 1)
+    assert c.info().step_seqs == 1
+    c.extend([2, 3], [1, 200])
+    c.trim([2], 1)
+    assert c.info().step_seqs == 2
+    c.trim([2, 3], 1)
+    assert c.info().step_seqs == 0
+    assert c.pages(3) == [-1, -1, -1, c.pages(3)[3]] and c.pages(3)[3] >= 0
