@@ -800,11 +800,11 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
       }
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const float w = __shfl(f[i], (s0 + s * kGroups + grp) & (LANES - 1), LANES);   // 0 past the end
-        if (w > 0.f) {
-          x[0] += v[s][0].x * w, x[1] += v[s][0].y * w, x[2] += v[s][0].z * w, x[3] += v[s][0].w * w;
-          x[4] += v[s][1].x * w, x[5] += v[s][1].y * w, x[6] += v[s][1].z * w, x[7] += v[s][1].w * w;
-        }
+        // 0 past the end, and where a slice's weight underflows: what is not finite there stays so (a row's O is finite
+        // in slices that it does not see)
+        const float w = __shfl(f[i], (s0 + s * kGroups + grp) & (LANES - 1), LANES);
+        x[0] += v[s][0].x * w, x[1] += v[s][0].y * w, x[2] += v[s][0].z * w, x[3] += v[s][0].w * w;
+        x[4] += v[s][1].x * w, x[5] += v[s][1].y * w, x[6] += v[s][1].z * w, x[7] += v[s][1].w * w;
       }
     }
 #pragma unroll

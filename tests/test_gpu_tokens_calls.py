@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests.gpu_common import f64, require_gpu
-from tests.test_gpu_tokens import D, check_step, draw, poison, read
+from tests.test_gpu_tokens import D, check_step, draw, fill, poison, read
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,29 @@ def test_small_integer_counts_are_not_summed_in_their_own_type():
     got = read(cache, 0)[0]
     assert cache.tokens(0) == 200 and np.array_equal(got, f64(k)[[*range(99, -1, -1), *range(199, 99, -1)]])
     assert np.array_equal(read(cache, 1)[0], f64(k)[200:][::-1])
+
+
+@pytest.mark.parametrize("new,heads", [(1, 2), (40, 2)])
+@pytest.mark.parametrize("split", [False, True])
+def test_a_value_that_is_not_finite_reaches_its_rows_whatever_its_weight(new, heads, split):
+    """One key outweighs the others by over 150 bits, so that theirs underflow beside it, in its slice and in others."""
+    P = require_gpu()
+    cache = P.TokenCache(1, 1, 70, 1, 4200, 64)
+    poison(cache)
+    k, v, q = draw((4000 + new, 1, D), 1), draw((4000 + new, 1, D), 2), draw((new, heads, D), 3, 0.02)
+    q += draw((1, 1, D), 4)
+    k[3900] = 12 * draw((1, D), 4)                       # 12 |q|^2 / sqrt(128), over 100 = 104 / ln 2 bits
+    gain = (f64(q[:, :, :]) @ f64(k[3900, 0])).min() / D ** 0.5 - 20
+    assert gain > 105
+    for bad, kind in ((100, "nan"), (3899, "nan"), (100, "inf")):
+        v2 = v.clone()
+        v2[bad] = float(kind)
+        fill(cache, [0], [4000], 0, k[:4000], v2[:4000])
+        fill(cache, [0], [new], 0, k[4000:], v2[4000:])
+        cache.n_cu = 256 if split else 0
+        assert (cache.work_bytes(heads) > 0) == split
+        o, lse = cache.attention(0, q, lse=True)
+        torch.cuda.synchronize()
+        assert lse.isfinite().all()
+        assert not o.isfinite().any(), (bad, kind, int(o.isfinite().sum()))
+        cache.free([0])
