@@ -226,10 +226,10 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb) acc[mb] = f32x16{};
   const float c2 = a.scale_log2;
-  // P (at most 1) is formed 2^15 times too large, and dV and dK are scaled back at the end, so that it can be handed
-  // over in fp16: off by 2^-11 of itself, below weights of 2^-29 by 2^-40 at most, where bf16's 2^-8 put 20 % on dK's
-  // error
-  const float pad = key_ok ? 15.f : -INFINITY; // keys that are none weigh nothing
+  const float pad = key_ok ? 0.f : -INFINITY;  // keys that are none weigh nothing
+  // P (at most 1) is handed over in fp16, 2^15 times as large: off by 2^-11 of itself, below weights of 2^-29 by 2^-40 at
+  // most, where bf16's 2^-8 put 20 % on dK's error
+  constexpr float kHandUp = 0x1p15f, kHandDown = 0x1p-15f;
   uint4* const pslot = &sP[0][kw][0][lane];
   constexpr uint32_t kPStep = sizeof(sP[0]) / 16;
   // Operand addresses within the current ring slots, advanced once per phase: tr,
@@ -316,8 +316,8 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
       const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[qb][2 * e], c2, pad));
       const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[qb][2 * e + 1], c2, pad));
       put(op[qb], e, w0, w1);
-      hand[2 * (e & 3)] = (_Float16)w0;
-      hand[2 * (e & 3) + 1] = (_Float16)w1;
+      hand[2 * (e & 3)] = (_Float16)__builtin_fmaf(w0, kHandUp, 0.f);        // (one mixed-type instruction each)
+      hand[2 * (e & 3) + 1] = (_Float16)__builtin_fmaf(w1, kHandUp, 0.f);
       if ((e & 3) == 3) pslot[par * kPStep + (qb * 2 + (e >> 2)) * 64] = __builtin_bit_cast(uint4, hand);
     };
     fence();
@@ -352,8 +352,8 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
 #pragma unroll
     for (int i = i0; i < i0 + kAhead; ++i) x[i] = load(i);
     auto ds = [&](int qb, int e) {
-      put(op[qb], e, float(pk[qb][e >> 2][2 * (e & 3)]) * ov[qb][2 * e],
-          float(pk[qb][e >> 2][2 * (e & 3) + 1]) * ov[qb][2 * e + 1]);
+      put(op[qb], e, __builtin_fmaf(float(pk[qb][e >> 2][2 * (e & 3)]), kHandDown, 0.f) * ov[qb][2 * e],
+          __builtin_fmaf(float(pk[qb][e >> 2][2 * (e & 3) + 1]), kHandDown, 0.f) * ov[qb][2 * e + 1]);
     };
     fence();
     if (kDk && !kDp) {
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
   }
   if (key < a.tokens) {
     uint16_t* dst = (grp ? a.dk : a.dv) + ((size_t(b) * a.tokens + key) * H + h) * kD + 4 * hl;
-    const float f = grp ? a.scale * 0x1p-15f : 0x1p-15f;
+    const float f = grp ? a.scale : 1.f;
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(256) void sum_kernel(BwdArgs a, Cut cut, const floa
       s.w = __builtin_fmaf(v[i].w, on, s.w);
     }
   }
-  const float f = key < len ? (grp ? a.scale * 0x1p-15f : 0x1p-15f) : 0.f;
+  const float f = key < len ? (grp ? a.scale : 1.f) : 0.f;
   uint2 u;
   u.x = pack_bf16x2(s.x * f, s.y * f);
   u.y = pack_bf16x2(s.z * f, s.w * f);

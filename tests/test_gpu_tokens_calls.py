@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.gpu_common import f64, require_gpu
+from tests.gpu_common import f64, log, require_gpu
 from tests.test_gpu_tokens import D, check_step, draw, fill, poison, read
 
 pytestmark = pytest.mark.gpu
@@ -60,3 +60,21 @@ def test_a_value_that_is_not_finite_reaches_its_rows_whatever_its_weight(new, he
         assert lse.isfinite().all()
         assert not o.isfinite().any(), (bad, kind, int(o.isfinite().sum()))
         cache.free([0])
+
+
+@pytest.mark.parametrize("tokens,kv,group,window,sinks", [(300, 2, 3, 6, 2), (1500, 1, 2, 20, 3), (200, 1, 1, 0, 0)])
+def test_gradients_scale_with_do_over_the_range_of_bf16(tokens, kv, group, window, sinks):
+    """Gradients are linear in dO, and a power of two leaves every rounding as it is: the same bits, times that power, as
+    long as neither side leaves bf16's range (2^-126 to 2^128)."""
+    P = require_gpu()
+    q, do = draw((1, tokens, kv * group, D), 1), draw((1, tokens, kv * group, D), 2)
+    k, v = draw((1, tokens, kv, D), 3), draw((1, tokens, kv, D), 4)
+    o, lse = P.window_attention(q, k, v, window, sinks)
+    want = P.window_attention_bwd(q, k, v, o, lse, do, window, sinks)
+    torch.cuda.synchronize()
+    for power in (112, 40, -40):
+        got = P.window_attention_bwd(q, k, v, o, lse, (do.float() * 2.0 ** power).to(torch.bfloat16), window, sinks)
+        torch.cuda.synchronize()
+        for name, a, b in zip(("dq", "dk", "dv"), got, want):
+            log(f"  2^{power} {name}: largest {float(b.float().abs().max()):.3g}, finite {bool(a.isfinite().all())}")
+            assert torch.equal(a.float(), b.float() * 2.0 ** power), (power, name)
