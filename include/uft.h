@@ -18,9 +18,9 @@
  * a query that sees nothing gets O = 0 and LSE = -inf.  Query head n reads key
  * head n / (q_heads / kv_heads).  Scores, weights' sums and accumulators are fp32;
  * weights are rounded to bf16 for their product with V.  A key or value that is not
- * finite reaches the queries that see it and no others (where there is one, the rows
- * beside it are formed key by key, which is slow).  The gradients' products run over
- * whole tiles: there such a token can make NaN of its neighbours' gradients.  Memory
+ * finite reaches the queries that see it and no others, and in the gradients the rows
+ * that they take part in and no others, Q and dO alike (where there is one, the rows
+ * beside it are formed key by key, which is slow: a backward of 2 ms takes 40).  Memory
  * past a sequence's end, padding and pages of others are never read.
  */
 #ifndef UFT_H

@@ -410,6 +410,44 @@ __global__ __launch_bounds__(512, 2) void dkdv_kernel(BwdArgs a, Cut cut, float*
     issue_all(source(1, 1, 1));
     if (grp == 0) run(std::integral_constant<int, 0>{});
     else run(std::integral_constant<int, 1>{});
+    // A row that does not see a key has a weight of zero there, and zero times what is not finite in the row is not zero:
+    // where any of the wave's results is not finite they are formed again row by row, each from the rows that see its key
+    // (4 us a row; a few are enough to make the launch 20 times as long).
+    float probe = 0.f;
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) probe += acc[mb][r];
+    if (__ballot(not_finite(probe)) != 0) {
+      bf16x8 kf[8], vf[8];
+      const int64_t at = key_ok ? key : 0;
+      const uint16_t* kp = a.k + int64_t(b) * a.k_batch + int64_t(h) * a.k_head + at * a.k_token + 8 * hl;
+      const uint16_t* vp = a.v + int64_t(b) * a.v_batch + int64_t(h) * a.v_head + at * a.v_token + 8 * hl;
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        kf[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(kp + 16 * ks));
+        vf[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(vp + 16 * ks));
+      }
+      float out[64];
+#pragma unroll
+      for (int i = 0; i < 64; ++i) out[i] = 0.f;
+      const int rows_end = min(end * UQ, len * G);
+      for (int row = first * UQ; row < rows_end; ++row) {
+        const bool on = key_ok && row >= row_lo && row < row_hi;
+        if (__ballot(on) == 0) continue;
+        const int tok = div_nt(uint32_t(row), a.group_div), g = row - tok * G;
+        const uint8_t* qr = qb + int64_t(tok) * a.q_token * 2 + size_t(g) * qh2;
+        const uint8_t* orow = ob + int64_t(tok) * ot2 + size_t(g) * (kD * 2);
+        const float* seed = reinterpret_cast<const float*>(seeds + size_t(row / kT) * kSeeds) + row % kT;
+        const float w = __builtin_amdgcn_exp2f((dot_row(kf, qr, hl) + seed[0]) * c2);
+        if (grp == 0) add_row<16>(w, orow, on, 4 * hl, out);
+        else add_row<16>(w * (dot_row(vf, orow, hl) + seed[kT]), qr, on, 4 * hl, out);
+      }
+#pragma unroll
+      for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[mb][r] = out[16 * mb + r];
+    }
   }
 
   // lane holds key `key`, dims mb*32 + 8*(r/4) + 4*hl + r%4
@@ -700,6 +738,32 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
     next = unit_of(min(u + 2, U - 1));
   } while (++u < U);
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));           // no copy outlives the workgroup
+  // What is not finite in a key that a row does not see: as in the forward and in dkdv, key by key.
+  float probe = 0.f;
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) probe += dqt[mb][r];
+  if (__ballot(not_finite(probe)) != 0) {
+    float out[64];
+#pragma unroll
+    for (int i = 0; i < 64; ++i) out[i] = 0.f;
+    for (int i = 0; i < U; ++i) {
+      const Unit c = unit_of(i);
+      const uint64_t see = seen_bits(pos, c.key0, a.window, a.sinks);
+      for (int k = 0; k < kKeyUnit; ++k) {
+        const bool on = row < rows && ((see >> k) & 1u);
+        if (__ballot(on) == 0) continue;
+        const uint8_t* kr1 = c.k + uint32_t(k) * kstep;
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot_row(qf, kr1, hl), c2, nl));
+        add_row<16>(w * (dot_row(of, c.v + uint32_t(k) * vstep, hl) + nd), kr1, on, 4 * hl, out);
+      }
+    }
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dqt[mb][r] = out[16 * mb + r];
+  }
   int r_out = row;                                     // (its address is formed here, not held across the walk)
   asm volatile("" : "+v"(r_out));
   if (r_out >= a.tokens * G) return;

@@ -50,30 +50,37 @@ __device__ inline uint64_t seen_bits_tree(int pos, int key0, int window, int sin
   return see | (d > -64 ? node >> -d : 0);
 }
 
-// One key's term of a lane's row by itself, where the tiles' products cannot be used: the
-// score from the row's Q operand (dims 16 ks + 8 hl .. in registers, the other half in
-// lane l ^ 32), then V's dims d0 + 8 i .. + 3 (i < N) into out.
-template <int N>
-__device__ inline void add_key(const bf16x8 (&q)[8], const uint8_t* k, const uint8_t* v, int hl, bool on, float c2, float m,
-                               int d0, float* out) {
+// Rows one by one, where the tiles' products cannot be used.  dot_row: of 128 dimensions, 16 ks + 8 hl .. in registers, the
+// other half in lane l ^ 32, with a row in memory.  add_row: dims d0 + 8 i .. + 3 (i < N) of w times such a row to out.
+__device__ inline float dot_row(const bf16x8 (&q)[8], const uint8_t* row, int hl) {
   float s = 0.f;
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) {
-    const bf16x8 x = attn::as_bf16x8(*reinterpret_cast<const uint4*>(k + (16 * ks + 8 * hl) * 2));
+    const bf16x8 x = attn::as_bf16x8(*reinterpret_cast<const uint4*>(row + (16 * ks + 8 * hl) * 2));
+    bf16x8 y = q[ks];
+    asm volatile("" : "+v"(y));   // (its fp32 form is made here, not held in 64 registers across the kernel)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s += float(q[ks][e]) * float(x[e]);
+    for (int e = 0; e < 8; ++e) s += float(y[e]) * float(x[e]);
   }
-  s = attn::pair_sum(s);
-  const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, c2, -m));
+  return attn::pair_sum(s);
+}
+template <int N>
+__device__ inline void add_row(float w, const uint8_t* row, bool on, int d0, float* out) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const uint2 x = *reinterpret_cast<const uint2*>(v + (d0 + 8 * i) * 2);
+    const uint2 x = *reinterpret_cast<const uint2*>(row + (d0 + 8 * i) * 2);
     const float y[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
                         __uint_as_float(x.y & 0xffff0000u)};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (on) out[4 * i + e] += w * y[e];
   }
+}
+// One key's term of a lane's row of O.
+template <int N>
+__device__ inline void add_key(const bf16x8 (&q)[8], const uint8_t* k, const uint8_t* v, int hl, bool on, float c2, float m,
+                               int d0, float* out) {
+  add_row<N>(__builtin_amdgcn_exp2f(__builtin_fmaf(dot_row(q, k, hl), c2, -m)), v, on, d0, out);
 }
 __device__ inline bool not_finite(float x) { return !(fabsf(x) < INFINITY); }
 

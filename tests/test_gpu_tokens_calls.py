@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import tokens as O
 from tests.gpu_common import f64, log, require_gpu
 from tests.test_gpu_tokens import D, check_step, draw, fill, poison, read
 
@@ -78,3 +79,86 @@ def test_gradients_scale_with_do_over_the_range_of_bf16(tokens, kv, group, windo
         for name, a, b in zip(("dq", "dk", "dv"), got, want):
             log(f"  2^{power} {name}: largest {float(b.float().abs().max()):.3g}, finite {bool(a.isfinite().all())}")
             assert torch.equal(a.float(), b.float() * 2.0 ** power), (power, name)
+
+
+def _bad_rows(x, n):
+    return ~np.isfinite(x).all(-1)[:n]
+
+
+def check_gradients_beside(q, k, v, do, grads, window, sinks, n, scale=D ** -0.5):
+    """One sequence of n tokens, some of whose rows hold values that are not finite: a gradient is finite, and within the
+    bounds, exactly where no such row takes part in it."""
+    G = q.shape[1] // k.shape[1]
+    see = O.sees(np.arange(n), np.arange(n), window, sinks)
+    seen = {"dq": 0, "dk": 0, "dv": 0}
+    for hk in range(k.shape[1]):
+        sums = {"dk": [0.0, 0.0, np.zeros(n, bool)], "dv": [0.0, 0.0, np.zeros(n, bool)]}
+        bk, bv = _bad_rows(k[:, hk], n), _bad_rows(v[:, hk], n)
+        kk, vv = np.where(bk[:, None], 0, k[:n, hk]), np.where(bv[:, None], 0, v[:n, hk])
+        for h in range(hk * G, (hk + 1) * G):
+            bq, bd = _bad_rows(q[:, h], n), _bad_rows(do[:, h], n)
+            bad_p = bq | (see & bk).any(1)               # rows whose weights are not finite
+            bad_ds = bad_p | bd | (see & bv).any(1)
+            args = np.where(bq[:, None], 0, q[:n, h]), kk, vv, np.where(bd[:, None], 0, do[:n, h])
+            for name, bad, i in (("dq", bad_ds, 0), ("dk", bad_ds, 1), ("dv", bad_p | bd, 2)):
+                want, bound = O.grads(*args, see & ~bad[:, None], scale)[i]
+                if name == "dq":
+                    got = grads[0][:n, h]
+                    assert not np.isfinite(got[bad]).any() and np.isfinite(got[~bad]).all(), (name, h)
+                    assert (np.abs(got - want) <= bound)[~bad].all(), (name, h)
+                    seen["dq"] += bad.sum()
+                else:
+                    s = sums[name]
+                    s[0], s[1], s[2] = s[0] + want, s[1] + bound, s[2] | (see & bad[:, None]).any(0)
+        for name, got in (("dk", grads[1][:n, hk]), ("dv", grads[2][:n, hk])):
+            want, bound, bad = sums[name]
+            assert not np.isfinite(got[bad]).any() and np.isfinite(got[~bad]).all(), (name, hk)
+            assert (np.abs(got - want) <= bound)[~bad].all(), (name, hk)
+            seen[name] += bad.sum()
+    log(f"  not finite: {seen}")
+    return seen
+
+
+@pytest.mark.parametrize("kind", ["k nan", "v nan", "v inf", "q nan", "do nan", "do inf"])
+@pytest.mark.parametrize("tokens,kv,group,window,sinks,length,bad", [
+    (400, 2, 3, 40, 5, 400, [130, 131, 300]),
+    (333, 1, 5, 0, 0, 300, [250]),                       # no window, padding
+    (1500, 1, 2, 20, 3, 1500, [700, 1499]),              # the sinks' rows are cut into parts
+    (200, 1, 70, 9, 0, 200, [64, 65]),                   # a group larger than a unit
+    (130, 1, 1, 1, 0, 130, [0, 129])])                   # a window of one token
+def test_gradients_beside_values_that_are_not_finite(kind, tokens, kv, group, window, sinks, length, bad):
+    P = require_gpu()
+    x = {"q": draw((2, tokens, kv * group, D), 1), "k": draw((2, tokens, kv, D), 2), "v": draw((2, tokens, kv, D), 3),
+         "do": draw((2, tokens, kv * group, D), 4)}
+    what, value = kind.split()
+    x[what][1, bad, -1] = float(value)                   # of the second sequence's last head
+    for t in x.values():
+        t[:, length:] = float("nan")
+    lengths = torch.full((2,), length, dtype=torch.int32, device="cuda")
+    log(f"{kind} tokens={tokens} kv={kv} group={group} window={window} sinks={sinks}")
+    o, lse = P.window_attention(x["q"], x["k"], x["v"], window, sinks, lengths=lengths)
+    grads = P.window_attention_bwd(x["q"], x["k"], x["v"], o, lse, x["do"], window, sinks, lengths=lengths)
+    torch.cuda.synchronize()
+    for b in range(2):
+        own = [f64(t)[b] for t in (x["q"], x["k"], x["v"], x["do"])]
+        seen = check_gradients_beside(*own, [f64(g)[b] for g in grads], window, sinks, length)
+        assert (max(seen.values()) > 0) == (b == 1)
+        for g in grads:
+            assert not g[b, length:].any()
+
+
+def test_one_element_of_do_that_is_not_finite_stays_in_its_dimension_of_dv():
+    P = require_gpu()
+    q, do, k, v = (draw((1, 300, 2, D), i) for i in range(4))
+    want = P.window_attention_bwd(q, k, v, *P.window_attention(q, k, v, 30), do, 30)[2]
+    do[0, 100, 1, 77] = float("nan")
+    dv = P.window_attention_bwd(q, k, v, *P.window_attention(q, k, v, 30), do, 30)[2]
+    torch.cuda.synchronize()
+    hit = torch.zeros_like(dv, dtype=torch.bool)
+    hit[0, 71:101, 1, 77] = True
+    assert dv[hit].isnan().all() and dv[~hit].isfinite().all()
+    near = torch.zeros_like(hit)
+    near[0, :, 1] = True                                 # formed again key by key: another order of the sums
+    assert torch.equal(dv[~near], want[~near])
+    a, b = dv[near & ~hit].float(), want[near & ~hit].float()
+    assert (a - b).norm() < 2 ** -7 * b.norm()
