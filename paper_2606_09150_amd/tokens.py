@@ -16,11 +16,13 @@ from . import _tokens as T
 D = 128
 SCALE = 1.0 / math.sqrt(D)
 _NO_STRIDE = T.uft_stride(0, 0, 0)
+_forward_ad = torch.autograd.forward_ad                    # (its level is -1 where no tangents are held)
 
 
 def _check(t, name, shape, dtype=torch.bfloat16, device=None):
-    """A device tensor of this type, shape and device."""
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.shape == shape and not t.requires_grad:
+    """A device tensor of this type, shape and device, of which no derivative is recorded."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.shape == shape and not t.requires_grad
+            and _forward_ad._current_level < 0):
         return                                           # (device: a GPU's)
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a tensor (got {type(t).__name__})")
@@ -34,6 +36,8 @@ def _check(t, name, shape, dtype=torch.bfloat16, device=None):
         raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, which this call does not record: detach it, or call under no_grad")
+    if _forward_ad._current_level >= 0 and _forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name} has a tangent, which this call does not carry on: hand over its primal")
 
 
 def _dense(t, name, shape, dtype=torch.bfloat16, device=None):

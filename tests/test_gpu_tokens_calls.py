@@ -162,3 +162,28 @@ def test_one_element_of_do_that_is_not_finite_stays_in_its_dimension_of_dv():
     assert torch.equal(dv[~near], want[~near])
     a, b = dv[near & ~hit].float(), want[near & ~hit].float()
     assert (a - b).norm() < 2 ** -7 * b.norm()
+
+
+def test_tangents_are_refused():
+    """Forward-mode derivatives are no more recorded than gradients are."""
+    P = require_gpu()
+    fwd = torch.autograd.forward_ad
+    q, k, v = draw((1, 9, 4, D), 1), draw((1, 9, 2, D), 2), draw((1, 9, 2, D), 3)
+    cache = P.TokenCache(1, 2, 8, 1, 100, 64)
+    cache.extend([0], [9])
+    cache.write(0, k[0], v[0])
+    o, lse = P.window_attention(q, k, v)
+    with fwd.dual_level():
+        dual = [fwd.make_dual(t, torch.ones_like(t)) for t in (q, k, v, o, lse)]
+        dq, dk, dv, do, dl = dual
+        for call in (lambda: P.window_attention(dq, k, v), lambda: P.window_attention(q, dk, v), lambda: P.window_attention(q, k, dv),
+                     lambda: P.window_attention_bwd(q, k, v, do, lse, q), lambda: P.window_attention_bwd(q, k, v, o, dl, q),
+                     lambda: P.window_attention_bwd(q, k, v, o, lse, dq), lambda: cache.write(0, dk[0], v[0]),
+                     lambda: cache.write(0, k[0], dv[0]), lambda: cache.attention(0, dq[0])):
+            with pytest.raises(ValueError):
+                call()
+        # no tangent, or one that was taken off
+        again = P.window_attention(fwd.unpack_dual(dq).primal, k, v)
+        assert torch.equal(again[0], o) and torch.equal(cache.attention(0, q[0]), cache.attention(0, fwd.unpack_dual(dq).primal[0]))
+    with pytest.raises(Exception):
+        torch.func.jvp(lambda x: P.window_attention(x, k, v)[0], (q,), (q,))
