@@ -4,6 +4,7 @@ its gradients with bounds on what rounding may change, and the token cache's pag
 import numpy as np
 
 BF16 = 2.0 ** -8      # relative half step
+FP16 = 2.0 ** -11
 FP32 = 2.0 ** -24
 
 
@@ -59,21 +60,65 @@ def grads(q, k, v, do, see, scale):
     dp = do @ v.T
     ds = p * (dp - delta)
     dq, dk, dv = scale * ds @ k, scale * ds.T @ q, p.T @ do
-    # P is rounded to bf16 (and off as its score is), dS formed from it and rounded again; delta comes from O rounded to
-    # bf16, whose own error is attend_bound's; sums in fp32; one rounding of the result to bf16
+    # P is off as its score is.  For dV it is rounded to bf16; for dQ it stays fp32, and dS formed from it is rounded to two
+    # bf16 parts (the second a half step off the remainder, which is a half step of dS); for dK it passes through fp16,
+    # 2^15 times as large: off by 2^-11, or where that is subnormal (spacing 2^-24, weights below 2^-14 / 2^15) by half a
+    # spacing, 2^-25 / 2^15, whatever its own size; and dS is rounded once.  delta comes from O rounded to bf16, whose own
+    # error is attend_bound's; sums in fp32; one rounding of each result to bf16
     off = 2 * score_error(q, k, scale) + (2 * max(k.shape[0], q.shape[0]) + 64) * FP32
     d_delta = (np.abs(do) * attend_bound(q, k, v, p, o, scale)).sum(1, keepdims=True)
     d_dp = (np.abs(do) @ np.abs(v).T + np.abs(delta)) * (do.shape[1] + 8) * FP32
-    e_ds = np.abs(ds) * (2 * BF16 + BF16 ** 2 + off) + p * (d_delta + d_dp) * (1 + 2 * BF16)
-    e_p = p * (BF16 + off)
-    # for dK the weights pass through fp16, 2^15 times as large: where that is subnormal (spacing 2^-24, weights below
-    # 2^-14 / 2^15) they are off by half a spacing, 2^-25 / 2^15, whatever their own size
-    e_dsk = e_ds + 2.0 ** -40 * np.abs(dp - delta) * see * (1 + BF16)
-    b_dq, b_dk, b_dv = scale * e_ds @ np.abs(k), scale * e_dsk.T @ np.abs(q), e_p.T @ np.abs(do)
+    inner = p * (d_delta + d_dp) * (1 + off)             # what dP - delta is off by, weighed
+    e_q = np.abs(ds) * off + inner
+    e_q += (np.abs(ds) + e_q) * BF16 ** 2
+    e_k = np.abs(ds) * (off + FP16) + inner * (1 + FP16) + 2.0 ** -40 * (np.abs(dp - delta) + d_delta + d_dp) * see
+    e_k += (np.abs(ds) + e_k) * BF16
+    e_p = p * (off + BF16 * (1 + off))
+    b_dq, b_dk, b_dv = scale * e_q @ np.abs(k), scale * e_k.T @ np.abs(q), e_p.T @ np.abs(do)
     sums = (2 * max(k.shape[0], q.shape[0]) + 64) * FP32
     return [(g, b + s * sums + (np.abs(g) + b) * BF16 + 1e-30)
             for g, b, s in ((dq, b_dq, scale * np.abs(ds) @ np.abs(k)), (dk, b_dk, scale * np.abs(ds).T @ np.abs(q)),
                             (dv, b_dv, p.T @ np.abs(do)))]
+
+
+# ---- what the stated roundings alone do, as norms ---------------------------------
+#
+# The bounds above add absolute values: they hold for every element, and leave room for a rounding too many.  Norms over a
+# tensor leave none: the same operations with exactly the stated roundings, everything else in float64.
+
+def keep_bits(x, bits):
+    """x to so many significant bits, ties to even (bf16: 8)."""
+    m, e = np.frexp(x)
+    return np.ldexp(np.rint(np.ldexp(m, bits)), e - bits)
+
+
+def rounded_attend(q, k, v, see, scale, p_bits=8):
+    """(O before its own rounding, O exactly): weights rounded for their product with V.  They are formed relative to an
+    offset that need not be the row's largest score (it is raised on a row's first units only, and by far larger scores
+    later), so the largest is off as the others are: here relative to the sum, where none is a power of two by design."""
+    o, _, p = attend(q, k, v, see, scale)
+    return keep_bits(p, p_bits) @ v, o
+
+
+def rounded_grads(q, k, v, do, o, lse, see, scale, p_bits=8, ds_bits=(16, 8), delta_off=0.0, ds_off=0.0):
+    """dq, dk, dv of one head before their own rounding, from O and LSE as the forward left them.  ds_bits: of dS for dQ
+    (two parts of 8) and for dK."""
+    s = np.where(see, q @ k.T * scale, -np.inf)
+    with np.errstate(invalid="ignore"):
+        p = np.where(see, np.exp(s - np.where(np.isfinite(lse), lse, 0.0)[:, None]), 0.0)
+    inner = do @ v.T - (do * o).sum(1, keepdims=True) * (1 + delta_off)
+    hand = (p * 2.0 ** 15).astype(np.float16).astype(np.float64) * 2.0 ** -15
+    dsq, dsk = (keep_bits(x * inner * (1 + ds_off), b) for x, b in zip((p, hand), ds_bits))
+    return scale * dsq @ k, scale * dsk.T @ q, keep_bits(p, p_bits).T @ do
+
+
+def norm_limit(before, *parts):
+    """The most that a result may be off, as a norm: its own rounding to bf16, ``parts`` and 2^-11 of the result for fp32, all
+    independent of each other, and a tenth more of their squares for chance.  Where fp32 (scores and LSE off by e, 1e-6 at
+    scores of 10) carries a value over a rounding's border it changes by a step u, with chance e / u: sqrt(e u) of a weight,
+    7e-5 at u = 2^-8, and sums in fp32 are off by less."""
+    own = [keep_bits(before, 8) - before, 2.0 ** -11 * before, *parts]
+    return np.sqrt(1.1 * sum(float((x * x).sum()) for x in own))
 
 
 class PageModel:
