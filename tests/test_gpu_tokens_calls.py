@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from oracle import tokens as O
+from tests import test_oracle_token_units as units
 from tests.gpu_common import f64, log, require_gpu
 from tests.test_gpu_tokens import D, check_step, draw, fill, poison, read
 
@@ -187,3 +188,59 @@ def test_tangents_are_refused():
         assert torch.equal(again[0], o) and torch.equal(cache.attention(0, q[0]), cache.attention(0, fwd.unpack_dual(dq).primal[0]))
     with pytest.raises(Exception):
         torch.func.jvp(lambda x: P.window_attention(x, k, v)[0], (q,), (q,))
+
+
+@pytest.mark.parametrize("new,heads", [(1, 2), (4, 8), (40, 1), (33, 2)])
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("held,hole,page,window,sinks", [
+    (70000, (20032, 39936), 64, 0, 0),                   # past a table of 1,024 units and a wave's 64 pages, and a hole
+    (66000, None, 128, 0, 0), (70000, None, 64, 20000, 300), (4200, None, 64, 0, 0), (2300, None, 128, 1000, 70)])
+def test_every_unit_of_a_long_walk_counts_once(new, heads, split, held, hole, page, window, sinks):
+    P = require_gpu()
+    n = held + new
+    cache = P.TokenCache(1, 1, -(-n // page) + 2, 1, n, page)
+    poison(cache)
+    k, v = units.marked(n)
+    k, v = (torch.from_numpy(x).to(torch.bfloat16)[:, None].cuda() for x in (k, v))
+    fill(cache, [0], [held], 0, k[:held], v[:held])
+    if hole:
+        cache.trim([0], held - hole[1], hole[0])
+        assert [p for p, x in enumerate(cache.pages(0)) if x < 0] == list(range(hole[0] // page, hole[1] // page))
+    fill(cache, [0], [new], 0, k[held:], v[held:])
+    q = units.queries(new, heads, new)
+    cache.n_cu = cache.n_cu if split else 0
+    for tree in (False, True):
+        bits = None
+        if tree:                                         # a chain: each new token sees those before it
+            bits = torch.tensor([(1 << (t + 1)) - 1 for t in range(new)], dtype=torch.int64, device="cuda")
+        log(f"units: {held}+{new} heads={heads} split={split} page={page} window={window} sinks={sinks} tree={tree}")
+        assert (cache.work_bytes(heads, window, sinks) > 0) == split
+        o, lse = cache.attention(0, torch.from_numpy(q).to(torch.bfloat16).cuda(), window, sinks, tree=bits, lse=True)
+        torch.cuda.synchronize()
+        see = O.sees(np.arange(held, n), np.arange(n), window, sinks)
+        if hole:
+            see[:, hole[0]:hole[1]] = False
+        for h in range(heads):
+            want, wl = units.expected(q[:, h], f64(k)[:, 0], f64(v)[:, 0], see)
+            assert units.accepted(f64(o)[:, h], f64(lse)[:, h], want, wl), h
+
+
+@pytest.mark.parametrize("tokens,kv,group,window,sinks", [(4500, 1, 1, 0, 0), (3000, 2, 3, 700, 130)])
+def test_every_unit_of_a_prompt_counts_once(tokens, kv, group, window, sinks):
+    """At once through the cache, and as a whole sequence."""
+    P = require_gpu()
+    k, v = units.marked(tokens)
+    q = units.queries(tokens, kv * group)
+    kt, vt = (torch.from_numpy(x).to(torch.bfloat16)[:, None].expand(-1, kv, -1).contiguous().cuda() for x in (k, v))
+    qt = torch.from_numpy(q).to(torch.bfloat16).cuda()
+    cache = P.TokenCache(1, kv, tokens // 64 + 2, 1, tokens, 64)
+    poison(cache)
+    fill(cache, [0], [tokens], 0, kt, vt)
+    out = cache.attention(0, qt, window, sinks, lse=True)
+    whole = P.window_attention(qt[None], kt[None], vt[None], window, sinks)
+    torch.cuda.synchronize()
+    see = O.sees(np.arange(tokens), np.arange(tokens), window, sinks)
+    for h in range(kv * group):
+        want, lse = units.expected(q[:, h], k, v, see)
+        assert units.accepted(f64(out[0])[:, h], f64(out[1])[:, h], want, lse), h
+        assert units.accepted(f64(whole[0])[0, :, h], f64(whole[1])[0, h], want, lse), h
