@@ -57,7 +57,7 @@ struct KeepHead {
   Pool pool;
   const int32_t* table;     // page table of all sequences
   const int32_t* index;
-  int32_t n, n_pages, row;
+  int32_t n, n_pages;
 };
 template <class Head, int N>
 struct Worded : Head {

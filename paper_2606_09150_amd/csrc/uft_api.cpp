@@ -561,7 +561,6 @@ int uft_keep(uft_cache* c, int32_t n, const int32_t* seqs, const int32_t* starts
       a.pool = c->pool_of(0);
       a.table = c->table + c->rows_at();
       a.index = d_index;
-      a.row = c->row;
       auto words = [&](int32_t i) {
         const Move& m = moves[size_t(i)];
         int32_t* w = a.words + tok::kKeepWords * a.n++;
