@@ -179,7 +179,8 @@ int uft_attn(const uft_cache* cache, int32_t layer, const uft_attn_desc* desc, c
  * O = 0, LSE = -inf and zero gradients.  q.head times the query heads of a key head
  * is at most 2^30; scale as for uft_attn, and at least 2^-100.  Errors: UF_ERR_ARG, UF_ERR_HIP.
  *
- * Backward: d_o and d_lse as the forward left them, d_do [batch, tokens, q_heads,
+ * Backward: d_o and d_lse as the forward of the same call left them (a row's weights,
+ * exp(scale q.k - LSE), are taken to sum to 1), d_do [batch, tokens, q_heads,
  * head_dim] bf16 contiguous; outputs d_dq (as q) and d_dk, d_dv (as k) bf16,
  * contiguous, fully overwritten; gradients of a key head add over its query heads
  * in fp32.  d_work (16-byte aligned, >= uft_window_bwd_work_bytes) is scratch.  No

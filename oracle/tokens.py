@@ -63,15 +63,16 @@ def grads(q, k, v, do, see, scale):
     # P is off as its score is.  For dV it is rounded to bf16; for dQ it stays fp32, and dS formed from it is rounded to two
     # bf16 parts (the second a half step off the remainder, which is a half step of dS); for dK it passes through fp16,
     # 2^15 times as large: off by 2^-11, or where that is subnormal (spacing 2^-24, weights below 2^-14 / 2^15) by half a
-    # spacing, 2^-25 / 2^15, whatever its own size; and dS is rounded once.  delta comes from O rounded to bf16, whose own
-    # error is attend_bound's; sums in fp32; one rounding of each result to bf16
+    # spacing, 2^-25 / 2^15, whatever its own size; and dS is rounded once.  For dQ delta comes from O rounded to bf16, whose
+    # own error is attend_bound's (where rows see few keys it is corrected as for dK: the bound is wide there); for dK
+    # it is the sum of P dP over the row's keys.  Sums in fp32; one rounding of each result to bf16
     off = 2 * score_error(q, k, scale) + (2 * max(k.shape[0], q.shape[0]) + 64) * FP32
     d_delta = (np.abs(do) * attend_bound(q, k, v, p, o, scale)).sum(1, keepdims=True)
     d_dp = (np.abs(do) @ np.abs(v).T + np.abs(delta)) * (do.shape[1] + 8) * FP32
-    inner = p * (d_delta + d_dp) * (1 + off)             # what dP - delta is off by, weighed
-    e_q = np.abs(ds) * off + inner
+    e_q = np.abs(ds) * off + p * (d_delta + d_dp) * (1 + off)     # what P and dP - delta are off by
     e_q += (np.abs(ds) + e_q) * BF16 ** 2
-    e_k = np.abs(ds) * (off + FP16) + inner * (1 + FP16) + 2.0 ** -40 * (np.abs(dp - delta) + d_delta + d_dp) * see
+    d_sum = (p * (np.abs(dp) * off + d_dp)).sum(1, keepdims=True) + np.abs(delta) * off
+    e_k = np.abs(ds) * (off + FP16) + (p * (1 + off + FP16) + 2.0 ** -40 * see) * (d_sum + d_dp) + 2.0 ** -40 * np.abs(dp - delta) * see
     e_k += (np.abs(ds) + e_k) * BF16
     e_p = p * (off + BF16 * (1 + off))
     b_dq, b_dk, b_dv = scale * e_q @ np.abs(k), scale * e_k.T @ np.abs(q), e_p.T @ np.abs(do)
@@ -100,15 +101,24 @@ def rounded_attend(q, k, v, see, scale, p_bits=8):
     return keep_bits(p, p_bits) @ v, o
 
 
-def rounded_grads(q, k, v, do, o, lse, see, scale, p_bits=8, ds_bits=(16, 8), delta_off=0.0, ds_off=0.0):
+def few_keys(n, window=0, sinks=0, group=1, g=0):
+    """bool [n]: the tokens whose rows, of head g of a group, lie in tiles of 128 rows that see 128 keys at most."""
+    row = np.arange(n) * group + g
+    last = (np.minimum(row // 128 * 128 + 128, n * group) - 1) // group
+    return np.minimum(last + 1, window + sinks if window else n) <= 128
+
+
+def rounded_grads(q, k, v, do, o, lse, see, scale, few, p_bits=8, ds_bits=(16, 8), delta_off=0.0, ds_off=0.0):
     """dq, dk, dv of one head before their own rounding, from O and LSE as the forward left them.  ds_bits: of dS for dQ
-    (two parts of 8) and for dK."""
+    (two parts of 8) and for dK.  delta: the sum of P dP for dK and for dQ's rows of ``few`` keys, for its others from O."""
     s = np.where(see, q @ k.T * scale, -np.inf)
     with np.errstate(invalid="ignore"):
         p = np.where(see, np.exp(s - np.where(np.isfinite(lse), lse, 0.0)[:, None]), 0.0)
-    inner = do @ v.T - (do * o).sum(1, keepdims=True) * (1 + delta_off)
+    dp = do @ v.T
+    exact = (p * dp).sum(1, keepdims=True)
+    delta = np.where(few[:, None], exact, (do * o).sum(1, keepdims=True))
     hand = (p * 2.0 ** 15).astype(np.float16).astype(np.float64) * 2.0 ** -15
-    dsq, dsk = (keep_bits(x * inner * (1 + ds_off), b) for x, b in zip((p, hand), ds_bits))
+    dsq, dsk = (keep_bits(x * (dp - d * (1 + delta_off)) * (1 + ds_off), b) for x, d, b in zip((p, hand), (delta, exact), ds_bits))
     return scale * dsq @ k, scale * dsk.T @ q, keep_bits(p, p_bits).T @ do
 
 

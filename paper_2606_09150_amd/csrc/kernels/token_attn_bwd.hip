@@ -12,7 +12,8 @@
 //  * dq: one workgroup of four waves per 128 rows, two per CU: delta from the rows' dO and
 //    O, then per 32 keys S^T = K Q^T, dP^T = V dO^T, dS^T and dQ^T += K^T dS^T (dS in two
 //    parts).  It leaves -LSE/scale (-inf where there is no row, so that its weights vanish)
-//    and -delta in the workspace, the seeds of dkdv's S and dP accumulators;
+//    and -delta, corrected (see there), in the workspace, the seeds of dkdv's S and dP
+//    accumulators;
 //  * dkdv: one workgroup of eight waves per 128 keys of a head.  Waves w and w + 4
 //    share 32 keys: wave w computes S = Q K^T and P, hands P to wave w + 4 through LDS
 //    and accumulates dV^T += dO^T P, while wave w + 4 computes dP = dO V^T and, one unit
@@ -21,6 +22,11 @@
 //    sees), the parts' dK and dV in fp32, added in order.
 // (A pass that copied Q and dO into records of 128 rows and formed delta took 123 us of
 // 2,660 at 16,384 tokens, 32 heads, window 2,048, and 66 KB of workspace a record.)
+// Rounding: scores, P, dP, dS and all sums are fp32.  What a product takes is bf16, the
+// matrix cores' type for its other operand: P for dV, dS for dK, once each; dS for dQ in two
+// parts.  Each such rounding is about as large as the result's own (1.7e-3 of its norm), so
+// that dV and dK are 2.3e-3 to 2.4e-3 off and dQ 1.7e-3 to 2.1e-3.  A second part for dV or
+// dK would be a quarter more products in a kernel that they bound.
 // The transposed operands come from row-major LDS tiles through transposing reads.
 // Every output row is owned by one workgroup and sums have one order: no atomics.
 #include <type_traits>
@@ -519,10 +525,19 @@ __global__ __launch_bounds__(256) void sum_kernel(BwdArgs a, Cut cut, const floa
 // GHz: 1,135 TFLOP/s at 16,384 tokens, 32 heads over 8, window 2,048 (908 us).  Two
 // operands are read ahead: three to six, which the registers hold too, changed nothing.
 // dS goes to its product in two bf16 parts, its rounding and the remainder: rounded once it
-// is the largest part of dQ's error (2.8e-3 of dQ, now 2.1e-3, of which 1.7e-3 are dQ's own
-// rounding and the rest delta from the rounded O).  The remainder's product costs 200 us of
-// a backward of 1,950 at that size, in whichever order the two are issued.
+// puts 1.6e-3 on dQ.  The remainder's product costs 200 us of a backward of 1,950 at that
+// size, in whichever order the two are issued.
+//
+// delta from the rounded O is off by 2e-3 of |dO| |O|, which is large where a row sees few
+// keys (3.1e-3 of dQ and dK at a window of 6, 2.6e-3 at 16).  But P sums to 1, so that the sum
+// of a row's dS, which the walk forms beside dS (up to 2 % of the backward), is what delta
+// was off by: dkdv gets delta with that.  dQ has been formed with the other by then, and
+// what it is off by is small where rows see many keys; tiles that see kFewKeys at most, whose walks
+// are short, walk again with the corrected delta.  (dQ at 95 to 160 tokens 2.4e-3 without and
+// 1.7e-3 with; 2 x 1,531 tokens, 6 heads, window 200: 44.1 and 44.8 us, 16,384 tokens 1,974 and
+// 1,965.)
 constexpr uint32_t kUnitBytes = 32768;
+constexpr int kFewKeys = 128;
 
 __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
   __shared__ uint4 sbuf[2][kUnitBytes / 16];
@@ -577,12 +592,9 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
         nd -= bf16f(o[e] & 0xffffu) * float(of[ks][2 * e]) + bf16f(o[e] >> 16) * float(of[ks][2 * e + 1]);
     }
     nd = pair_sum(nd);
-    if (hl == 0) {
-      float* seeds = reinterpret_cast<float*>(a.work + (size_t(bh) * a.tiles + tile) * kSeeds);
-      seeds[q] = nl;
-      seeds[kT + q] = nd;
-    }
+    if (hl == 0) reinterpret_cast<float*>(a.work + (size_t(bh) * a.tiles + tile) * kSeeds)[q] = nl;
   }
+  const float nd0 = nd;                                // from O as it was rounded
   const float c2 = a.scale_log2;
   nl *= c2;
 
@@ -638,8 +650,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
   auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
 
   f32x16 dqt[4];                                       // [4 dim blocks][32 dims x 32 rows]
-#pragma unroll
-  for (int mb = 0; mb < 4; ++mb) dqt[mb] = f32x16{};
+  float eps = 0.f;                                     // the row's sum of dS
 
   // Products of a unit: S0, dP0, S1, dP1, dQ0, dQ1 (eight each, per 32-key block).
   constexpr int kSP = 32, kReads = 2;
@@ -673,6 +684,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
       for (int i = 0; i < 2; ++i) {
         const int at = 2 * (e & 3) + i;
         const float d = sv[n][2 * e + i] * (dp[n][2 * e + i] + nd);
+        eps += d;
         op[n][e >> 2][at] = (__bf16)d;
         rest[n][e >> 2][at] = (__bf16)(d - float(op[n][e >> 2][at]));
       }
@@ -718,26 +730,42 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
     eight(std::integral_constant<int, 40>{});
   };
   const int U = range.count;
-  Unit cur = unit_of(0), next = unit_of(min(1, U - 1));
-  {
-    const Offsets co = offsets(cur);
+  const bool twice = min(int64_t(last) + 1, a.window > 0 ? int64_t(a.window) + a.sinks : INT64_MAX) <= kFewKeys;
+  for (int pass = twice ? 0 : 1;; ++pass) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) issue(cur, co, 0, k);
+    for (int mb = 0; mb < 4; ++mb) dqt[mb] = f32x16{};
+    Unit cur = unit_of(0), next = unit_of(min(1, U - 1));
+    {
+      const Offsets co = offsets(cur);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) issue(cur, co, 0, k);
+    }
+    int u = 0;
+    do {
+      meet<0>();                                       // unit u has landed; the other buffer is free
+      const uint32_t nbuf = uint32_t(u + 1) & 1u;
+      body(cur, next, nbuf);                           // past the end the last unit is copied again, and not read
+      const uint32_t d = (u & 1) ? uint32_t(-int(kUnitBytes)) : kUnitBytes;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) kr[k] += d;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) kt[k >> 1][k & 1] += d;
+      cur = next;
+      next = unit_of(min(u + 2, U - 1));
+    } while (++u < U);
+    if (pass == 1) break;
+    if (U & 1) {                                       // the units start in buffer 0 again
+#pragma unroll
+      for (int k = 0; k < 4; ++k) kr[k] -= kUnitBytes;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) kt[k >> 1][k & 1] -= kUnitBytes;
+    }
+    nd -= pair_sum(eps);
+    eps = 0.f;
+    meet<0>();                                         // both buffers are free
   }
-  int u = 0;
-  do {
-    meet<0>();                                         // unit u has landed; the other buffer is free
-    const uint32_t nbuf = uint32_t(u + 1) & 1u;
-    body(cur, next, nbuf);                             // past the end the last unit is copied again, and not read
-    const uint32_t d = (u & 1) ? uint32_t(-int(kUnitBytes)) : kUnitBytes;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) kr[k] += d;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) kt[k >> 1][k & 1] += d;
-    cur = next;
-    next = unit_of(min(u + 2, U - 1));
-  } while (++u < U);
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));           // no copy outlives the workgroup
+  eps = pair_sum(eps);
   // What is not finite in a key that a row does not see: as in the forward and in dkdv, key by key.
   float probe = 0.f;
 #pragma unroll
@@ -746,24 +774,33 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(BwdArgs a) {
     for (int r = 0; r < 16; ++r) probe += dqt[mb][r];
   if (__ballot(not_finite(probe)) != 0) {
     float out[64];
+    nd = nd0;
+    for (int pass = twice ? 0 : 1;; ++pass) {
+      eps = 0.f;
 #pragma unroll
-    for (int i = 0; i < 64; ++i) out[i] = 0.f;
-    for (int i = 0; i < U; ++i) {
-      const Unit c = unit_of(i);
-      const uint64_t see = seen_bits(pos, c.key0, a.window, a.sinks);
-      for (int k = 0; k < kKeyUnit; ++k) {
-        const bool on = row < rows && ((see >> k) & 1u);
-        if (__ballot(on) == 0) continue;
-        const uint8_t* kr1 = c.k + uint32_t(k) * kstep;
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot_row(qf, kr1, hl), c2, nl));
-        add_row<16>(w * (dot_row(of, c.v + uint32_t(k) * vstep, hl) + nd), kr1, on, 4 * hl, out);
+      for (int i = 0; i < 64; ++i) out[i] = 0.f;
+      for (int i = 0; i < U; ++i) {
+        const Unit c = unit_of(i);
+        const uint64_t see = seen_bits(pos, c.key0, a.window, a.sinks);
+        for (int k = 0; k < kKeyUnit; ++k) {
+          const bool on = row < rows && ((see >> k) & 1u);
+          if (__ballot(on) == 0) continue;
+          const uint8_t* kr1 = c.k + uint32_t(k) * kstep;
+          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot_row(qf, kr1, hl), c2, nl));
+          const float d = w * (dot_row(of, c.v + uint32_t(k) * vstep, hl) + nd);
+          if (on) eps += d;
+          add_row<16>(d, kr1, on, 4 * hl, out);
+        }
       }
+      if (pass == 1) break;
+      nd -= eps;
     }
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dqt[mb][r] = out[16 * mb + r];
   }
+  if (hl == 0) reinterpret_cast<float*>(a.work + (size_t(bh) * a.tiles + tile) * kSeeds)[kT + q] = nd - eps;
   int r_out = row;                                     // (its address is formed here, not held across the walk)
   asm volatile("" : "+v"(r_out));
   if (r_out >= a.tokens * G) return;
