@@ -23,11 +23,13 @@
 // weights; P is rounded to bf16 for the products (the matrix cores' type: half of O's
 // error, the other half is its own rounding), O once at the end.
 //
-// What bounds it: the matrix cores under the power limit where the launch is large, 990
-// TFLOP/s of seen pairs at 16,384 tokens, 32 heads over 8, window 4,096 (970 us; a
-// library product of 8,192 cubed reaches 1,082 on the same card; matrix cores busy 56 %
-// of the cycles at 1.8 GHz); where a CU has one workgroup, a wave's own instructions and
-// waits, 2,800 to 3,700 cycles a unit for 1,024 of products.  (Eight waves a tile, each
+// What bounds it: the matrix cores under the power limit where the launch is large, 1,005
+// to 1,040 TFLOP/s of seen pairs at 16,384 tokens, 32 heads over 8, window 4,096 (925 to
+// 958 us by the card; a library product of 8,192 cubed reaches 1,082 to 1,125; matrix cores
+// busy 55 % of the cycles at 1.85 GHz); where a CU has one workgroup, a unit takes 2,800 to
+// 3,700 cycles for 1,024 of products: of a wave's cycles 46 % issue, 33 % are at wait counts
+// and barriers and 21 % ready but not issued (360 tiles, window 1,024), or 35, 51 and 14 %
+// (64 slices of two units).  (Eight waves a tile, each
 // with one of a unit's key blocks, and four units in LDS took 17.9 us for 16.7 on tiles
 // of 6 units and 87 for 89 on tiles of 65; reading three, five or six operands ahead
 // changed nothing.)

@@ -96,8 +96,8 @@ __host__ __device__ inline void unit_range(int len, int G, int k0, int window, i
   *end = k0 < len ? int((last * G + 63) / 64) : *first;
 }
 
-// What bounds it: four products per pair on the matrix cores, busy 55 % of the cycles
-// at 1.85 GHz: 930 to 980 TFLOP/s at 16,384 tokens, 32 heads over 8, window 2,048
+// What bounds it: four products per pair on the matrix cores, busy 52 % of the cycles
+// at 1.95 GHz: 930 to 980 TFLOP/s at 16,384 tokens, 32 heads over 8, window 2,048
 // (1,050 to 1,110 us).  Phase s is unit s for
 // group 0 and for group 1's dP, unit s-1 for group 1's dS and dK, one workgroup barrier
 // after it.  Q rows live in a ring of four units, dO rows in a ring of three, so that a
@@ -521,8 +521,8 @@ __global__ __launch_bounds__(256) void sum_kernel(BwdArgs a, Cut cut, const floa
 // ------------------------------------------------------------------ dq ----
 //
 // The walk, the unit's layout and its copies are the forward's (token_attn.hip).  What
-// bounds it: four products per pair on the matrix cores, busy 66 % of the cycles at 1.75
-// GHz: 1,135 TFLOP/s at 16,384 tokens, 32 heads over 8, window 2,048 (908 us).  Two
+// bounds it: four products per pair on the matrix cores, busy 63 % of the cycles at 1.8
+// GHz: 1,115 TFLOP/s at 16,384 tokens, 32 heads over 8, window 2,048 (924 us).  Two
 // operands are read ahead: three to six, which the registers hold too, changed nothing.
 // dS goes to its product in two bf16 parts, its rounding and the remainder: rounded once it
 // puts 1.6e-3 on dQ.  The remainder's product costs 200 us of a backward of 1,950 at that

@@ -252,7 +252,8 @@ int check_scale(float scale, float* log2) {
 // sequence as the longest has (`each`), where most of those would find nothing; 0: for each.  Measured (us, for each / to
 // what there is): 255 single tokens and a piece of 512 over 1,000 earlier ones, 8 key heads, attention 408 / 237, write 32 /
 // 11, and 4,160 / 16 MiB of scratch; 7 x 64 and 512 tokens 58 / 36.5; near to even, 3 x 256 and 512 tokens, 45.6 / 44.4; 1,023
-// of 1,024 sequences with few rows 304 / 420: looking up costs a round of 64 sequences after the other.
+// of 1,024 sequences with few rows 304 / 420 (looking up costs a round of 64 sequences after the other): the rule takes the
+// first in those last two.
 int32_t deal_packed(int64_t each, int64_t tiles) { return each > 2 * tiles && tiles <= INT32_MAX ? int32_t(tiles) : 0; }
 
 int check_fork(uft_cache* c, int32_t n, const int32_t* src, const int32_t* dst) {
