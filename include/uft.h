@@ -99,7 +99,8 @@ int uft_write(const uft_cache* cache, int32_t layer, const void* d_k, const uft_
  * not empty), UF_ERR_EMPTY (src has no token), UF_ERR_HIP. */
 int uft_fork(uft_cache* cache, int32_t n, const int32_t* src, const int32_t* dst, void* stream);
 
-/* The same with pages of their own: rows of src are copied (all layers).
+/* The same with pages of their own: rows of src are copied as they are (all layers;
+ * those of a step that is not written yet may hold anything).
  * Errors: as uft_fork, and UF_ERR_CAPACITY. */
 int uft_copy(uft_cache* cache, int32_t n, const int32_t* src, const int32_t* dst, void* stream);
 
@@ -183,7 +184,8 @@ int uft_attn(const uft_cache* cache, int32_t layer, const uft_attn_desc* desc, c
  * exp(scale q.k - LSE), are taken to sum to 1), d_do [batch, tokens, q_heads,
  * head_dim] bf16 contiguous; outputs d_dq (as q) and d_dk, d_dv (as k) bf16,
  * contiguous, fully overwritten; gradients of a key head add over its query heads
- * in fp32.  d_work (16-byte aligned, >= uft_window_bwd_work_bytes) is scratch.  No
+ * in fp32.  The weights are rounded to bf16 for dV, their gradient for dK and, in two
+ * parts, for dQ; everything between is fp32.  d_work (16-byte aligned, >= uft_window_bwd_work_bytes) is scratch.  No
  * atomics: results are reproducible. */
 typedef struct {
   int32_t batch, tokens, q_heads, kv_heads, head_dim;

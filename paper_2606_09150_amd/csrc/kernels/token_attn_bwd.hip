@@ -25,7 +25,7 @@
 // Rounding: scores, P, dP, dS and all sums are fp32.  What a product takes is bf16, the
 // matrix cores' type for its other operand: P for dV, dS for dK, once each; dS for dQ in two
 // parts.  Each such rounding is about as large as the result's own (1.7e-3 of its norm), so
-// that dV and dK are 2.3e-3 to 2.4e-3 off and dQ 1.7e-3 to 2.1e-3.  A second part for dV or
+// that dV and dK are 2.2e-3 to 2.5e-3 off and dQ 1.6e-3 to 2.2e-3.  A second part for dV or
 // dK would be a quarter more products in a kernel that they bound.
 // The transposed operands come from row-major LDS tiles through transposing reads.
 // Every output row is owned by one workgroup and sums have one order: no atomics.
