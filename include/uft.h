@@ -184,9 +184,10 @@ int uft_attn(const uft_cache* cache, int32_t layer, const uft_attn_desc* desc, c
  * exp(scale q.k - LSE), are taken to sum to 1), d_do [batch, tokens, q_heads,
  * head_dim] bf16 contiguous; outputs d_dq (as q) and d_dk, d_dv (as k) bf16,
  * contiguous, fully overwritten; gradients of a key head add over its query heads
- * in fp32.  The weights are rounded to bf16 for dV, their gradient for dK and, in two
- * parts, for dQ; everything between is fp32.  d_work (16-byte aligned, >= uft_window_bwd_work_bytes) is scratch.  No
- * atomics: results are reproducible. */
+ * in fp32.  The weights are rounded to bf16 for dV, the scores' gradients for dK (from
+ * weights in fp16, scaled) and, in two parts, for dQ; everything else is fp32.  d_work
+ * (16-byte aligned, >= uft_window_bwd_work_bytes) is scratch.  No atomics: results are
+ * reproducible. */
 typedef struct {
   int32_t batch, tokens, q_heads, kv_heads, head_dim;
   int32_t window, sinks;
