@@ -16,6 +16,10 @@ The same at the granularity of tokens (``include/uft.h``, bound by ``_tokens``):
 ``TokenCache``, a paged cache of keys and values with the attention that reads it
 (a sliding window with sinks, trees of drafted tokens), and ``window_attention``
 with its gradient for whole sequences.
+
+Linear attention, whose past is one matrix a head (``include/ufs.h``, bound by ``_states``):
+``linear_attention`` with its gradient, ``StateCache`` for the states of prompts and
+single tokens, and ``beam_select``, the selection of a beam search.
 """
 
 from . import _lib
@@ -55,6 +59,7 @@ from ._lib import (
     uf_tile_lists_bytes,
     uf_tile_lists_layout,
 )
+from .states import StateCache, beam_select, linear_attention, linear_attention_bwd
 from .tokens import TokenCache, window_attention, window_attention_bwd
 from .window import KVWindow
 
@@ -67,4 +72,5 @@ __all__ = [
     "uf_sparse_causal_attn_fwd_split_rows", "uf_sparse_causal_attn_bwd", "uf_sparse_causal_attn_bwd_noalloc", "uf_status_string",
     "uf_tile_lists_bytes", "uf_tile_lists_layout", "KVWindow",
     "TokenCache", "window_attention", "window_attention_bwd",
+    "StateCache", "linear_attention", "linear_attention_bwd", "beam_select",
 ]

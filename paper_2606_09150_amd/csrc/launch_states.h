@@ -1,0 +1,123 @@
+// Launch interface of the state operators (internal to libuf.so).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "ufs.h"
+
+namespace uf {
+namespace lin {
+
+constexpr int kD = 128;
+constexpr int kState = kD * kD;              // floats of a state
+constexpr int kChunk = 32;                   // tokens of a chunk
+
+// The cache's device table, the step: kHeader words (sequences, tokens, parts, chunks of a part), then kEntry words for
+// each sequence: its number, its first token of the step, its new tokens, the tokens it held before, its first part.
+constexpr int kHeader = 4;
+constexpr int kEntry = 5;
+
+// Sequences in a launch.  Workgroup or part k * kv_heads + h is part k of the launch and key head h: of plain tensors part
+// k % parts of sequence k / parts, of a step the entry's whose first part is the last at or before k.
+struct Geo {
+  const float* decay;         // [kv_heads]
+  const int32_t* lengths;     // plain tensors: [n] or null
+  const int32_t* step;        // a step's table, or null
+  int32_t n, tokens;          // sequences; tokens of each, or of the step
+  int32_t kv_heads, group;
+  int32_t parts, chunks;      // plain: parts of a sequence, a step: of all; chunks of a part (plain)
+  int32_t max_seqs;           // a step: states of the pool
+  float scale;
+};
+
+struct Src {
+  const uint16_t* p;
+  int64_t batch, token, head;                // elements
+};
+
+// out_t = row weight x_t . M + sum of weights (x_t . y_j) z_j, M = sum of key weights y_j z_j^T: forwards over j <= t (o
+// from q, k, v; dq from do, v, k), or backwards over j >= t (dk from v, do, q; dv from k, q, do).
+struct Walk {
+  Src x, y, z;
+  uint16_t* out;
+  const float* first;         // M where the walk begins, or null
+  float* last;                // M where it ends, or null
+  const float* starts;        // M where each part begins, or null: the only part begins with `first`
+  int32_t trans;              // first and starts hold M transposed
+};
+constexpr int kWalks = 3;
+struct WalkArgs {
+  Geo geo;
+  Walk walk[kWalks];
+  int32_t n;
+};
+// Parts' own M without the parts before (after) them, in their places of `starts`.
+struct PartArgs {
+  Geo geo;
+  struct {
+    Src y, z;
+    const float* first;
+    float* starts;
+    int32_t back;
+  } sum[2];
+  int32_t n;
+};
+
+hipError_t launch_linear_parts(const PartArgs& a, int32_t groups, bool exact, hipStream_t stream);
+hipError_t launch_linear_scan(const PartArgs& a, hipStream_t stream);
+hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, hipStream_t stream);
+hipError_t launch_linear_bwd(const WalkArgs& a, int32_t groups, bool exact, hipStream_t stream);
+
+// Few tokens a sequence: token by token.
+constexpr int kFewTokens = 8;
+struct StepArgs {
+  Geo geo;                    // of a step
+  Src q, k, v;
+  uint16_t* o;
+  float* states;              // of the layer
+  int32_t longest;
+};
+hipError_t launch_linear_step(const StepArgs& a, hipStream_t stream);
+
+// (source, target) sequences in the launch's words
+constexpr int kPairs = 400;
+struct ForkArgs {
+  float* pool;
+  int64_t layer, seq;         // floats of a layer and of a sequence's states in it
+  int32_t layers, n;
+  int32_t words[2 * kPairs];
+};
+hipError_t launch_state_fork(const ForkArgs& a, hipStream_t stream);
+
+constexpr int kMaxBeams = 64;
+struct ReorderArgs {
+  float* pool;
+  int64_t layer, seq;
+  const int32_t* parents;     // of the launch's groups
+  int32_t layers, groups, beams;
+  int32_t seqs[2 * kPairs];
+};
+hipError_t launch_state_reorder(const ReorderArgs& a, hipStream_t stream);
+
+// Selection: slices of rows of logits, then what they hold per request.
+constexpr int kMaxSelect = 64;
+struct SelectArgs {
+  const void* logits;
+  int64_t group_stride, beam_stride;         // elements
+  const float* scores;
+  const uint8_t* done;
+  float* best;
+  int32_t* parents;
+  int32_t* tokens;
+  uint8_t* work;
+  int32_t groups, beams, vocab, k, type, end;
+  int32_t splits, slice;                     // slices of a row, vectors of 16 bytes of each
+};
+void plan_select(SelectArgs* a);
+size_t select_work_bytes(const SelectArgs& a);
+hipError_t launch_select(const SelectArgs& a, hipStream_t stream);
+
+}  // namespace lin
+}  // namespace uf
