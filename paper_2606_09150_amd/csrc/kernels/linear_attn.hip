@@ -30,42 +30,66 @@
 #include "linear_place.h"
 #include "token_common.h"
 
+#include <type_traits>
+
 namespace uf {
 namespace lin {
 namespace {
 
 using namespace attn;
-using tok::bits_upto;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+
 using tok::lds_row;
 using tok::lds_tr2;
 using tok::swz_k;
 
 constexpr uint32_t kTile = 8192, kHalf = 4096, kStage = 3 * kTile;
 constexpr int kStages = 3;
-// LDS behind the stages, in floats: L^e for e = 0 .. 32, and the key weights of a whole chunk and of the last one.
+// LDS behind the stages: P, a row of 32 values in two parts (and 16 bytes, so that rows begin in banks of their own) for each
+// token; then, in floats, L^e for e = 0 .. 32, and the key weights of a whole chunk and of the last one.
+constexpr uint32_t kRow = 144, kP = kStages * kStage, kTable = kP + kChunk * kRow;
 constexpr int kPowers = 36;
-constexpr uint32_t kShared = kStages * kStage + 4 * (kPowers + 2 * kChunk);
+constexpr uint32_t kShared = kTable + 4 * (kPowers + 2 * kChunk);
+static_assert(2 * kShared <= 163840, "two workgroups a CU");
 
-// x as parts of 8 bits each, the first ones cut off and the last one rounded.
-__device__ inline bf16x8 top_part(float (&x)[8], bool rest) {
+// x as parts of 8 bits each, the first ones cut off and the last one rounded.  (Three operations a value and part; by dot products with
+// (-1, 0), which leave out the masking, the copies and waits that those need cost as much.)
+__device__ inline bf16x8 top_part(float (&x)[8]) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     w[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]), 0x07060302u);
-  if (rest)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] -= __uint_as_float(__float_as_uint(x[i]) & 0xffff0000u);
+  for (int i = 0; i < 8; ++i) x[i] -= __uint_as_float(__float_as_uint(x[i]) & 0xffff0000u);
   return as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
 }
 __device__ inline bf16x8 last_part(const float (&x)[8]) {
   return as_bf16x8(make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])));
 }
+// The workgroup's barrier behind its LDS accesses alone.
+constexpr int waitcnt_lds() { return 15 | (7 << 4) | (0 << 8) | (3 << 14); }   // vmcnt 63: none, lgkmcnt 0
+__device__ __forceinline__ void meet_lds() {
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  __builtin_amdgcn_s_waitcnt(waitcnt_lds());
+  __builtin_amdgcn_s_barrier();
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+}
+// A branch that is hardly ever taken: nothing of it is done ahead of it.
+__device__ inline bool seldom(bool x) {
+  const bool y = __builtin_expect(x, 0);
+  return y;
+}
+__device__ inline void stay() { asm volatile("" ::: "memory"); }
 // Sign bits of the halves that are not finite (junk in the others).
 __device__ inline uint32_t odd_halves(uint32_t u) { return (u & 0x7f807f80u) + 0x00800080u; }
 
 __device__ inline double power(double g, int e) { return e == 0 ? 1.0 : exp(g * double(e)); }
 
-// OUT: results are wanted, not M alone.  begin: M where the walk begins, or null; last: where to put it at the end, or null.
+// OUT: results are wanted, not M alone: a part's own M is summed against the walk, so that what is read last is what the
+// walk reads first, with a factor for each chunk in the place of M's.  begin: M where the walk begins, or null; last: where
+// to put it at the end, or null.
 template <bool BACK, bool OUT, int PARTS>
 __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& xs, const Src& ys, const Src& zs, uint16_t* out,
                                      const float* begin, bool trans, float* last, uint8_t* smem) {
@@ -79,34 +103,54 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   // copies: rows 8 wave + lane / 8 of each tile
   const int crow = 8 * wave + (lane >> 3);
   const uint32_t cchunk = uint32_t(16 * ((lane & 7) ^ swz_k(crow & 15)));
-  const int n_items = p.chunks * G;
-  int next_c = 0, next_g = 0;                          // the next item to copy
-  auto issue = [&](uint32_t stage) {
-    const int c = BACK ? p.chunk0 + p.chunks - 1 - next_c : p.chunk0 + next_c;
-    const int t0 = c * kChunk, row = min(crow, p.tokens - 1 - t0);
-    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + stage * kStage + uint32_t(wave) * 1024u);
-    auto copy = [&](const Src& s, int head, uint32_t at) {
-      const uint8_t* base = uniform_ptr(reinterpret_cast<const uint8_t*>(
-          s.p + (geo.step == nullptr ? int64_t(p.seq) * s.batch : 0) + (p.row + t0) * s.token + int64_t(head) * s.head));
-      const uint32_t off = uint32_t(row) * uint32_t(s.token * 2) + cchunk;
-      dma16(base, off, dst + at);
-      dma16(base + 128, off, dst + at + kHalf);
-    };
-    const int hg = h * G + next_g;
-    if (OUT) copy(xs, BACK ? h : hg, 0);
-    copy(ys, BACK ? hg : h, kTile);
-    copy(zs, BACK ? hg : h, 2 * kTile);
-    // past the end the last item is copied again, and not read
-    if (next_g + 1 < G) ++next_g;
-    else if (next_c + 1 < p.chunks) ++next_c, next_g = 0;
+  const int heads = OUT || BACK ? G : 1;               // items of a chunk
+  constexpr bool kDown = OUT == BACK;                  // from the last chunk to the first
+  // (the copies' sources move on by steps of a chunk, or of a query head)
+  struct Tile {
+    const uint8_t* at;
+    int64_t head;
+    int32_t token;
   };
-  if (n_items > 0) {
+  auto tile = [&](const Src& src, bool grouped) {
+    Tile t;
+    const int first = kDown ? p.chunk0 + p.chunks - 1 : p.chunk0;
+    t.at = uniform_ptr(reinterpret_cast<const uint8_t*>(src.p + (geo.step == nullptr ? int64_t(p.seq) * src.batch : 0) +
+                                                        (p.row + first * kChunk) * src.token + int64_t(grouped ? h * G : h) * src.head));
+    t.head = grouped ? 2 * src.head : 0;
+    t.token = int32_t(2 * src.token);                  // (at most 2^25)
+    return t;
+  };
+  Tile tx = OUT ? tile(xs, !BACK) : Tile{}, ty = tile(ys, BACK), tz = tile(zs, BACK);
+  int next_t = (kDown ? p.chunk0 + p.chunks - 1 : p.chunk0) * kChunk, next_c = 0, next_g = 0;   // the next item to copy
+  auto issue = [&](uint32_t stage) {
+    const int row = min(crow, p.tokens - 1 - next_t);
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + stage * kStage + uint32_t(wave) * 1024u);
+    auto copy = [&](const Tile& t, uint32_t at) {
+      const uint32_t off = uint32_t(row) * uint32_t(t.token) + cchunk;
+      dma16(t.at, off, dst + at);
+      dma16(t.at + 128, off, dst + at + kHalf);
+    };
+    if (OUT) copy(tx, 0);
+    copy(ty, kTile);
+    copy(tz, 2 * kTile);
+    // past the end the last item is copied again, and not read
+    if (next_g + 1 < heads) {
+      ++next_g;
+      tx.at += tx.head, ty.at += ty.head, tz.at += tz.head;
+    } else if (next_c + 1 < p.chunks) {
+      auto on = [&](Tile& t) { t.at += int64_t(kDown ? -kChunk : kChunk) * t.token - (heads - 1) * t.head; };
+      on(tx), on(ty), on(tz);
+      ++next_c, next_g = 0;
+      next_t += kDown ? -kChunk : kChunk;
+    }
+  };
+  if (p.chunks > 0) {
     issue(0);
     issue(1);
   }
 
   // weights
-  float* const tab = reinterpret_cast<float*>(smem + kStages * kStage);
+  float* const tab = reinterpret_cast<float*>(smem + kTable);
   const double gd = double(geo.decay[h]);
   const float scale = geo.scale;
   if (tid < 33) tab[tid] = float(power(gd, tid));
@@ -117,21 +161,21 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   const double dw = power(gd, kChunk);
   const float whole_hi = float(dw), whole_lo = float(dw - double(whole_hi)), rest_dec = float(power(gd, max(rest, 0)));
   __syncthreads();
-  float pw[16];                                        // of (x_t.y_j), j = 8 (r / 4) + 4 hl + r % 4 of the chunk
-  uint32_t see = 0;
-  if (OUT) {
+  // P: this wave's quarter, x_t.y_j for j = pj .. pj + 3 and t = pt
+  const int pq = lane >> 4, pj = 16 * (wave >> 1) + 4 * pq, pt = 16 * (wave & 1) + rp;
+  float pw[4];
+  bool seen[4];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int j = 8 * (r >> 2) + 4 * hl + (r & 3), age = BACK ? j - ln : ln - j;
-      pw[r] = scale * tab[max(age, 0)];
-      see |= uint32_t(age >= 0) << r;
-    }
+  for (int r = 0; r < 4; ++r) {
+    const int age = BACK ? pj + r - pt : pt - pj - r;
+    pw[r] = scale * tab[max(age, 0)];
+    seen[r] = age >= 0;
   }
   const float row_whole = BACK ? tab[31 - ln] : scale * tab[ln + 1];
   const float row_rest = BACK ? tab[max(rest - 1 - ln, 0)] : row_whole;
 
   // operand addresses within a stage
-  uint32_t kr[4], yt[2][2], zt[2];
+  uint32_t kr[4], yt[2][2], zt[2], py[2], px[2];
 #pragma unroll
   for (int k = 0; k < 4; ++k) kr[k] = lds0 + uint32_t(ln * 128 + 16 * ((2 * k + hl) ^ swz_k(ln & 15)));
 #pragma unroll
@@ -143,7 +187,16 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     zt[hh] = lds0 + 2 * kTile + uint32_t(wave >> 1) * kHalf +
              uint32_t(r * 128 + 16 * ((4 * (wave & 1) + 2 * gr + ((rp >> 1) & 1)) ^ swz_k(r)) + 8 * (rp & 1));
   }
-  const uint32_t kwt = lds0 + kStages * kStage + 4 * (kPowers + 4 * hl);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {                        // rows 16 .. of Y and X, dims 32 k + 8 pq ..
+    const uint32_t c = 16 * ((4 * k + pq) ^ swz_k(rp));
+    py[k] = lds0 + kTile + uint32_t((16 * (wave >> 1) + rp) * 128) + c;
+    px[k] = lds0 + uint32_t((16 * (wave & 1) + rp) * 128) + c;
+  }
+  // P's places of j within 16 have bits 2 and 3 swapped, as the k-slots of Z^T
+  const uint32_t pput = lds0 + kP + uint32_t(pt) * kRow + 2 * (16 * (wave >> 1) + 4 * (2 * (pq & 1) + (pq >> 1)));
+  const uint32_t pget = lds0 + kP + uint32_t(ln) * kRow + 16 * hl;
+  const uint32_t kwt = lds0 + kTable + 4 * (kPowers + 4 * hl);
 
   // M: y-dim 32 mt + 16 (r / 8) + 8 hl + r % 8, z-dim 32 wave + ln
   f32x16 S[4];
@@ -160,160 +213,236 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
       }
   }
 
-  f32x16 o = f32x16{};
-  uint2 pend[4];                                       // a result that waits to be stored
-  uint16_t* pend_at = nullptr;
-  auto flush = [&] {
-    if (pend_at != nullptr)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint2*>(pend_at + 8 * i) = pend[i];
-  };
+  f32x16 os = f32x16{}, op = f32x16{};                  // O^T: of M, without the row's weight, and of P
   const int out_heads = geo.kv_heads * (BACK ? 1 : G);
-  uint16_t* const out_row = out + (p.row + (geo.step == nullptr ? int64_t(p.seq) * p.rows : 0)) * out_heads * kD + 32 * wave + 4 * hl;
+  // a result on its way: through the place of x in LDS, from where whole rows are stored, by the wave that then copies the next
+  // item's rows there
+  const uint32_t put = lds0 + uint32_t(wave >> 1) * kHalf + uint32_t(ln * 128 + 8 * hl);
+  const uint32_t get = lds0 + uint32_t(rp >> 3) * kHalf;
+  uint16_t* const out_row = OUT ? out + (p.row + (geo.step == nullptr ? int64_t(p.seq) * p.rows : 0)) * out_heads * kD + 8 * rp : nullptr;
+  int held_n = 0;                                      // its rows, or none
+  int64_t held_at = 0;
+  auto flush = [&](uint32_t stage) {
+    if (held_n == 0) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = 8 * wave + 4 * i + pq;
+      const uint4 u = __builtin_bit_cast(uint4, lds_row(get + stage * kStage + uint32_t(row * 128 + 16 * ((rp & 7) ^ swz_k(row & 15)))));
+      if (row < held_n) *reinterpret_cast<uint4*>(out_row + held_at + int64_t(row) * out_heads * kD) = u;
+    }
+    __builtin_amdgcn_s_waitcnt(waitcnt_lds());         // (read, before the copies to come)
+    held_n = 0;
+  };
   float err = 0.f;                                     // of the factors so far, relative
-  int c = 0, g = 0;
+  double far = 1.0;                                    // without results: the chunk's factor
   uint32_t stage = 0;
-  for (int i = 0; i < n_items; ++i) {
-    meet<OUT ? 6 : 4>();                               // this item has landed, and the last one's buffer is free
-    if (OUT) flush();
-    issue(stage == 0 ? 2 : stage - 1);
-    const int chunk = BACK ? p.chunk0 + p.chunks - 1 - c : p.chunk0 + c;
-    const int n = min(kChunk, p.tokens - chunk * kChunk);
-    const bool full = n == kChunk;
-    const uint32_t at = stage * kStage;
+  int chunk = 0, n = 0;                                // the chunk and its tokens
+  bool full = true;
+  bf16x8 z[2];                                         // Z^T: z-dim zd, tokens 16 kk + 4 hl .. + 3 and 8 more
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
 
-    // Z^T: z-dim zd, tokens 16 kk + 4 hl .. + 3 and 8 more
-    bf16x8 z[2], zf[2];
+  // An item's way to its result; FIRST: the first query head of the chunk.  Products and vector work are dealt out so that each
+  // has the other to run beside.
+  auto result = [&](auto first, int g) {
+    constexpr bool kOfM = decltype(first)::value || !BACK;   // (backwards the sum over the query heads begins)
+    const uint32_t at = stage * kStage;
+    // (its parts are formed anew for each query head: held, they would take 64 registers that are not there)
+    if (kOfM) asm volatile("" : "+v"(S[0]), "+v"(S[1]), "+v"(S[2]), "+v"(S[3]));
+    // this wave's quarter of P^T = Y X^T
+    f32x4 s = f32x4{};
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      const uint32_t c = at + (ks >> 1) * kHalf;
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row(py[ks & 1] + c), lds_row(px[ks & 1] + c), s, 0, 0, 0);
+    }
+    auto row = [&](int ks) { return lds_row(kr[ks & 3] + at + (ks >> 2) * kHalf); };
+    bf16x8 x[3];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) x[k] = row(k);
+    fence();
+    {
+      float w[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        w[r] = seen[r] ? s[r] * pw[r] : 0.f;
+        if (BACK && pj + r >= n) w[r] = 0.f;
+      }
+      uint32_t top[2], low[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        top[i] = __builtin_amdgcn_perm(__float_as_uint(w[2 * i + 1]), __float_as_uint(w[2 * i]), 0x07060302u);
+        low[i] = pack_bf16x2(w[2 * i] - __uint_as_float(__float_as_uint(w[2 * i]) & 0xffff0000u),
+                             w[2 * i + 1] - __uint_as_float(__float_as_uint(w[2 * i + 1]) & 0xffff0000u));
+      }
+      *(lds_u32x2*)(uintptr_t)(pput) = u32x2{top[0], top[1]};
+      *(lds_u32x2*)(uintptr_t)(pput + 64) = u32x2{low[0], low[1]};
+    }
+    if (kOfM) {
+      os = f32x16{};
+      op = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        fence();
+        if (ks + 2 < 8) x[(ks + 2) % 3] = row(ks + 2);
+        float m[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m[e] = S[ks >> 1][8 * (ks & 1) + e];
+        const bf16x8 hi = top_part(m), lo = last_part(m);
+        os = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, x[ks % 3], os, 0, 0, 0);
+        os = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, x[ks % 3], os, 0, 0, 0);
+      }
+    }
+    fence();
+    bf16x8 zf[2] = {z[0], z[1]};
+    uint32_t bits = 0;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      const uint4 u = __builtin_bit_cast(uint4, z[kk]);
+      bits |= odd_halves(u.x) | odd_halves(u.y) | odd_halves(u.z) | odd_halves(u.w);
+    }
+    const bool any_odd = __ballot((bits & 0x80008000u) != 0) != 0;
+    int odd = BACK ? -1 : kChunk;                      // the first (last) token whose value zd is not finite
+    if (seldom(any_odd)) {                             // weights of zero would carry it to tokens that do not see it
+      stay();
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (tok::not_finite(float(z[kk][e]))) {
+            const int j = 16 * kk + 8 * (e >> 2) + 4 * hl + (e & 3);
+            odd = BACK ? max(odd, j) : min(odd, j);
+            zf[kk][e] = (__bf16)0.f;
+          }
+      const int other = __shfl_xor(odd, 32);
+      odd = BACK ? max(odd, other) : min(odd, other);
+    }
+    meet_lds();                                        // P is there, and nobody needs x any more
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      op = __builtin_amdgcn_mfma_f32_32x32x16_bf16(zf[kk], lds_row(pget + 32 * kk), op, 0, 0, 0);
+      op = __builtin_amdgcn_mfma_f32_32x32x16_bf16(zf[kk], lds_row(pget + 32 * kk + 64), op, 0, 0, 0);
+    }
+    if (seldom(any_odd)) {
+      stay();
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int of = __shfl(odd, 8 * (r >> 2) + 4 * hl + (r & 3));
+        if (BACK ? ln <= of : ln >= of) op[r] = __builtin_nanf("");
+      }
+    }
+  };
+  auto keep = [&](int g) {                             // the result, to be stored behind the next barrier
+    const float weight = full ? row_whole : row_rest;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float r[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(os[4 * k + i], weight, op[4 * k + i]);
+      *(lds_u32x2*)(uintptr_t)(put + stage * kStage + 16 * ((4 * (wave & 1) + k) ^ swz_k(ln & 15))) =
+          u32x2{pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
+    }
+    held_n = n;
+    held_at = (int64_t(chunk) * kChunk * out_heads + (BACK ? h : h * G + g)) * kD;
+  };
+  // M past the chunk (of its first query head, backwards), and the present item's part.
+  auto advance = [&](auto first, auto&& between) {
+    constexpr bool kForget = OUT && decltype(first)::value;
+    float dec = 1.f;
+    if (kForget) {
+      const float want = whole_lo + err;
+      dec = full ? whole_hi + want : rest_dec;
+      if (full) err = want - (dec - whole_hi);
+    }
+    const uint32_t kw = kwt + (full ? 0u : 4u * kChunk), at = stage * kStage;
+    bf16x8 part[2][PARTS], y[2][2];
+    auto operand = [&](int mt, int kk) {
+      const uint32_t ya = at + (mt >> 1) * kHalf + kk * 2048;
+      return lds_tr2(yt[0][mt & 1] + ya, yt[1][mt & 1] + ya);
+    };
+    float c8[2][8];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      const float4 a = __builtin_bit_cast(float4, *(const tok::lds_u32x4*)(uintptr_t)(kw + 64 * kk));
+      const float4 b = __builtin_bit_cast(float4, *(const tok::lds_u32x4*)(uintptr_t)(kw + 64 * kk + 32));
+      const float t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c8[kk][e] = t[e];
+      y[0][kk] = operand(0, kk);
+    }
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = float(z[kk][e]) * (OUT ? c8[kk][e] : c8[kk][e] * float(far));
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k) part[kk][k] = k == PARTS - 1 ? last_part(w) : top_part(w);
+    }
+    if (kForget) S[0] *= dec;
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt) {
+      fence();
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        if (mt < 3) y[(mt + 1) & 1][kk] = operand(mt + 1, kk);
+#pragma unroll
+        for (int k = PARTS - 1; k >= 0; --k) S[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[mt & 1][kk], part[kk][k], S[mt], 0, 0, 0);
+      }
+      if (kForget && mt < 3) S[mt + 1] *= dec;
+      if (mt == 1) between();
+    }
+    fence();
+  };
+  auto begin_item = [&] {
+    meet<OUT ? 6 : 4>();                               // this item has landed, and the last one's buffer is free
+    const uint32_t before = stage == 0 ? 2 : stage - 1;
+    if (OUT) flush(before);
+    issue(before);
+    const uint32_t at = stage * kStage;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) z[kk] = lds_tr2(zt[0] + at + kk * 2048, zt[1] + at + kk * 2048);
-    if (!full) {
+    if (seldom(!full)) {
+      stay();
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (16 * kk + 8 * (e >> 2) + 4 * hl + (e & 3) >= n) z[kk][e] = (__bf16)0.f;
     }
-    zf[0] = z[0];
-    zf[1] = z[1];
-    int odd = BACK ? -1 : kChunk;                      // the first (last) token whose value zd is not finite
-    bool any_odd = false;
-    if (OUT) {
-      uint32_t bits = 0;
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        const uint4 u = __builtin_bit_cast(uint4, z[kk]);
-        bits |= odd_halves(u.x) | odd_halves(u.y) | odd_halves(u.z) | odd_halves(u.w);
-      }
-      any_odd = __ballot((bits & 0x80008000u) != 0) != 0;
-      if (any_odd) {                                   // weights of zero would carry it to tokens that do not see it
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (tok::not_finite(float(z[kk][e]))) {
-              const int j = 16 * kk + 8 * (e >> 2) + 4 * hl + (e & 3);
-              odd = BACK ? max(odd, j) : min(odd, j);
-              zf[kk][e] = (__bf16)0.f;
-            }
-        const int other = __shfl_xor(odd, 32);
-        odd = BACK ? max(odd, other) : min(odd, other);
-      }
-    }
+  };
+  auto end_item = [&] { stage = stage == 2 ? 0 : stage + 1; };
+  const std::true_type yes;
+  const std::false_type no;
 
-    if (OUT) {
-      bf16x8 x[8];
-      f32x16 s = f32x16{};
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        x[ks] = lds_row(kr[ks & 3] + at + (ks >> 2) * kHalf);
-        const bf16x8 y = lds_row(kr[ks & 3] + at + kTile + (ks >> 2) * kHalf);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, x[ks], s, 0, 0, 0);
+  for (int c = 0; c < p.chunks; ++c) {
+    chunk = kDown ? p.chunk0 + p.chunks - 1 - c : p.chunk0 + c;
+    n = min(kChunk, p.tokens - chunk * kChunk);
+    full = n == kChunk;
+    begin_item();
+    if (BACK) {
+      if (OUT) result(yes, 0);
+      advance(yes, [&] { if (OUT && G == 1) keep(0); });
+      end_item();
+      for (int g = 1; g < G; ++g) {
+        begin_item();
+        if (OUT) result(no, g);
+        advance(no, [&] { if (OUT && g == G - 1) keep(0); });
+        end_item();
       }
-      if (!BACK || g == 0) {                           // (backwards the sum over the query heads begins)
-        o = f32x16{};
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-          float m[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) m[e] = S[ks >> 1][8 * (ks & 1) + e];
-          const bf16x8 hi = top_part(m, true), lo = last_part(m);
-          o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, x[ks], o, 0, 0, 0);
-          o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, x[ks], o, 0, 0, 0);
-        }
-        o *= full ? row_whole : row_rest;
+    } else {
+      for (int g = 0; g < heads - 1; ++g) {            // (without results there is one item a chunk)
+        result(yes, g);
+        keep(g);
+        end_item();
+        begin_item();
       }
-      uint32_t mask = see;
-      if (BACK && !full) {
-        mask = 0;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int j = 8 * (r >> 2) + 4 * hl + (r & 3);
-          mask |= uint32_t(j >= ln && j < n) << r;
-        }
-      }
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        float w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = (mask >> (8 * kk + e)) & 1u ? s[8 * kk + e] * pw[8 * kk + e] : 0.f;
-        const bf16x8 hi = top_part(w, true), lo = last_part(w);
-        o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(zf[kk], hi, o, 0, 0, 0);
-        o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(zf[kk], lo, o, 0, 0, 0);
-      }
-      if (any_odd) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int of = __shfl(odd, 8 * (r >> 2) + 4 * hl + (r & 3));
-          if (BACK ? ln <= of : ln >= of) o[r] = __builtin_nanf("");
-        }
-      }
-      if (!BACK || g == G - 1) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) pend[k] = make_uint2(pack_bf16x2(o[4 * k], o[4 * k + 1]), pack_bf16x2(o[4 * k + 2], o[4 * k + 3]));
-        pend_at = ln < n ? out_row + (int64_t(chunk * kChunk + ln) * out_heads + (BACK ? h : h * G + g)) * kD : nullptr;
-      } else {
-        pend_at = nullptr;
-      }
+      if (OUT) result(yes, G - 1);
+      advance(yes, [&] { if (OUT) keep(G - 1); });
+      end_item();
     }
-
-    // M past the chunk: forwards behind the last query head, backwards each one's own part
-    if (BACK ? g == 0 : g == G - 1) {
-      const float want = whole_lo + err;
-      const float dec = full ? whole_hi + want : rest_dec;
-      if (full) err = want - (dec - whole_hi);
-#pragma unroll
-      for (int mt = 0; mt < 4; ++mt) S[mt] *= dec;
-    }
-    if (BACK || g == G - 1) {
-      const uint32_t kw = kwt + (full ? 0u : 4u * kChunk);
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        float w[8];
-        {
-          const float4 a = __builtin_bit_cast(float4, *(const tok::lds_u32x4*)(uintptr_t)(kw + 64 * kk));
-          const float4 b = __builtin_bit_cast(float4, *(const tok::lds_u32x4*)(uintptr_t)(kw + 64 * kk + 32));
-          const float c8[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = float(z[kk][e]) * c8[e];
-        }
-        bf16x8 part[PARTS];
-#pragma unroll
-        for (int k = 0; k < PARTS; ++k) part[k] = k == PARTS - 1 ? last_part(w) : top_part(w, true);
-#pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
-          const uint32_t ya = at + (mt >> 1) * kHalf + kk * 2048;
-          const bf16x8 y = lds_tr2(yt[0][mt & 1] + ya, yt[1][mt & 1] + ya);
-#pragma unroll
-          for (int k = PARTS - 1; k >= 0; --k) S[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, part[k], S[mt], 0, 0, 0);
-        }
-      }
-    }
-    stage = stage == 2 ? 0 : stage + 1;
-    if (g + 1 < G) ++g;
-    else g = 0, ++c;
+    if (!OUT) far *= full ? dw : double(rest_dec);
   }
   meet<0>();                                           // no copy outlives the walk
-  if (OUT) flush();
+  if (OUT) flush(stage == 0 ? 2 : stage - 1);
   if (last != nullptr) {
 #pragma unroll
     for (int mt = 0; mt < 4; ++mt)
@@ -323,10 +452,10 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   if (OUT && geo.step == nullptr) {                    // padding
     const int from = max(p.tokens, p.part * geo.chunks * kChunk);
     const int to = p.part == geo.parts - 1 ? p.rows : min(p.rows, (p.part + 1) * geo.chunks * kChunk);
-    const int heads = BACK ? 1 : G;
-    uint16_t* const row0 = out + int64_t(p.seq) * p.rows * out_heads * kD + int64_t(h) * heads * kD;
-    for (int64_t k = tid; k < int64_t(max(to - from, 0)) * heads * 16; k += 256) {
-      const int64_t t = k / (heads * 16), w = k % (heads * 16);
+    const int own = BACK ? 1 : G;
+    uint16_t* const row0 = out + int64_t(p.seq) * p.rows * out_heads * kD + int64_t(h) * own * kD;
+    for (int64_t k = tid; k < int64_t(max(to - from, 0)) * own * 16; k += 256) {
+      const int64_t t = k / (own * 16), w = k % (own * 16);
       *reinterpret_cast<uint4*>(row0 + (from + t) * out_heads * kD + w * 8) = make_uint4(0, 0, 0, 0);
     }
   }
@@ -344,9 +473,10 @@ __device__ __forceinline__ void run_walk(const Geo& geo, const Walk& w, int idx,
   walk<BACK, true, PARTS>(geo, p, w.x, w.y, w.z, w.out, begin, w.trans != 0, ends && w.last != nullptr ? w.last + at : nullptr, smem);
 }
 
+template <int PARTS>
 __global__ __launch_bounds__(256, 2) void linear_fwd_kernel(WalkArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kShared];
-  run_walk<false, 3>(a.geo, a.walk[0], blockIdx.x, smem);
+  run_walk<false, PARTS>(a.geo, a.walk[0], blockIdx.x, smem);
 }
 
 // dk, dv and dq of eight workgroups' places one after the other: a place's three lie on one XCD, and share their reads there.
@@ -374,13 +504,14 @@ __global__ __launch_bounds__(256, 2) void linear_parts_kernel(PartArgs a, int gr
   }
 }
 
-// Parts' beginnings from their own M, part by part.  A workgroup per (sequence, key head, eighth of M).
-constexpr int kEighth = kState / 8;
+// Parts' beginnings from their own M, part by part, kAhead of them read at once.  A workgroup per (sequence, key head,
+// sixteenth of M).
+constexpr int kSlices = kState / 1024, kAhead = 16;
 __global__ __launch_bounds__(256) void linear_scan_kernel(PartArgs a) {
   const Geo& geo = a.geo;
   int k = blockIdx.x;
-  const int eighth = k % 8;
-  k /= 8;
+  const int slice = k % kSlices;
+  k /= kSlices;
   const int h = k % geo.kv_heads;
   k /= geo.kv_heads;
   const int e = k % geo.n;
@@ -403,32 +534,33 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(PartArgs a) {
   }
   const int chunks = geo.step == nullptr ? geo.chunks : max(1, ((const const_i32*)geo.step)[3]);
   const double gd = double(geo.decay[h]);
-  const int at = eighth * kEighth + threadIdx.x * 4;
-  constexpr int kV = kEighth / 1024;                   // float4 of a thread
-  float4 m[kV];
-#pragma unroll
-  for (int v = 0; v < kV; ++v) m[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (s.first != nullptr && p.held) {
-    const float* from = s.first + (size_t(p.seq) * geo.kv_heads + h) * kState + at;
-#pragma unroll
-    for (int v = 0; v < kV; ++v) m[v] = *reinterpret_cast<const float4*>(from + 1024 * v);
-  }
+  const int at = slice * 1024 + threadIdx.x * 4;
+  float4 m = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (s.first != nullptr && p.held)
+    m = *reinterpret_cast<const float4*>(s.first + (size_t(p.seq) * geo.kv_heads + h) * kState + at);
   const int tail = p.tokens - (p.parts - 1) * chunks * kChunk;
   const double whole = power(gd, chunks * kChunk), part = power(gd, max(tail, 0));
-  for (int i = 0; i < p.parts; ++i) {
+  auto slot = [&](int i) {
     const int q = s.back ? p.parts - 1 - i : i;
-    float* const slot = s.starts + (size_t(first + q) * geo.kv_heads + h) * kState + at;
-    const double d = q == p.parts - 1 ? part : whole;
-    const float hi = float(d), lo = float(d - double(hi));
+    return reinterpret_cast<float4*>(s.starts + (size_t(first + q) * geo.kv_heads + h) * kState + at);
+  };
+  for (int i0 = 0; i0 < p.parts; i0 += kAhead) {
+    float4 own[kAhead];
 #pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      float4* const to = reinterpret_cast<float4*>(slot + 1024 * v);
-      const float4 own = i + 1 < p.parts ? *to : make_float4(0.f, 0.f, 0.f, 0.f);
-      *to = m[v];
-      m[v].x = __builtin_fmaf(m[v].x, hi, __builtin_fmaf(m[v].x, lo, own.x));
-      m[v].y = __builtin_fmaf(m[v].y, hi, __builtin_fmaf(m[v].y, lo, own.y));
-      m[v].z = __builtin_fmaf(m[v].z, hi, __builtin_fmaf(m[v].z, lo, own.z));
-      m[v].w = __builtin_fmaf(m[v].w, hi, __builtin_fmaf(m[v].w, lo, own.w));
+    for (int i = 0; i < kAhead; ++i) {
+      own[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i0 + i + 1 < p.parts) own[i] = *slot(i0 + i);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (i0 + i >= p.parts) break;
+      *slot(i0 + i) = m;
+      const double d = (s.back ? i0 + i == 0 : i0 + i == p.parts - 1) ? part : whole;
+      const float hi = float(d), lo = float(d - double(hi));
+      m.x = __builtin_fmaf(m.x, hi, __builtin_fmaf(m.x, lo, own[i].x));
+      m.y = __builtin_fmaf(m.y, hi, __builtin_fmaf(m.y, lo, own[i].y));
+      m.z = __builtin_fmaf(m.z, hi, __builtin_fmaf(m.z, lo, own[i].z));
+      m.w = __builtin_fmaf(m.w, hi, __builtin_fmaf(m.w, lo, own[i].w));
     }
   }
 }
@@ -442,12 +574,13 @@ hipError_t launch_linear_parts(const PartArgs& a, int32_t groups, bool exact, hi
 }
 
 hipError_t launch_linear_scan(const PartArgs& a, hipStream_t stream) {
-  linear_scan_kernel<<<dim3(unsigned(8 * a.geo.kv_heads) * a.geo.n * a.n), 256, 0, stream>>>(a);
+  linear_scan_kernel<<<dim3(unsigned(kSlices * a.geo.kv_heads) * a.geo.n * a.n), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, hipStream_t stream) {
-  linear_fwd_kernel<<<dim3(unsigned(groups)), 256, 0, stream>>>(a);
+hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, bool exact, hipStream_t stream) {
+  if (exact) linear_fwd_kernel<3><<<dim3(unsigned(groups)), 256, 0, stream>>>(a);
+  else linear_fwd_kernel<2><<<dim3(unsigned(groups)), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

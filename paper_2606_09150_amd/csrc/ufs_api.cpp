@@ -152,6 +152,7 @@ int ufs_linear_fwd(const ufs_linear_desc* d, const void* d_q, const void* d_k, c
     a.geo.decay = d_decay;
     a.geo.lengths = d_lengths;
     const int32_t groups = a.geo.n * a.geo.parts * a.geo.kv_heads;
+    const bool exact = true;
     float* starts = nullptr;
     if (a.geo.parts > 1) {
       starts = static_cast<float*>(d_work);
@@ -159,12 +160,12 @@ int ufs_linear_fwd(const ufs_linear_desc* d, const void* d_q, const void* d_k, c
       p.geo = a.geo;
       p.n = 1;
       p.sum[0] = {src(d_k, d->k), src(d_v, d->v), d_state, starts, 0};
-      if (int s = check_hip(lin::launch_linear_parts(p, groups, true, st), "linear attention")) return s;
+      if (int s = check_hip(lin::launch_linear_parts(p, groups, exact, st), "linear attention")) return s;
       if (int s = check_hip(lin::launch_linear_scan(p, st), "linear attention")) return s;
     }
     a.n = 1;
     a.walk[0] = lin::Walk{src(d_q, d->q), src(d_k, d->k), src(d_v, d->v), static_cast<uint16_t*>(d_o), d_state, d_final, starts, 0};
-    if (int s = check_hip(lin::launch_linear_fwd(a, groups, st), "linear attention")) return s;
+    if (int s = check_hip(lin::launch_linear_fwd(a, groups, exact, st), "linear attention")) return s;
     return ok();
   });
 }
@@ -473,7 +474,7 @@ int ufs_attn(const ufs_cache* c, int32_t layer, const ufs_attn_desc* d, const vo
     a.geo = g;
     a.n = 1;
     a.walk[0] = lin::Walk{src(d_q, d->q), src(d_k, d->k), src(d_v, d->v), static_cast<uint16_t*>(d_o), states, states, starts, 0};
-    if (int s = check_hip(lin::launch_linear_fwd(a, groups, st), "linear attention")) return s;
+    if (int s = check_hip(lin::launch_linear_fwd(a, groups, true, st), "linear attention")) return s;
     return ok();
   });
 }
