@@ -10,10 +10,10 @@
 //
 // A list holds 64-bit keys, the value in an order of integers, then the place, lowest
 // first: all different, so that what is selected does not depend on the order in
-// which threads add to it.  The first block's threshold comes from the lanes' maxima: each of
-// four waves has ceil(n / 4) lanes at or above its own such maximum, so that n
-// values are at or above the least of the four.  Later values pass only above it; what
-// passes lies in LDS, and is cut down to the n largest where the next block might not fit.
+// which it was found.  In a slice each wave keeps a list of its own in LDS, without a
+// barrier: values above a bar join it, and the bar is the n-th largest of the lanes' maxima, at
+// first of the first block's, later of the list's (n values are at or above it, and what comes
+// later has a higher place).  A list that might not hold the next block is cut down to its n largest.
 #include <algorithm>
 
 #include "../launch_states.h"
@@ -24,10 +24,12 @@ namespace uf {
 namespace lin {
 namespace {
 
-constexpr int kThreads = 256, kVectors = 2;            // 16-byte vectors of a thread and block
-constexpr int kBlock = kThreads * kVectors * 8;        // values of a block at most
-constexpr int kRoom = kBlock + kThreads;               // keys in LDS
-constexpr int kMine = kRoom / kThreads;                // of a thread
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kEach = 16;                              // values of a lane and block
+constexpr int kBlock = 64 * kEach;                     // of a wave and block
+constexpr int kRoom = kBlock + 128, kMine = kRoom / 64;   // keys of a wave's list; of a lane
+constexpr int kFew = 128;                              // keys of a list that are put in order by counting
+constexpr float kLog2e = 1.44269504f;
 constexpr uint32_t kNone = 0x007fffffu;                // -inf in the order of integers: nothing at or below it is taken
 
 // float32 in the order of unsigned integers, -0 as 0.
@@ -36,97 +38,130 @@ __device__ inline uint32_t ordered(float x) {
   return u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
 }
 __device__ inline float value_of(uint32_t o) { return __uint_as_float(o ^ (uint32_t(~int32_t(o) >> 31) | 0x80000000u)); }
+__device__ inline int below_me(uint64_t mask) {        // lanes of the mask before this one
+  return __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
+}
+// A t that n values are at or above, the largest whose last `rest` bits are 0, bit by bit; `above` counts them over the wave.  (Loops over bits stay loops
+// here: a workgroup goes through this code once, and waits for every line of it to be fetched.)
+template <class Above>
+__device__ inline uint32_t nth(int n, int rest, Above above) {
+  uint32_t t = 0;
+#pragma unroll 1
+  for (int bit = 31; bit >= rest; --bit) {
+    const uint32_t c = t | (1u << bit);
+    if (above(c) >= n) t = c;
+  }
+  return t;
+}
 
-struct Shared {
-  uint64_t keys[kRoom];
-  uint64_t out[kMaxSelect + 1];
-  uint32_t count, sum[2];
-  uint32_t low[4];
-};
-
-// The n largest keys of what a workgroup is shown.
-struct Best {
-  Shared& s;
+// A wave's list: the n largest keys of what it is shown, among others.  All calls by whole waves.
+struct List {
+  uint64_t* keys;
   int n;
   bool ascending;                                      // blocks come in the order of their places
+  int count = 0, seen = 0;                             // keys; of them when the bar was last raised
   uint32_t bar = kNone;                                // values above it pass
 
-  __device__ Best(Shared& s_, int n_, bool ascending_) : s(s_), n(n_), ascending(ascending_) {
-    if (threadIdx.x == 0) s.count = 0;
-    __syncthreads();
-  }
-  // A bar from the threads' largest values so far (`top`), of which at least n have to stay above it.
-  __device__ void set_bar(uint32_t top) {
-    const int want = (n + 3) / 4;
-    uint32_t t = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t c = t | (1u << bit);
-      if (__popcll(__ballot(top >= c)) >= want) t = c;
-    }
-    if ((threadIdx.x & 63) == 0) s.low[threadIdx.x >> 6] = t;
-    __syncthreads();
-    const uint32_t low = min(min(s.low[0], s.low[1]), min(s.low[2], s.low[3]));
-    bar = max(low, kNone + 1) - 1;
-    __syncthreads();
+  __device__ List(uint64_t* keys_, int n_, bool ascending_) : keys(keys_), n(n_), ascending(ascending_) {}
+  // A bar that at least n of the values in `top`, one a lane, are above.
+  __device__ void begin(uint32_t top) {
+    bar = max(nth(n, 16, [&](uint32_t c) { return int(__popcll(__ballot(top >= c))); }), kNone + 1) - 1;
   }
   __device__ void push(uint32_t order, uint32_t place) {
-    if (order > bar) s.keys[atomicAdd(&s.count, 1u)] = (uint64_t(order) << 32) | uint32_t(~place);
+    const bool in = order > bar;
+    const uint64_t mask = __ballot(in);
+    if (mask == 0) return;
+    if (in) keys[count + below_me(mask)] = (uint64_t(order) << 32) | uint32_t(~place);
+    count += __popcll(mask);
   }
-  // Before a block of `most` values: room for them.  (Ends with a barrier.)
-  __device__ void room(int most) {
-    __syncthreads();
-    const int c = int(s.count);
-    __syncthreads();                                   // (nobody adds before all have read it)
-    if (c + most > kRoom) shrink();
-  }
-  __device__ void shrink() {                           // by all threads
-    uint64_t mine[kMine];
-    const int c = int(s.count);
+  // The bar up to the n-th largest of the list's values (2^-13 below it at most), and what is below it out of the list.
+  __device__ void raise() {
+    const int lane = threadIdx.x & 63, m = (count + 63) / 64;
+    uint32_t mine[kMine];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int at = int(threadIdx.x) + i * kThreads;
-      mine[i] = at < c ? s.keys[at] : 0;
+    for (int i = 0; i < kMine; ++i) mine[i] = lane + 64 * i < count ? uint32_t(keys[lane + 64 * i] >> 32) : 0;
+    const uint32_t t = nth(n, 10, [&](uint32_t c) {
+      int found = 0;
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        if (i >= m) break;
+        found += __popcll(__ballot(mine[i] >= c));
+      }
+      return found;
+    });
+    if (t > kNone) bar = max(bar, ascending ? t : t - 1);
+    keep(uint64_t(t) << 32);
+  }
+  // (in place: what is kept moves down)
+  __device__ void keep(uint64_t low) {
+    const int lane = threadIdx.x & 63;
+    int left = 0;
+#pragma unroll 1
+    for (int i0 = 0; i0 < count; i0 += 64) {
+      const uint64_t key = i0 + lane < count ? keys[i0 + lane] : 0;
+      const bool in = i0 + lane < count && key >= low;
+      const uint64_t mask = __ballot(in);
+      if (in) keys[left + below_me(mask)] = key;
+      left += __popcll(mask);
     }
-    if (c <= n) return;
-    if (threadIdx.x < 2) s.sum[threadIdx.x] = 0;
-    __syncthreads();
-    uint64_t t = 0;                                    // the n-th largest, bit by bit
+    count = seen = left;
+  }
+  // Room for the next block, which may all pass; `now`: the bar in any case.
+  __device__ void room(int most, bool now) {
+    if (!now && count <= seen + 64 && count + most <= kRoom) return;
+    raise();
+    if (count + most > kRoom) cut();
+  }
+  // Down to the n largest, where many are equal.
+  __device__ void cut() {
+    if (count <= n) return;
+    const int lane = threadIdx.x & 63;
+    uint64_t t = 0;                                    // the n-th largest key, bit by bit
+#pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
-      const uint64_t cand = t | (uint64_t(1) << bit);
-      uint32_t found = 0;
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) found += __popcll(__ballot(mine[i] >= cand));
-      if ((threadIdx.x & 63) == 0) atomicAdd(&s.sum[bit & 1], found);
-      __syncthreads();
-      if (int(s.sum[bit & 1]) >= n) t = cand;
-      if (threadIdx.x == 0) s.sum[(bit & 1) ^ 1] = 0;
-      __syncthreads();
+      const uint64_t c = t | (uint64_t(1) << bit);
+      int found = 0;
+#pragma unroll 1
+      for (int i0 = 0; i0 < count; i0 += 64) found += __popcll(__ballot(i0 + lane < count && keys[i0 + lane] >= c));
+      if (found >= n) t = c;
     }
-    if (threadIdx.x == 0) s.count = 0;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-      if (mine[i] >= t) s.keys[atomicAdd(&s.count, 1u)] = mine[i];
-    // what equals the last one has a higher place if it comes later, or may have a lower one
+    keep(t);
     bar = max(bar, uint32_t(t >> 32) - (ascending ? 0u : 1u));
-    __syncthreads();
-  }
-  // s.out[0 .. n): the largest, in order, 0 behind the last.  (Ends with a barrier.)
-  __device__ void finish() {
-    __syncthreads();
-    if (s.count > 2 * kThreads) shrink();
-    const int c = int(s.count);
-    for (int i = threadIdx.x; i < n; i += kThreads)
-      if (i >= c) s.out[i] = 0;
-    for (int i = threadIdx.x; i < c; i += kThreads) {
-      const uint64_t mine = s.keys[i];
-      int rank = 0;
-      for (int k = 0; k < c; ++k) rank += s.keys[k] > mine;
-      if (rank < n) s.out[rank] = mine;
-    }
-    __syncthreads();
   }
 };
+
+// The lists of a workgroup's waves as one: s.out[0 .. n), in order, 0 behind the last.  By all threads; ends with a barrier.
+struct Shared {
+  uint64_t keys[kWaves][kRoom];
+  uint64_t out[kMaxSelect];
+  uint32_t low[kWaves];
+  int count[kWaves];
+};
+__device__ inline void join(Shared& s, List& list) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  // what is below any wave's n-th largest is left out
+  if (lane == 0) s.low[wave] = list.bar;
+  __syncthreads();
+  const uint32_t low = max(max(s.low[0], s.low[1]), max(s.low[2], s.low[3]));
+  uint64_t* const keys = s.keys[wave];
+  list.keep(uint64_t(low) << 32);                      // (a list's own n-th may equal its bar)
+  if (list.count > kFew) list.cut();
+  if (lane == 0) s.count[wave] = list.count;
+  for (int i = threadIdx.x; i < list.n; i += kThreads) s.out[i] = 0;
+  __syncthreads();
+  for (int i = lane; i < list.count; i += 64) {
+    const uint64_t mine = keys[i];
+    int rank = 0;
+#pragma unroll 1
+    for (int w = 0; w < kWaves; ++w) {
+      const int c = s.count[w];
+#pragma unroll 4
+      for (int k = 0; k < c; ++k) rank += s.keys[w][k] > mine;
+    }
+    if (rank < list.n) s.out[rank] = mine;
+  }
+  __syncthreads();
+}
 
 // A row's logits in vectors of 16 bytes, counted from its first element wherever that lies: rows that are alike are
 // taken apart alike, and their sums are the same bits.
@@ -159,14 +194,17 @@ struct Logits {
       __builtin_memcpy(&u, row + int64_t(t) * kSize, 16);   // (one load: any alignment will do)
       return u;
     }
-    uint32_t w[4] = {0, 0, 0, 0};
+    uint32_t b[kE], w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {                     // (all of them in flight, the row's last one in the place of those it lacks)
+      const int at = min(t + e, vocab - 1);
+      b[e] = kSize == 2 ? uint32_t(reinterpret_cast<const uint16_t*>(row)[at]) : reinterpret_cast<const uint32_t*>(row)[at];
+    }
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
-      uint32_t b = TYPE == UFS_BF16 ? 0xff80u : TYPE == UFS_FP16 ? 0xfc00u : 0xff800000u;
-      if (t + e < vocab)
-        b = kSize == 2 ? uint32_t(reinterpret_cast<const uint16_t*>(row)[t + e]) : reinterpret_cast<const uint32_t*>(row)[t + e];
-      if (kSize == 2) w[e / 2] |= b << (16 * (e & 1));
-      else w[e] = b;
+      if (t + e >= vocab) b[e] = TYPE == UFS_BF16 ? 0xff80u : TYPE == UFS_FP16 ? 0xfc00u : 0xff800000u;
+      if (kSize == 2) w[e / 2] |= b[e] << (16 * (e & 1));
+      else w[e] = b[e];
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
@@ -177,64 +215,75 @@ struct Logits {
   }
 };
 
-// A slice's results: its maximum and sum of exponentials, then its list.
-__device__ __host__ inline size_t slice_bytes(int k) { return 16 + size_t(k + 1) * 8; }
-struct Slice {
-  float top, sum;
-  uint64_t unused;
-};
-
+// A slice's results: its maximum and sum of exponentials, then its list of k + 1 (lanes bound a list to 64).
+__device__ __host__ inline int listed_of(int k) { return k + 1 < 64 ? k + 1 : 64; }
+__device__ __host__ inline size_t slice_bytes(int k) { return 16 + size_t(listed_of(k)) * 8; }
 __device__ inline bool in_use(const SelectArgs& a, int row) { return a.scores[row] > -INFINITY; }
 
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
   using L = Logits<TYPE>;
   constexpr int kE = L::kE;
+  constexpr int kVectors = kEach / kE;                 // of a lane and block
   __shared__ Shared s;
-  __shared__ float stop[4];
-  __shared__ double ssum[4];
+  __shared__ float stop[kWaves];
+  __shared__ double ssum[kWaves];
   const int row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
   if (!in_use(a, row) || (a.done != nullptr && a.done[row] != 0)) return;
   const L x(a, row % a.beams, row / a.beams);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int v0 = split * a.slice, v1 = min(v0 + a.slice, (a.vocab + kE - 1) / kE);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // the waves take the slice's blocks in turn
+  const int v1 = min((split + 1) * a.slice, (a.vocab + kE - 1) / kE), step = kWaves * 64 * kVectors;
+  const int v0 = split * a.slice + wave * 64 * kVectors;
 
-  Best best(s, a.k + 1, true);
+  List list(s.keys[wave], listed_of(a.k), true);
   float top = -INFINITY, sum = 0.f;
-  uint4 next[kVectors];
-  auto fetch = [&](int v) {
+  uint4 next[2][kVectors];                             // two blocks ahead
+  auto fetch = [&](uint4 (&to)[kVectors], int v) {
 #pragma unroll
-    for (int u = 0; u < kVectors; ++u) next[u] = x.bits(v + u * kThreads + tid < v1 ? v + u * kThreads + tid : (1 << 27));
+    for (int u = 0; u < kVectors; ++u) to[u] = x.bits(v + 64 * u + lane < v1 ? v + 64 * u + lane : (1 << 27));
   };
-  fetch(v0);
-  for (int v = v0; v < v1; v += kThreads * kVectors) {
+  auto block = [&](const uint4 (&bits)[kVectors], int v) {
     float y[kVectors][kE];
 #pragma unroll
-    for (int u = 0; u < kVectors; ++u) L::unpack(next[u], y[u]);
-    if (v + kThreads * kVectors < v1) fetch(v + kThreads * kVectors);
+    for (int u = 0; u < kVectors; ++u) L::unpack(bits[u], y[u]);
     float most = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kVectors; ++u)
 #pragma unroll
       for (int e = 0; e < kE; ++e) most = fmaxf(most, y[u][e]);
     if (most > top) {
-      sum *= __builtin_amdgcn_exp2f((top - most) * 1.44269504f);
+      sum *= __builtin_amdgcn_exp2f((top - most) * kLog2e);
       top = most;
     }
     const float off = top > -INFINITY ? top : 0.f;
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < kVectors; ++u)
 #pragma unroll
-      for (int e = 0; e < kE; ++e) sum += __builtin_amdgcn_exp2f((y[u][e] - off) * 1.44269504f);
-    const uint32_t order = ordered(most);
-    if (v == v0) best.set_bar(order);
-    else best.room(kThreads * kVectors * kE);
-    if (order > best.bar) {
+      for (int e = 0; e < kE; ++e) part[e & 3] += __builtin_amdgcn_exp2f((y[u][e] - off) * kLog2e);
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
+    if (v == v0) list.begin(ordered(most));
+    // the bar as a value: -inf where all pass; the place between 0 and the largest value below it is no other value's
+    const float bar = value_of(list.bar == 0x7fffffffu ? 0x7ffffffeu : list.bar);
+    if (__ballot(most > bar) != 0) {
 #pragma unroll
       for (int u = 0; u < kVectors; ++u)
 #pragma unroll
-        for (int e = 0; e < kE; ++e) best.push(ordered(y[u][e]), uint32_t((v + u * kThreads + tid) * kE + e));
+        for (int e = 0; e < kE; ++e)
+          if (__ballot(y[u][e] > bar) != 0) list.push(ordered(y[u][e]), uint32_t((v + 64 * u + lane) * kE + e));
     }
+    list.room(kBlock, v + step >= v1 && list.count > max(2 * list.n, 24));
+  };
+  fetch(next[0], v0);
+  fetch(next[1], v0 + step);
+#pragma unroll 1
+  for (int v = v0; v < v1; v += step) {
+    uint4 now[kVectors];
+#pragma unroll
+    for (int u = 0; u < kVectors; ++u) now[u] = next[0][u], next[0][u] = next[1][u];
+    if (v + 2 * step < v1) fetch(next[1], v + 2 * step);
+    block(now, v);
   }
   // the slice's maximum and sum
   float all = top;
@@ -243,17 +292,14 @@ __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
   if (lane == 0) stop[wave] = all;
   __syncthreads();
   all = fmaxf(fmaxf(stop[0], stop[1]), fmaxf(stop[2], stop[3]));
-  double part = sum != 0.f ? double(sum) * exp(double(top) - double(all)) : 0.0;
+  float part = sum != 0.f ? sum * __builtin_amdgcn_exp2f((top - all) * kLog2e) : 0.f;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) part += __shfl_xor(part, d);
-  if (lane == 0) ssum[wave] = part;
-  best.finish();
+  if (lane == 0) ssum[wave] = double(part);
+  join(s, list);
   uint8_t* const to = a.work + size_t(blockIdx.x) * slice_bytes(a.k);
-  if (tid == 0) {
-    reinterpret_cast<float*>(to)[0] = all;
-    reinterpret_cast<float*>(to)[1] = float(ssum[0] + ssum[1] + (ssum[2] + ssum[3]));
-  }
-  if (tid <= a.k) reinterpret_cast<uint64_t*>(to + 16)[tid] = s.out[tid];
+  if (tid == 0) *reinterpret_cast<float2*>(to) = make_float2(all, float((ssum[0] + ssum[1]) + (ssum[2] + ssum[3])));
+  if (tid < list.n) reinterpret_cast<uint64_t*>(to + 16)[tid] = s.out[tid];
 }
 
 template <int TYPE>
@@ -263,89 +309,113 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
   __shared__ Shared s;
   __shared__ float slse[kMaxBeams], sscore[kMaxBeams];
   __shared__ uint8_t skind[kMaxBeams];                 // 0: not in use, 1: goes on, 2: finished
-  __shared__ int sagain;
-  const int g = blockIdx.x, W = a.beams, tid = threadIdx.x;
+  const int g = blockIdx.x, W = a.beams, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint8_t* const work = a.work + size_t(g) * W * a.splits * slice_bytes(a.k);
   auto slice_at = [&](int i) { return work + size_t(i) * slice_bytes(a.k); };
-  for (int w = tid; w < W; w += kThreads) {
-    const float score = a.scores[g * W + w];
+  const int n = listed_of(a.k), slices = W * a.splits, listed = slices * n;
+
+  // the first of this thread's entries of the lists come while the sums are joined
+  constexpr int kHeld = 4;
+  uint64_t held[kHeld];
+  auto entry = [&](int i) { return i < listed ? reinterpret_cast<const uint64_t*>(slice_at(i / n) + 16)[i % n] : 0; };
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = entry(tid + i * kThreads);
+  if (tid < W) {
+    const float score = a.scores[g * W + tid];
     int kind = score > -INFINITY ? 1 : 0;
-    if (a.done != nullptr && a.done[g * W + w] != 0) kind *= 2;
+    if (a.done != nullptr && a.done[g * W + tid] != 0) kind *= 2;
     float lse = 0.f;
     if (kind == 1) {
       float top = -INFINITY;
-      for (int i = 0; i < a.splits; ++i) top = fmaxf(top, *reinterpret_cast<const float*>(slice_at(w * a.splits + i)));
+      for (int i = 0; i < a.splits; ++i) top = fmaxf(top, *reinterpret_cast<const float*>(slice_at(tid * a.splits + i)));
       double sum = 0.0;
       for (int i = 0; i < a.splits; ++i) {
-        const float2 t = *reinterpret_cast<const float2*>(slice_at(w * a.splits + i));
-        sum += t.y != 0.f ? double(t.y) * exp(double(t.x) - double(top)) : 0.0;
+        const float2 t = *reinterpret_cast<const float2*>(slice_at(tid * a.splits + i));
+        sum += t.y != 0.f ? double(t.y * __builtin_amdgcn_exp2f((t.x - top) * kLog2e)) : 0.0;
       }
       lse = float(double(top) + log(sum));
     }
-    slse[w] = lse;
-    sscore[w] = score;
-    skind[w] = uint8_t(kind);
+    slse[tid] = lse;
+    sscore[tid] = score;
+    skind[tid] = uint8_t(kind);
   }
   __syncthreads();
   auto score_of = [&](int w, float logit) { return sscore[w] + (logit - slse[w]); };   // (float32 each)
-  // NaN is no candidate
-  auto order_of = [&](float score) { return score > -INFINITY ? ordered(score) : 0u; };
+  auto order_of = [&](float score) { return score > -INFINITY ? ordered(score) : 0u; };   // NaN is no candidate
+  // Whether a slice has to be read again where `limit` is the score that decides.
+  auto again = [&](int i, uint32_t limit) {
+    const int w = i / a.splits;
+    if (skind[w] != 1) return false;
+    const uint64_t last = reinterpret_cast<const uint64_t*>(slice_at(i) + 16)[n - 1];
+    if (uint32_t(last >> 32) <= kNone) return false;   // (it has fewer: none was left out)
+    const float x = value_of(uint32_t(last >> 32)), score = score_of(w, x);
+    return order_of(score) > kNone && order_of(score) >= limit && score_of(w, L::below(x)) == score;
+  };
+  // Entry i of the lists as a candidate: its score, and its place.
+  auto candidate = [&](int i, uint64_t key, uint32_t* place) {
+    const int w = i / n / a.splits;
+    if (i >= listed || skind[w] != 1 || uint32_t(key >> 32) <= kNone) return 0u;
+    *place = uint32_t(w) * uint32_t(a.vocab) + uint32_t(~uint32_t(key));
+    return order_of(score_of(w, value_of(uint32_t(key >> 32))));
+  };
+  auto finished = [&](List& list) {
+    if (wave == 0) {
+      list.room(64, false);
+      const bool ends = lane < W && skind[lane] == 2;
+      list.push(ends ? order_of(sscore[lane]) : 0u, uint32_t(lane) * uint32_t(a.vocab) + uint32_t(a.end));
+    }
+  };
 
-  // first by the slices' lists; then, where some have to be read again, by those slices' scores and the others' lists
-  const int listed = W * a.splits * (a.k + 1);
-  for (int pass = 0; pass < 2; ++pass) {
-    Best best(s, a.k, false);
-    const uint32_t limit = pass == 0 ? 0u : uint32_t(s.out[a.k - 1] >> 32);   // the score that decides
-    auto again = [&](int i) {                          // whether slice i has to be read again
-      const int w = i / a.splits;
-      if (skind[w] != 1) return false;
-      const uint64_t last = reinterpret_cast<const uint64_t*>(slice_at(i) + 16)[a.k];
-      if (uint32_t(last >> 32) <= kNone) return false;   // (it has fewer: none was left out)
-      const float x = value_of(uint32_t(last >> 32)), score = score_of(w, x);
-      return order_of(score) > kNone && order_of(score) >= limit && score_of(w, L::below(x)) == score;
-    };
-    if (pass == 1) {
-      if (tid == 0) sagain = 0;
-      __syncthreads();
-      for (int i = tid; i < W * a.splits; i += kThreads)
-        if (again(i)) sagain = 1;
-      __syncthreads();
-      if (sagain == 0) break;
-    }
-    auto candidate = [&](int i, uint32_t* place) {      // entry i of the lists
-      const int slice = i / (a.k + 1), w = slice / a.splits;
-      if (i >= listed || skind[w] != 1) return 0u;
-      const uint64_t key = reinterpret_cast<const uint64_t*>(slice_at(slice) + 16)[i - slice * (a.k + 1)];
-      if (uint32_t(key >> 32) <= kNone || (pass == 1 && again(slice))) return 0u;
-      *place = uint32_t(w) * uint32_t(a.vocab) + uint32_t(~uint32_t(key));
-      return order_of(score_of(w, value_of(uint32_t(key >> 32))));
-    };
-    uint32_t top = 0, place = 0;
-    for (int i = tid; i < listed; i += kThreads) top = max(top, candidate(i, &place));
-    best.set_bar(top);
-    for (int i0 = 0; i0 < listed; i0 += kThreads) {
-      const uint32_t order = candidate(i0 + tid, &place);
-      best.room(kThreads);
-      best.push(order, place);
-    }
-    best.room(kThreads);
-    if (tid < W && skind[tid] == 2) best.push(order_of(sscore[tid]), uint32_t(tid) * uint32_t(a.vocab) + uint32_t(a.end));
-    if (pass == 1)
-      for (int i = 0; i < W * a.splits; ++i) {
-        if (!again(i)) continue;
-        const int w = i / a.splits;
-        const L x(a, w, g);
-        const int v0 = (i % a.splits) * a.slice, v1 = min(v0 + a.slice, (a.vocab + kE - 1) / kE);
-        for (int v = v0; v < v1; v += kThreads) {
-          float y[kE];
-          L::unpack(x.bits(v + tid < v1 ? v + tid : (1 << 27)), y);
-          best.room(kThreads * kE);
+  {
+    List list(s.keys[wave], a.k, false);
+    uint32_t place = 0, order[kHeld], places[kHeld], top = 0;
 #pragma unroll
-          for (int e = 0; e < kE; ++e)
-            best.push(order_of(score_of(w, y[e])), uint32_t(w) * uint32_t(a.vocab) + uint32_t((v + tid) * kE + e));
-        }
+    for (int i = 0; i < kHeld; ++i) {
+      order[i] = candidate(tid + i * kThreads, held[i], &places[i]);
+      top = max(top, order[i]);
+    }
+    list.begin(top);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) list.push(order[i], places[i]);
+    for (int i0 = kHeld * kThreads; i0 < listed; i0 += kThreads) {
+      const uint32_t o = candidate(i0 + tid, entry(i0 + tid), &place);
+      list.room(64, false);
+      list.push(o, place);
+    }
+    finished(list);
+    list.raise();
+    join(s, list);
+  }
+  const uint32_t limit = uint32_t(s.out[a.k - 1] >> 32);
+  int reads = 0;
+  for (int i = tid; i < slices; i += kThreads) reads |= again(i, limit);
+  if (__syncthreads_or(reads)) {                       // those slices by their scores, and the others' lists
+    List list(s.keys[wave], a.k, false);
+    for (int i0 = 0; i0 < listed; i0 += kThreads) {
+      const int i = i0 + tid;
+      uint32_t place = 0, o = candidate(i, entry(i), &place);
+      if (o != 0 && again(i / n, limit)) o = 0;
+      list.room(64, false);
+      list.push(o, place);
+    }
+    finished(list);
+    for (int i = 0; i < slices; ++i) {
+      if (!again(i, limit)) continue;
+      const int w = i / a.splits;
+      const L x(a, w, g);
+      const int v1 = min((i % a.splits + 1) * a.slice, (a.vocab + kE - 1) / kE);
+      for (int v = (i % a.splits) * a.slice + wave * 64; v < v1; v += kThreads) {
+        float y[kE];
+        L::unpack(x.bits(v + lane < v1 ? v + lane : (1 << 27)), y);
+        list.room(64 * kE, false);
+#pragma unroll
+        for (int e = 0; e < kE; ++e)
+          list.push(order_of(score_of(w, y[e])), uint32_t(w) * uint32_t(a.vocab) + uint32_t((v + lane) * kE + e));
       }
-    best.finish();
+    }
+    list.raise();
+    __syncthreads();
+    join(s, list);
   }
   if (tid < a.k) {
     const uint64_t key = s.out[tid];
@@ -369,7 +439,7 @@ hipError_t run(const SelectArgs& a, hipStream_t stream) {
 }  // namespace
 
 void plan_select(SelectArgs* a) {
-  const int e = a->type == UFS_FP32 ? 4 : 8, block = kThreads * kVectors;
+  const int e = a->type == UFS_FP32 ? 4 : 8, block = kWaves * kBlock / e;
   const int64_t vectors = (int64_t(a->vocab) + e - 1) / e, rows = int64_t(a->groups) * a->beams;
   const int64_t blocks = (vectors + block - 1) / block;
   const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({blocks, 32, (1024 + rows - 1) / rows}));
