@@ -85,7 +85,23 @@ __device__ inline void stay() { asm volatile("" ::: "memory"); }
 // Sign bits of the halves that are not finite (junk in the others).
 __device__ inline uint32_t odd_halves(uint32_t u) { return (u & 0x7f807f80u) + 0x00800080u; }
 
-__device__ inline double power(double g, int e) { return e == 0 ? 1.0 : exp(g * double(e)); }
+// Powers of L: squares of exp(g), and the product of those that an exponent is made of.
+template <int BITS>
+struct Powers {
+  double square[BITS];
+  __device__ explicit Powers(double g) {
+    square[0] = exp(g);
+#pragma unroll
+    for (int i = 1; i < BITS; ++i) square[i] = square[i - 1] * square[i - 1];
+  }
+  __device__ double operator()(int e) const {
+    double x = 1.0;
+#pragma unroll
+    for (int i = 0; i < BITS; ++i)
+      if ((e >> i) & 1) x *= square[i];
+    return x;
+  }
+};
 
 // OUT: results are wanted, not M alone: a part's own M is summed against the walk, so that what is read last is what the
 // walk reads first, with a factor for each chunk in the place of M's.  begin: M where the walk begins, or null; last: where
@@ -149,18 +165,33 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     issue(1);
   }
 
+  // M: y-dim 32 mt + 16 (r / 8) + 8 hl + r % 8, z-dim 32 wave + ln
+  f32x16 S[4];
+  const int zd = 32 * wave + ln;
+#pragma unroll
+  for (int mt = 0; mt < 4; ++mt) S[mt] = f32x16{};
+  if (begin != nullptr) {
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int yd = 32 * mt + 16 * (r >> 3) + 8 * hl + (r & 7);
+        S[mt][r] = trans ? begin[zd * kD + yd] : begin[yd * kD + zd];
+      }
+  }
+
   // weights
   float* const tab = reinterpret_cast<float*>(smem + kTable);
-  const double gd = double(geo.decay[h]);
+  const Powers<6> power(double(geo.decay[h]));
   const float scale = geo.scale;
-  if (tid < 33) tab[tid] = float(power(gd, tid));
+  if (tid < 33) tab[tid] = float(power(tid));
   if (tid >= 64 && tid < 128) {
     const int j = tid & 31, n = tid < 96 ? kChunk : rest;
-    tab[kPowers + tid - 64] = j >= n ? 0.f : BACK ? scale * float(power(gd, j + 1)) : float(power(gd, n - 1 - j));
+    tab[kPowers + tid - 64] = j >= n ? 0.f : BACK ? scale * float(power(j + 1)) : float(power(n - 1 - j));
   }
-  const double dw = power(gd, kChunk);
-  const float whole_hi = float(dw), whole_lo = float(dw - double(whole_hi)), rest_dec = float(power(gd, max(rest, 0)));
-  __syncthreads();
+  const double dw = power.square[5];
+  const float whole_hi = float(dw), whole_lo = float(dw - double(whole_hi)), rest_dec = float(power(max(rest, 0)));
+  meet_lds();                                          // (M and the first copies are on their way)
   // P: this wave's quarter, x_t.y_j for j = pj .. pj + 3 and t = pt
   const int pq = lane >> 4, pj = 16 * (wave >> 1) + 4 * pq, pt = 16 * (wave & 1) + rp;
   float pw[4];
@@ -197,21 +228,6 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   const uint32_t pput = lds0 + kP + uint32_t(pt) * kRow + 2 * (16 * (wave >> 1) + 4 * (2 * (pq & 1) + (pq >> 1)));
   const uint32_t pget = lds0 + kP + uint32_t(ln) * kRow + 16 * hl;
   const uint32_t kwt = lds0 + kTable + 4 * (kPowers + 4 * hl);
-
-  // M: y-dim 32 mt + 16 (r / 8) + 8 hl + r % 8, z-dim 32 wave + ln
-  f32x16 S[4];
-  const int zd = 32 * wave + ln;
-#pragma unroll
-  for (int mt = 0; mt < 4; ++mt) S[mt] = f32x16{};
-  if (begin != nullptr) {
-#pragma unroll
-    for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int yd = 32 * mt + 16 * (r >> 3) + 8 * hl + (r & 7);
-        S[mt][r] = trans ? begin[zd * kD + yd] : begin[yd * kD + zd];
-      }
-  }
 
   f32x16 os = f32x16{}, op = f32x16{};                  // O^T: of M, without the row's weight, and of P
   const int out_heads = geo.kv_heads * (BACK ? 1 : G);
@@ -533,13 +549,13 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(PartArgs a) {
     if (first < 0 || first + p.parts > geo.parts) return;
   }
   const int chunks = geo.step == nullptr ? geo.chunks : max(1, ((const const_i32*)geo.step)[3]);
-  const double gd = double(geo.decay[h]);
+  const Powers<31> power(double(geo.decay[h]));
   const int at = slice * 1024 + threadIdx.x * 4;
   float4 m = make_float4(0.f, 0.f, 0.f, 0.f);
   if (s.first != nullptr && p.held)
     m = *reinterpret_cast<const float4*>(s.first + (size_t(p.seq) * geo.kv_heads + h) * kState + at);
   const int tail = p.tokens - (p.parts - 1) * chunks * kChunk;
-  const double whole = power(gd, chunks * kChunk), part = power(gd, max(tail, 0));
+  const double whole = power(chunks * kChunk), part = power(max(tail, 0));
   auto slot = [&](int i) {
     const int q = s.back ? p.parts - 1 - i : i;
     return reinterpret_cast<float4*>(s.starts + (size_t(first + q) * geo.kv_heads + h) * kState + at);

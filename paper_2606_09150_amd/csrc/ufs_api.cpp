@@ -60,12 +60,30 @@ int check_work(const void* work, size_t bytes, size_t need) {
   return UF_OK;
 }
 
-// Chunks of a part, for sequences of so many chunks in all and the longest of them, and key heads: a launch should have
-// two workgroups for each of 256 CUs, and a part should outlast the 128 KB that its state's way through memory costs.
-int32_t part_chunks(int64_t all, int64_t longest, int64_t heads) {
-  const int64_t groups = 512, least = 8;
-  const int64_t want = (all * heads + groups - 1) / groups;
-  return int32_t(std::max<int64_t>(1, std::min(longest, std::max(want, least))));
+// Chunks of a part: of n sequences with `all` chunks, the longest with `longest`, of `heads` key heads each; `walks` 1, or
+// the backward's 3 beside two sums.  Parts are walked side by side, and pay with a sum of each, two launches and their states'
+// way through memory.  The time of either is estimated from what these launches took (us; c chunks a part, P parts of
+// a sequence, W workgroups): walks 2.0 c on a CU of their own (W up to 160), 2.8 c where W = 256, 5.1 c at 512, the backward's 1.9 c
+// and W c / 136; sums 0.9 c, and 2.05 c at 512; the states carried on 0.36 P, or 13 us for 512 of them.  Whole / in parts
+// of 2 / 4 / 8 chunks: 1 x 256 tokens, 16 heads, 20 / 20.5 / 24 / -, backward 20 / 31 / 32 / -; 1 x 1,024 68 / 29 / 30 / 37, backward
+// 66 / 61 / 48 / 47.  1 x 16,384 tokens, 32 heads, in 8 / 16 parts 231 / 216, backward 486 / 514.
+int32_t part_chunks(int64_t all, int64_t longest, int64_t n, int64_t heads, int walks) {
+  const int sums = walks > 1 ? 2 : 1;
+  auto time = [&](int64_t c) {
+    const double parts = double((longest + c - 1) / c);
+    const double groups = double(heads) * (c < longest ? std::ceil(double(all) / double(c)) + 0.5 * double(n - 1) : double(n));
+    // rounds of two workgroups a CU, and what is left
+    const double all_walks = walks * groups, whole = std::floor(all_walks / 512.0), rest = all_walks - 512.0 * whole;
+    const double walk = double(c) * (walks > 1 ? std::max(1.9, all_walks / 136.0)
+                                               : whole * 5.05 + (rest > 0.0 ? std::max(2.0, 0.6 + rest / 115.0) : 0.0));
+    if (c >= longest) return 4.0 + walk;
+    return (walks > 1 ? 18.0 : 13.0) + walk + double(c) * std::max(0.9, sums * groups / (walks > 1 ? 290.0 : 250.0)) +
+           sums * std::max(0.36 * parts, 0.026 * groups);
+  };
+  int64_t best = std::max<int64_t>(longest, 1);
+  for (int64_t c = 1; c < longest; c += std::max<int64_t>(1, c / 8))
+    if (time(c) < time(best)) best = c;
+  return int32_t(best);
 }
 
 lin::Src src(const void* p, const uft_stride& s) { return lin::Src{static_cast<const uint16_t*>(p), s.batch, s.token, s.head}; }
@@ -76,7 +94,7 @@ lin::Src src(const void* p, const uft_stride& s) { return lin::Src{static_cast<c
 
 namespace {
 
-int check_linear(const ufs_linear_desc* d, lin::Geo* g) {
+int check_linear(const ufs_linear_desc* d, int walks, lin::Geo* g) {
   if (d == nullptr) return fail(UF_ERR_ARG, "desc is null");
   if (d->batch < 1 || d->tokens < 1 || d->q_heads < 1 || d->kv_heads < 1)
     return fail(UF_ERR_ARG, "batch, tokens and heads must be >= 1");
@@ -98,7 +116,7 @@ int check_linear(const ufs_linear_desc* d, lin::Geo* g) {
   const int64_t chunks = (int64_t(d->tokens) + lin::kChunk - 1) / lin::kChunk;
   const double units = double(d->batch) * d->kv_heads;
   if (units * 8 * 2 > kMostGroups) return fail(UF_ERR_ARG, "shape too large: batch * kv_heads");
-  g->chunks = part_chunks(chunks * d->batch, chunks, d->kv_heads);
+  g->chunks = part_chunks(chunks * d->batch, chunks, d->batch, d->kv_heads, walks);
   g->parts = int32_t((chunks + g->chunks - 1) / g->chunks);
   if ((units * g->parts + 8) * 3 > kMostGroups || double(chunks) * g->group > 2.0e9)
     return fail(UF_ERR_ARG, "shape too large: batch * q_heads * tokens");
@@ -117,7 +135,7 @@ extern "C" {
 int ufs_linear_work_bytes(const ufs_linear_desc* d, size_t* bytes) {
   return guarded([&]() -> int {
     lin::Geo g;
-    if (int s = check_linear(d, &g)) return s;
+    if (int s = check_linear(d, 1, &g)) return s;
     if (bytes == nullptr) return fail(UF_ERR_ARG, "bytes is null");
     *bytes = starts_bytes(g);
     return ok();
@@ -127,7 +145,7 @@ int ufs_linear_work_bytes(const ufs_linear_desc* d, size_t* bytes) {
 int ufs_linear_bwd_work_bytes(const ufs_linear_desc* d, size_t* bytes) {
   return guarded([&]() -> int {
     lin::Geo g;
-    if (int s = check_linear(d, &g)) return s;
+    if (int s = check_linear(d, 3, &g)) return s;
     if (bytes == nullptr) return fail(UF_ERR_ARG, "bytes is null");
     *bytes = 2 * starts_bytes(g);
     return ok();
@@ -139,7 +157,7 @@ int ufs_linear_fwd(const ufs_linear_desc* d, const void* d_q, const void* d_k, c
                    size_t work_bytes, void* stream) {
   return guarded([&]() -> int {
     lin::WalkArgs a{};
-    if (int s = check_linear(d, &a.geo)) return s;
+    if (int s = check_linear(d, 1, &a.geo)) return s;
     for (const void* p : {d_q, d_k, d_v, static_cast<const void*>(d_o)}) {
       if (p == nullptr) return fail(UF_ERR_ARG, "q, k, v or o is null");
       if (!aligned(p, 16)) return fail(UF_ERR_ARG, "q, k, v and o must be 16-byte aligned");
@@ -175,7 +193,7 @@ int ufs_linear_bwd(const ufs_linear_desc* d, const void* d_q, const void* d_k, c
                    void* d_dq, void* d_dk, void* d_dv, float* d_dstate, void* d_work, size_t work_bytes, void* stream) {
   return guarded([&]() -> int {
     lin::WalkArgs a{};
-    if (int s = check_linear(d, &a.geo)) return s;
+    if (int s = check_linear(d, 3, &a.geo)) return s;
     for (const void* p : {d_q, d_k, d_v, d_do, static_cast<const void*>(d_dq), static_cast<const void*>(d_dk),
                           static_cast<const void*>(d_dv)}) {
       if (p == nullptr) return fail(UF_ERR_ARG, "a tensor is null");
@@ -364,7 +382,7 @@ int ufs_extend(ufs_cache* c, int32_t n, const int32_t* seqs, const int32_t* coun
       longest = std::max(longest, counts[i]);
     }
     if (total > (1 << 30)) return fail(UF_ERR_ARG, "more than 2^30 new tokens");
-    const int32_t part = part_chunks(chunks, (int64_t(longest) + lin::kChunk - 1) / lin::kChunk, c->d.kv_heads);
+    const int32_t part = part_chunks(chunks, (int64_t(longest) + lin::kChunk - 1) / lin::kChunk, n, c->d.kv_heads, 1);
     std::vector<Entry> step;
     std::vector<int32_t> words = {n, int32_t(total), 0, part};
     step.reserve(size_t(n));

@@ -120,6 +120,14 @@ class StateCache:
             self.table = torch.empty(S.ufs_table_bytes(self.desc), dtype=torch.uint8, device=self.device)
         self.handle = S.ufs_create(self.desc, self.pool, self.table)
         self._step = self._need = None
+        self._dense = {}
+
+    def _of(self, heads):
+        """The strides of contiguous [tokens, heads, 128]."""
+        got = self._dense.get(heads)
+        if got is None:
+            got = self._dense[heads] = S.uft_stride(0, heads * D, D)
+        return got
 
     def close(self):
         if getattr(self, "handle", None) is not None:
@@ -157,8 +165,9 @@ class StateCache:
     # -- sequences --------------------------------------------------------------
     def extend(self, seqs, counts, stream=None):
         """Begin a step: sequence seqs[i] grows by counts[i] tokens."""
+        counts = S.ints(counts)
         self._run(stream, lambda s: S.ufs_extend(self.handle, seqs, counts, s))
-        self._step = self._need = None
+        self._step, self._need = sum(counts), None
 
     def fork(self, src, dst, stream=None):
         """Sequences dst[i], empty before, continue src[i]: their states are copied."""
@@ -211,9 +220,10 @@ class StateCache:
         _dense(decay, "decay", (Hk,), torch.float32, self.device)
         if out is not None:
             _dense(out, "out", (n, Hq, D), device=self.device)
-        desc = S.ufs_attn_desc(Hq, scale, _strides(q, "q"), _strides(k, "k"), _strides(v, "v"))
-        need = self.work_bytes()
-        _work(work, need, self.device)
+        desc = S.ufs_attn_desc(Hq, scale, _strides(q, "q", self._of(Hq)), _strides(k, "k", self._of(Hk)), _strides(v, "v", self._of(Hk)))
+        need = self._need if self._need is not None else self.work_bytes()
+        if work is not None:
+            _work(work, need, self.device)
 
         def call(s):
             o = torch.empty((n, Hq, D), dtype=torch.bfloat16, device=self.device) if out is None else out

@@ -85,10 +85,13 @@ WHOLE = [
     (1, 33, 3, 1, None, False),
     (2, 64, 1, 3, [64, 33], False),
     (1, 97, 2, 5, None, True),
-    (2, 300, 2, 1, [300, 256], False),               # two parts: the second of one sequence is empty
+    (2, 300, 2, 1, [300, 256], False),
     (3, 515, 1, 2, [515, 1, 257], True),
-    (1, 1100, 7, 1, None, True),                     # every decay; five parts
+    (1, 1100, 7, 1, None, True),                     # every decay
     (2, 800, 1, 4, [0, 799], True),
+    # cut into parts both ways
+    (1, 2500, 1, 1, None, True),
+    (3, 1500, 1, 2, [1500, 37, 1409], True),
 ]
 
 
@@ -104,6 +107,9 @@ def test_whole_sequences(B, n, Hk, G, lengths, carry):
         for b, m in enumerate(lengths):
             for t in (q, k, v, do):
                 t[b, m:] = float("nan")
+    if n >= 1500:
+        desc = P.states._linear_desc(q, k, v, g, None, None)
+        assert P.states.S.ufs_linear_work_bytes(desc) and P.states.S.ufs_linear_bwd_work_bytes(desc)
     o, final = P.linear_attention(q, k, v, g, lengths=lens, state=state, final=True)
     got = P.linear_attention_bwd(q, k, v, do, g, lengths=lens, state=state, dfinal=dfinal)
     alone = P.linear_attention(q, k, v, g, lengths=lens, state=state)
@@ -125,7 +131,7 @@ def test_whole_sequences(B, n, Hk, G, lengths, carry):
 def test_strides_scales_and_given_buffers():
     """Views of one projection [B, n, q, k, v heads, D], of transposed tensors and of one broadcast head."""
     P = require_gpu()
-    B, n, Hk, G = 2, 270, 2, 2
+    B, n, Hk, G = 2, 1270, 2, 2
     both = draw((B, n, Hk * G + 2 * Hk, D), 11)
     q, k, v = both[:, :, :Hk * G], both[:, :, Hk * G:Hk * G + Hk], both[:, :, Hk * G + Hk:]
     turned = [t.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3) for t in (q, k, v)]
@@ -134,7 +140,8 @@ def test_strides_scales_and_given_buffers():
     back = P.linear_attention_bwd(q.contiguous(), k.contiguous(), v.contiguous(), do, g, scale=-0.3)
     for a in ((q, k, v), turned):
         out, last = torch.empty_like(want[0]), torch.empty_like(want[1])
-        need = P.states.S.ufs_linear_bwd_work_bytes(P.states._linear_desc(*a, g, None, None))
+        desc = P.states._linear_desc(*a, g, None, None)
+        need = max(P.states.S.ufs_linear_work_bytes(desc), P.states.S.ufs_linear_bwd_work_bytes(desc))
         work = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
         got = P.linear_attention(*a, g, scale=-0.3, final=last, out=out, work=work)
         assert got[0] is out and got[1] is last
