@@ -48,10 +48,11 @@ using tok::swz_k;
 constexpr uint32_t kTile = 8192, kHalf = 4096, kStage = 3 * kTile;
 constexpr int kStages = 3;
 // LDS behind the stages: P, a row of 32 values in two parts (and 16 bytes, so that rows begin in banks of their own) for each
-// token; then, in floats, L^e for e = 0 .. 32, and the key weights of a whole chunk and of the last one.
+// token; then, in floats, L^e for e = 0 .. 32, the key weights of a period's chunks and of the last one, and what M is read with.
 constexpr uint32_t kRow = 144, kP = kStages * kStage, kTable = kP + kChunk * kRow;
 constexpr int kPowers = 36;
-constexpr uint32_t kShared = kTable + 4 * (kPowers + 2 * kChunk);
+constexpr int kPeriod = 4, kWeights = (kPeriod + 1) * kChunk;
+constexpr uint32_t kShared = kTable + 4 * (kPowers + kWeights + kPeriod);
 static_assert(2 * kShared <= 163840, "two workgroups a CU");
 
 // x as parts of 8 bits each, the first ones cut off and the last one rounded.  (Three operations a value and part; by dot products with
@@ -170,27 +171,45 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   const int zd = 32 * wave + ln;
 #pragma unroll
   for (int mt = 0; mt < 4; ++mt) S[mt] = f32x16{};
-  if (begin != nullptr) {
+  if (begin != nullptr && trans) {
+    const float* const from = begin + zd * kD + 8 * hl;
 #pragma unroll
-    for (int mt = 0; mt < 4; ++mt)
+    for (int i = 0; i < 16; ++i) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(from + 16 * (i >> 1) + 4 * (i & 1));
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int yd = 32 * mt + 16 * (r >> 3) + 8 * hl + (r & 7);
-        S[mt][r] = trans ? begin[zd * kD + yd] : begin[yd * kD + zd];
-      }
+      for (int r = 0; r < 4; ++r) S[i >> 2][4 * (i & 3) + r] = x[r];
+    }
+  } else if (begin != nullptr) {
+    const float* const from = begin + 8 * hl * kD + zd;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) S[i >> 4][i & 15] = from[(16 * (i >> 3) + (i & 7)) * kD];
   }
 
   // weights
   float* const tab = reinterpret_cast<float*>(smem + kTable);
   const Powers<6> power(double(geo.decay[h]));
   const float scale = geo.scale;
+  // M is multiplied by L^32 not chunk by chunk, but for a period of four at once at its beginning; meanwhile it stands for the
+  // period's end: parts join it with their weights there, and it is read with L^-32 for each chunk that is to come (e^60 at
+  // most: heads that forget faster have periods of one chunk).
+  const double dw = power.square[5], dw4 = (dw * dw) * (dw * dw);
+  const int period = __builtin_amdgcn_readfirstlane(OUT && dw4 > 1e-26 ? kPeriod : 1);
   if (tid < 33) tab[tid] = float(power(tid));
-  if (tid >= 64 && tid < 128) {
-    const int j = tid & 31, n = tid < 96 ? kChunk : rest;
-    tab[kPowers + tid - 64] = j >= n ? 0.f : BACK ? scale * float(power(j + 1)) : float(power(n - 1 - j));
+  if (tid < kWeights) {
+    const int k = tid / kChunk, j = tid % kChunk, n = k < kPeriod ? kChunk : rest;
+    double w = j >= n ? 0.0 : BACK ? double(scale) * power(j + 1) : power(n - 1 - j);
+    if (k < kPeriod)
+      for (int i = k + 1; i < period; ++i) w *= dw;
+    tab[kPowers + tid] = float(w);
   }
-  const double dw = power.square[5];
-  const float whole_hi = float(dw), whole_lo = float(dw - double(whole_hi)), rest_dec = float(power(max(rest, 0)));
+  if (tid >= 192 && tid < 192 + kPeriod) {
+    double f = 1.0;
+    if (tid > 192)
+      for (int i = tid - 192; i < period; ++i) f *= dw;
+    tab[kPowers + kWeights + tid - 192] = float(1.0 / f);
+  }
+  const double dp = period == kPeriod ? dw4 : dw;
+  const float whole_hi = float(dp), whole_lo = float(dp - double(whole_hi)), rest_dec = float(power(max(rest, 0)));
   meet_lds();                                          // (M and the first copies are on their way)
   // P: this wave's quarter, x_t.y_j for j = pj .. pj + 3 and t = pt
   const int pq = lane >> 4, pj = 16 * (wave >> 1) + 4 * pq, pt = 16 * (wave & 1) + rp;
@@ -206,7 +225,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   const float row_rest = BACK ? tab[max(rest - 1 - ln, 0)] : row_whole;
 
   // operand addresses within a stage
-  uint32_t kr[4], yt[2][2], zt[2], py[2], px[2];
+  uint32_t kr[4], yt[2][2], zt[2], py[2], px[2], put[4];   // (of the present stage)
 #pragma unroll
   for (int k = 0; k < 4; ++k) kr[k] = lds0 + uint32_t(ln * 128 + 16 * ((2 * k + hl) ^ swz_k(ln & 15)));
 #pragma unroll
@@ -233,49 +252,61 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   const int out_heads = geo.kv_heads * (BACK ? 1 : G);
   // a result on its way: through the place of x in LDS, from where whole rows are stored, by the wave that then copies the next
   // item's rows there
-  const uint32_t put = lds0 + uint32_t(wave >> 1) * kHalf + uint32_t(ln * 128 + 8 * hl);
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    put[k] = lds0 + uint32_t(wave >> 1) * kHalf + uint32_t(ln * 128 + 8 * hl + 16 * ((4 * (wave & 1) + k) ^ swz_k(ln & 15)));
   const uint32_t get = lds0 + uint32_t(rp >> 3) * kHalf;
   uint16_t* const out_row = OUT ? out + (p.row + (geo.step == nullptr ? int64_t(p.seq) * p.rows : 0)) * out_heads * kD + 8 * rp : nullptr;
   int held_n = 0;                                      // its rows, or none
   int64_t held_at = 0;
-  auto flush = [&](uint32_t stage) {
-    if (held_n == 0) return;
+  bf16x8 going[2];
+  auto fetch = [&](uint32_t stage) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int row = 8 * wave + 4 * i + pq;
-      const uint4 u = __builtin_bit_cast(uint4, lds_row(get + stage * kStage + uint32_t(row * 128 + 16 * ((rp & 7) ^ swz_k(row & 15)))));
-      if (row < held_n) *reinterpret_cast<uint4*>(out_row + held_at + int64_t(row) * out_heads * kD) = u;
+      going[i] = lds_row(get + stage * kStage + uint32_t(row * 128 + 16 * ((rp & 7) ^ swz_k(row & 15))));
     }
-    __builtin_amdgcn_s_waitcnt(waitcnt_lds());         // (read, before the copies to come)
+  };
+  auto store = [&] {                                   // (waits for what was read: before the copies to its place)
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_s_waitcnt(waitcnt_lds());
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = 8 * wave + 4 * i + pq;
+      if (row < held_n) *reinterpret_cast<bf16x8*>(out_row + held_at + int64_t(row) * out_heads * kD) = going[i];
+    }
     held_n = 0;
   };
   float err = 0.f;                                     // of the factors so far, relative
   double far = 1.0;                                    // without results: the chunk's factor
   uint32_t stage = 0;
-  int chunk = 0, n = 0;                                // the chunk and its tokens
+  int chunk = 0, n = 0, phase = 0;                     // the chunk, its tokens, and its place in the period
   bool full = true;
   bf16x8 z[2];                                         // Z^T: z-dim zd, tokens 16 kk + 4 hl .. + 3 and 8 more
   auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  auto before = [&] { return stage == 0 ? 2 : stage - 1; };
 
   // An item's way to its result; FIRST: the first query head of the chunk.  Products and vector work are dealt out so that each
   // has the other to run beside.
   auto result = [&](auto first, int g) {
     constexpr bool kOfM = decltype(first)::value || !BACK;   // (backwards the sum over the query heads begins)
-    const uint32_t at = stage * kStage;
     // (its parts are formed anew for each query head: held, they would take 64 registers that are not there)
     if (kOfM) asm volatile("" : "+v"(S[0]), "+v"(S[1]), "+v"(S[2]), "+v"(S[3]));
     // this wave's quarter of P^T = Y X^T
     f32x4 s = f32x4{};
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
-      const uint32_t c = at + (ks >> 1) * kHalf;
+      const uint32_t c = (ks >> 1) * kHalf;
       s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row(py[ks & 1] + c), lds_row(px[ks & 1] + c), s, 0, 0, 0);
     }
-    auto row = [&](int ks) { return lds_row(kr[ks & 3] + at + (ks >> 2) * kHalf); };
+    auto row = [&](int ks) { return lds_row(kr[ks & 3] + (ks >> 2) * kHalf); };
     bf16x8 x[3];
 #pragma unroll
     for (int k = 0; k < 2; ++k) x[k] = row(k);
     fence();
+    store();
+    issue(before());
     {
       float w[4];
 #pragma unroll
@@ -348,74 +379,68 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     }
   };
   auto keep = [&](int g) {                             // the result, to be stored behind the next barrier
-    const float weight = full ? row_whole : row_rest;
+    const float weight = (full ? row_whole : row_rest) * tab[kPowers + kWeights + phase];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       float r[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(os[4 * k + i], weight, op[4 * k + i]);
-      *(lds_u32x2*)(uintptr_t)(put + stage * kStage + 16 * ((4 * (wave & 1) + k) ^ swz_k(ln & 15))) =
-          u32x2{pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
+      *(lds_u32x2*)(uintptr_t)(put[k]) = u32x2{pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
     }
     held_n = n;
     held_at = (int64_t(chunk) * kChunk * out_heads + (BACK ? h : h * G + g)) * kD;
   };
   // M past the chunk (of its first query head, backwards), and the present item's part.
   auto advance = [&](auto first, auto&& between) {
-    constexpr bool kForget = OUT && decltype(first)::value;
+    // (a partial chunk: M as it is, and no period)
+    const bool forget = OUT && decltype(first)::value && (phase == 0 || !full);
     float dec = 1.f;
-    if (kForget) {
+    if (forget) {
       const float want = whole_lo + err;
-      dec = full ? whole_hi + want : rest_dec;
+      dec = full ? whole_hi + want : rest_dec * tab[kPowers + kWeights + phase];
       if (full) err = want - (dec - whole_hi);
     }
-    const uint32_t kw = kwt + (full ? 0u : 4u * kChunk), at = stage * kStage;
-    bf16x8 part[2][PARTS], y[2][2];
-    auto operand = [&](int mt, int kk) {
-      const uint32_t ya = at + (mt >> 1) * kHalf + kk * 2048;
-      return lds_tr2(yt[0][mt & 1] + ya, yt[1][mt & 1] + ya);
-    };
-    float c8[2][8];
+    const uint32_t kw = kwt + 4u * kChunk * uint32_t(full ? phase : kPeriod);
+    if (forget) {
+      stay();
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
+      for (int mt = 0; mt < 4; ++mt) S[mt] *= dec;
+    }
+    auto operand = [&](int i) {                        // of tokens 16 (i / 4) .., y-dims 32 (i % 4) ..
+      const uint32_t ya = ((i & 3) >> 1) * kHalf + (i >> 2) * 2048;
+      return lds_tr2(yt[0][i & 1] + ya, yt[1][i & 1] + ya);
+    };
+    bf16x8 part[PARTS], y[3];
+    auto split = [&](int kk) {
       const float4 a = __builtin_bit_cast(float4, *(const tok::lds_u32x4*)(uintptr_t)(kw + 64 * kk));
       const float4 b = __builtin_bit_cast(float4, *(const tok::lds_u32x4*)(uintptr_t)(kw + 64 * kk + 32));
-      const float t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) c8[kk][e] = t[e];
-      y[0][kk] = operand(0, kk);
-    }
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
+      const float c8[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
       float w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = float(z[kk][e]) * (OUT ? c8[kk][e] : c8[kk][e] * float(far));
+      for (int e = 0; e < 8; ++e) w[e] = float(z[kk][e]) * (OUT ? c8[e] : c8[e] * float(far));
 #pragma unroll
-      for (int k = 0; k < PARTS; ++k) part[kk][k] = k == PARTS - 1 ? last_part(w) : top_part(w);
-    }
-    if (kForget) S[0] *= dec;
+      for (int k = 0; k < PARTS; ++k) part[k] = k == PARTS - 1 ? last_part(w) : top_part(w);
+    };
+    y[0] = operand(0);
+    y[1] = operand(1);
+    split(0);
 #pragma unroll
-    for (int mt = 0; mt < 4; ++mt) {
+    for (int i = 0; i < 8; ++i) {
       fence();
+      if (i + 2 < 8) y[(i + 2) % 3] = operand(i + 2);
+      if (i == 4) split(1);
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        if (mt < 3) y[(mt + 1) & 1][kk] = operand(mt + 1, kk);
-#pragma unroll
-        for (int k = PARTS - 1; k >= 0; --k) S[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[mt & 1][kk], part[kk][k], S[mt], 0, 0, 0);
-      }
-      if (kForget && mt < 3) S[mt + 1] *= dec;
-      if (mt == 1) between();
+      for (int k = PARTS - 1; k >= 0; --k) S[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[i % 3], part[k], S[i & 3], 0, 0, 0);
+      if (i == 3) between();
     }
     fence();
   };
   auto begin_item = [&] {
     meet<OUT ? 6 : 4>();                               // this item has landed, and the last one's buffer is free
-    const uint32_t before = stage == 0 ? 2 : stage - 1;
-    if (OUT) flush(before);
-    issue(before);
-    const uint32_t at = stage * kStage;
+    if (OUT) fetch(before());
+    else issue(before());
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) z[kk] = lds_tr2(zt[0] + at + kk * 2048, zt[1] + at + kk * 2048);
+    for (int kk = 0; kk < 2; ++kk) z[kk] = lds_tr2(zt[0] + kk * 2048, zt[1] + kk * 2048);
     if (seldom(!full)) {
       stay();
 #pragma unroll
@@ -425,7 +450,14 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
           if (16 * kk + 8 * (e >> 2) + 4 * hl + (e & 3) >= n) z[kk][e] = (__bf16)0.f;
     }
   };
-  auto end_item = [&] { stage = stage == 2 ? 0 : stage + 1; };
+  auto end_item = [&] {
+    const uint32_t d = stage == 2 ? uint32_t(-2) * kStage : kStage;
+    stage = stage == 2 ? 0 : stage + 1;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) kr[k] += d, yt[k >> 1][k & 1] += d, put[k] += d;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) zt[k] += d, py[k] += d, px[k] += d;
+  };
   const std::true_type yes;
   const std::false_type no;
 
@@ -456,10 +488,17 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
       end_item();
     }
     if (!OUT) far *= full ? dw : double(rest_dec);
+    phase = full && phase + 1 < period ? phase + 1 : 0;
   }
   meet<0>();                                           // no copy outlives the walk
-  if (OUT) flush(stage == 0 ? 2 : stage - 1);
+  if (OUT) {
+    fetch(before());
+    store();
+  }
   if (last != nullptr) {
+    if (phase > 0)
+#pragma unroll
+      for (int mt = 0; mt < 4; ++mt) S[mt] *= tab[kPowers + kWeights + phase];
 #pragma unroll
     for (int mt = 0; mt < 4; ++mt)
 #pragma unroll

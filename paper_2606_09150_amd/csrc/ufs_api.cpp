@@ -64,9 +64,10 @@ int check_work(const void* work, size_t bytes, size_t need) {
 // the backward's 3 beside two sums.  Parts are walked side by side, and pay with a sum of each, two launches and their states'
 // way through memory.  The time of either is estimated from what these launches took (us; c chunks a part, P parts of
 // a sequence, W workgroups): walks 2.0 c on a CU of their own (W up to 160), 2.8 c where W = 256, 5.1 c at 512, the backward's 1.9 c
-// and W c / 136; sums 0.9 c, and 2.05 c at 512; the states carried on 0.36 P, or 13 us for 512 of them.  Whole / in parts
+// and W c / 155; sums 0.9 c, and 2.05 c at 512; the states carried on 0.12 P, or 13 us for 512 of them.  Whole / in parts
 // of 2 / 4 / 8 chunks: 1 x 256 tokens, 16 heads, 20 / 20.5 / 24 / -, backward 20 / 31 / 32 / -; 1 x 1,024 68 / 29 / 30 / 37, backward
-// 66 / 61 / 48 / 47.  1 x 16,384 tokens, 32 heads, in 8 / 16 parts 231 / 216, backward 486 / 514.
+// 66 / 61 / 48 / 47.  1 x 16,384 tokens in 1 / 4 / 8 parts, 64 heads: - / 424 / 395, backward 996 / 878 / 902; of 4 heads in 43 / 64 / 128
+// parts 61 / 53 / 62, backward 79 / 86 / 108.
 int32_t part_chunks(int64_t all, int64_t longest, int64_t n, int64_t heads, int walks) {
   const int sums = walks > 1 ? 2 : 1;
   auto time = [&](int64_t c) {
@@ -74,11 +75,11 @@ int32_t part_chunks(int64_t all, int64_t longest, int64_t n, int64_t heads, int 
     const double groups = double(heads) * (c < longest ? std::ceil(double(all) / double(c)) + 0.5 * double(n - 1) : double(n));
     // rounds of two workgroups a CU, and what is left
     const double all_walks = walks * groups, whole = std::floor(all_walks / 512.0), rest = all_walks - 512.0 * whole;
-    const double walk = double(c) * (walks > 1 ? std::max(1.9, all_walks / 136.0)
+    const double walk = double(c) * (walks > 1 ? std::max(1.9, all_walks / 155.0)
                                                : whole * 5.05 + (rest > 0.0 ? std::max(2.0, 0.6 + rest / 115.0) : 0.0));
     if (c >= longest) return 4.0 + walk;
-    return (walks > 1 ? 18.0 : 13.0) + walk + double(c) * std::max(0.9, sums * groups / (walks > 1 ? 290.0 : 250.0)) +
-           sums * std::max(0.36 * parts, 0.026 * groups);
+    return (walks > 1 ? 18.0 : 13.0) + walk + double(c) * std::max(0.9, sums * groups / (walks > 1 ? 310.0 : 250.0)) +
+           std::max(0.12 * parts, 0.026 * sums * groups);
   };
   int64_t best = std::max<int64_t>(longest, 1);
   for (int64_t c = 1; c < longest; c += std::max<int64_t>(1, c / 8))
