@@ -4,10 +4,13 @@
 // What bounds all three is HBM: a state of 64 KB is read and written for 256 bytes of k and
 // v, and products and sums are done in fp32 on the vector ALUs beside it.
 //
-// A step's workgroup holds COLS columns (of v) of a state in registers, 16 bytes a thread and row,
-// loads in flight all at once, and takes its sequence's tokens one by one:
-// S = L S + k v^T, o = scale S^T q, rows summed over lanes and then over waves through LDS.
-// L goes as two floats: one would be off by the same 2^-25 in each of thousands of steps.
+// A step's wave holds 32 columns (of v: whole cache lines) of a state in registers, a lane four columns of 16
+// rows, loads in flight all at once.  It takes its sequence's tokens one by one, S = L S + k v^T and
+// o = scale S^T q, rows summed over lanes; no wave waits for another.  Where states are few a wave has 32 of their
+// rows, all tokens' k, v and queries come through LDS at once, and the waves' sums meet there behind the last token: a wave's way through a token is as long as its part of a state
+// (192 states, 2 query heads, 7 tokens: 14.8 us whole).  (Fewer columns a wave have XCDs read each
+// other's lines: 192 states, 1 token, 6.9 us of 32 columns, 13 of 16, 19.6 of 8.)  L goes as two
+// floats: one would be off by the same 2^-25 in each of thousands of steps.
 #include <algorithm>
 
 #include "linear_place.h"
@@ -21,135 +24,123 @@ using namespace attn;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kHeads = 8;                              // query heads taken at a time
 
-template <int COLS>
+// Sums over the lanes of the same columns (lane % 8), in all of them.
+__device__ inline float column_sum(float x) {
+  x += __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x128, 0xf, 0xf, false));   // lane ^ 8
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+template <int N>
+struct Dims {                                          // N dimensions of a row, bf16
+  typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
+  words w;
+  __device__ static Dims of(const uint16_t* p) { return Dims{*reinterpret_cast<const words*>(p)}; }
+  __device__ void unpack(float (&x)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+};
+
+constexpr int kCols = 32, kSums = 64;                  // columns of a wave; (token, query head) pairs whose sums LDS holds
+// SPLIT: the waves of a workgroup have the rows of the same columns, or the columns of the same state.
+template <bool SPLIT>
 __global__ __launch_bounds__(kThreads) void linear_step_kernel(StepArgs a) {
-  constexpr int kC4 = COLS / 4;                        // threads along a row
-  constexpr int kGroups = kThreads / kC4;              // rows side by side
-  constexpr int kRows = kD / kGroups;                  // rows of a thread: group + kGroups i
-  constexpr int kLane = 64 / kC4;                      // groups of a wave
-  constexpr int kSlices = kD / COLS;
-  __shared__ float sk[kD], sv[COLS], sq[kHeads][kD];
-  __shared__ float so[kHeads][4][COLS];
-
+  constexpr int kRows = SPLIT ? 4 : 16;                // of a lane
+  __shared__ float sums[SPLIT ? kSums : 1][4][kCols];
+  __shared__ __attribute__((aligned(16))) uint16_t sk[SPLIT ? kFewTokens : 1][kD], sv[SPLIT ? kFewTokens : 1][kCols], sq[SPLIT ? kSums : 1][kD];
   const Geo& geo = a.geo;
-  int idx = blockIdx.x;
-  const int slice = idx % kSlices;
-  idx /= kSlices;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int slice = SPLIT ? blockIdx.x % 4 : wave, idx = SPLIT ? blockIdx.x / 4 : blockIdx.x;
   const int h = idx % geo.kv_heads, e = idx / geo.kv_heads;
-  if (e >= ((const const_i32*)geo.step)[0]) return;
+  if (e >= min(geo.n, ((const const_i32*)geo.step)[0])) return;
   Place p;
   entry_of(geo, e, p);
   if (p.seq < 0 || p.tokens == 0) return;
 
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int c4 = tid % kC4, group = tid / kC4;
-  float* const state = a.states + (size_t(p.seq) * geo.kv_heads + h) * kState + slice * COLS + 4 * c4;
-  float4 S[kRows];
+  const int col = slice * kCols + 4 * (lane & 7), row0 = (SPLIT ? wave * 32 : 0) + kRows * (lane >> 3);
+  float* const state = a.states + (size_t(p.seq) * geo.kv_heads + h) * kState + row0 * kD + col;
+  f32x4 S[kRows];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
-    S[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (p.held) S[i] = *reinterpret_cast<const float4*>(state + (group + kGroups * i) * kD);
+    S[i] = f32x4{};
+    if (p.held) S[i] = *reinterpret_cast<const f32x4*>(state + i * kD);
   }
-  const double gd = double(geo.decay[h]), dd = exp(gd);
+  const int G = geo.group, tokens = min(p.tokens, a.longest);
+  const uint16_t* const kp = a.k.p + p.row * a.k.token + int64_t(h) * a.k.head;
+  const uint16_t* const vp = a.v.p + p.row * a.v.token + int64_t(h) * a.v.head + slice * kCols;
+  const uint16_t* const qp = a.q.p + p.row * a.q.token + int64_t(h) * G * a.q.head;
+  if (SPLIT) {                                         // chunks of 16 bytes: of q, of k, of v
+    const int nq = tokens * G * 16, nk = nq + tokens * 16, all = nk + tokens * 4;
+    for (int i = threadIdx.x; i < all; i += kThreads) {
+      if (i < nq) {
+        const int r = i / 16, t = r / G;
+        *reinterpret_cast<uint4*>(&sq[r][8 * (i % 16)]) = *reinterpret_cast<const uint4*>(qp + t * a.q.token + (r - t * G) * a.q.head + 8 * (i % 16));
+      } else if (i < nk) {
+        const int t = (i - nq) / 16;
+        *reinterpret_cast<uint4*>(&sk[t][8 * (i % 16)]) = *reinterpret_cast<const uint4*>(kp + t * a.k.token + 8 * (i % 16));
+      } else {
+        const int t = (i - nk) / 4;
+        *reinterpret_cast<uint4*>(&sv[t][8 * (i % 4)]) = *reinterpret_cast<const uint4*>(vp + t * a.v.token + 8 * (i % 4));
+      }
+    }
+    __syncthreads();
+  }
+  const double dd = exp(double(geo.decay[h]));
   const float hi = float(dd), lo = float(dd - double(hi));
-  const int G = geo.group;
-  const int tokens = min(p.tokens, a.longest);
+  uint16_t* const op = a.o + (p.row * geo.kv_heads * G + h * G) * kD + col;
+  auto keys = [&](int t) { return Dims<kRows>::of(SPLIT ? &sk[t][row0] : kp + t * a.k.token + row0); };
+  auto values = [&](int t) { return *reinterpret_cast<const uint2*>(SPLIT ? &sv[t][4 * (lane & 7)] : vp + t * a.v.token + 4 * (lane & 7)); };
+  auto queries = [&](int t, int g) { return Dims<kRows>::of(SPLIT ? &sq[t * G + g][row0] : qp + t * a.q.token + g * a.q.head + row0); };
 
-  // what a token and block of query heads bring: k, v and the queries, a pair of dimensions a thread
-  constexpr int kPairs2 = (kD + COLS + kHeads * kD) / 2, kLoads = (kPairs2 + kThreads - 1) / kThreads;
-  uint32_t next[kLoads];
-  auto fetch = [&](int t, int g0) {
-    const int64_t row = p.row + t;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      int k = 2 * (tid + kThreads * i);
-      const uint16_t* from = nullptr;
-      if (k < kD) {
-        if (g0 == 0) from = a.k.p + row * a.k.token + int64_t(h) * a.k.head + k;
-      } else if (k < kD + COLS) {
-        if (g0 == 0) from = a.v.p + row * a.v.token + int64_t(h) * a.v.head + slice * COLS + (k - kD);
-      } else {
-        k -= kD + COLS;
-        const int g = g0 + k / kD;
-        if (k < kHeads * kD && g < G) from = a.q.p + row * a.q.token + int64_t(h * G + g) * a.q.head + k % kD;
-      }
-      next[i] = from != nullptr ? *reinterpret_cast<const uint32_t*>(from) : 0u;
-    }
-  };
-  auto place_in_lds = [&](int g0) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      int k = 2 * (tid + kThreads * i);
-      const float2 x = make_float2(__uint_as_float(next[i] << 16), __uint_as_float(next[i] & 0xffff0000u));
-      if (k < kD) {
-        if (g0 == 0) *reinterpret_cast<float2*>(&sk[k]) = x;
-      } else if (k < kD + COLS) {
-        if (g0 == 0) *reinterpret_cast<float2*>(&sv[k - kD]) = x;
-      } else {
-        k -= kD + COLS;
-        if (k < kHeads * kD) *reinterpret_cast<float2*>(&sq[k / kD][k % kD]) = x;
-      }
-    }
-  };
-  fetch(0, 0);
+  Dims<kRows> q = queries(0, 0);
+#pragma unroll 1
   for (int t = 0; t < tokens; ++t) {
-    for (int g0 = 0; g0 < G; g0 += kHeads) {
-      const int heads = min(kHeads, G - g0);
-      place_in_lds(g0);
-      __syncthreads();
-      {
-        const bool more = g0 + kHeads < G;             // the next block, or the next token's first
-        if (more || t + 1 < tokens) fetch(more ? t : t + 1, more ? g0 + kHeads : 0);
-      }
-      if (g0 == 0) {
-        const float4 v = *reinterpret_cast<const float4*>(&sv[4 * c4]);
+    {
+      float x[kRows];
+      keys(t).unpack(x);
+      const uint2 w = values(t);
+      const float y[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                          __uint_as_float(w.y & 0xffff0000u)};
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-          const float k = sk[group + kGroups * i];
-          S[i].x = __builtin_fmaf(S[i].x, hi, __builtin_fmaf(S[i].x, lo, k * v.x));
-          S[i].y = __builtin_fmaf(S[i].y, hi, __builtin_fmaf(S[i].y, lo, k * v.y));
-          S[i].z = __builtin_fmaf(S[i].z, hi, __builtin_fmaf(S[i].z, lo, k * v.z));
-          S[i].w = __builtin_fmaf(S[i].w, hi, __builtin_fmaf(S[i].w, lo, k * v.w));
-        }
-      }
-      for (int g = 0; g < heads; ++g) {
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < kRows; ++i)
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-          const float q = sq[g][group + kGroups * i];
-          o.x = __builtin_fmaf(q, S[i].x, o.x);
-          o.y = __builtin_fmaf(q, S[i].y, o.y);
-          o.z = __builtin_fmaf(q, S[i].z, o.z);
-          o.w = __builtin_fmaf(q, S[i].w, o.w);
-        }
+        for (int c = 0; c < 4; ++c) S[i][c] = __builtin_fmaf(S[i][c], hi, __builtin_fmaf(S[i][c], lo, x[i] * y[c]));
+    }
+#pragma unroll 1
+    for (int g = 0; g < G; ++g) {
+      float x[kRows], o[4] = {0.f, 0.f, 0.f, 0.f};
+      q.unpack(x);
+      if (g + 1 < G || t + 1 < tokens) q = g + 1 < G ? queries(t, g + 1) : queries(t + 1, 0);   // the next ones
 #pragma unroll
-        for (int d = kC4; d < 64; d <<= 1) {           // the wave's groups
-          o.x += __shfl_xor(o.x, d);
-          o.y += __shfl_xor(o.y, d);
-          o.z += __shfl_xor(o.z, d);
-          o.w += __shfl_xor(o.w, d);
-        }
-        if (lane < kC4) *reinterpret_cast<float4*>(&so[g][wave][4 * lane]) = o;
-      }
-      __syncthreads();
-      for (int k = 2 * tid; k < heads * COLS; k += 2 * kThreads) {
-        const int g = k / COLS, c = k % COLS;
-        float2 s = make_float2(0.f, 0.f);
+      for (int i = 0; i < kRows; ++i)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          s.x += so[g][w][c];
-          s.y += so[g][w][c + 1];
-        }
-        *reinterpret_cast<uint32_t*>(a.o + ((p.row + t) * geo.kv_heads * G + h * G + g0 + g) * kD + slice * COLS + c) =
-            pack_bf16x2(geo.scale * s.x, geo.scale * s.y);
+        for (int c = 0; c < 4; ++c) o[c] = __builtin_fmaf(x[i], S[i][c], o[c]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] = column_sum(o[c]);
+      if (SPLIT) {
+        if (lane < 8) *reinterpret_cast<f32x4*>(&sums[t * G + g][wave][4 * lane]) = f32x4{o[0], o[1], o[2], o[3]};
+      } else if (lane < 8) {
+        *reinterpret_cast<uint2*>(op + (int64_t(t) * geo.kv_heads * G + g) * kD) =
+            make_uint2(pack_bf16x2(geo.scale * o[0], geo.scale * o[1]), pack_bf16x2(geo.scale * o[2], geo.scale * o[3]));
       }
     }
   }
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) *reinterpret_cast<float4*>(state + (group + kGroups * i) * kD) = S[i];
-  static_assert(kLane * kC4 == 64, "whole groups in a wave");
+  for (int i = 0; i < kRows; ++i) *reinterpret_cast<f32x4*>(state + i * kD) = S[i];
+  if (SPLIT) {
+    __syncthreads();
+    for (int k = threadIdx.x; k < tokens * G * (kCols / 2); k += kThreads) {
+      const int i = k / (kCols / 2), c = 2 * (k % (kCols / 2)), t = i / G, g = i - t * G;
+      const float2 s0 = *reinterpret_cast<const float2*>(&sums[i][0][c]), s1 = *reinterpret_cast<const float2*>(&sums[i][1][c]),
+                   s2 = *reinterpret_cast<const float2*>(&sums[i][2][c]), s3 = *reinterpret_cast<const float2*>(&sums[i][3][c]);
+      *reinterpret_cast<uint32_t*>(a.o + ((p.row + t) * geo.kv_heads * G + h * G + g) * kD + slice * kCols + c) =
+          pack_bf16x2(geo.scale * ((s0.x + s1.x) + (s2.x + s3.x)), geo.scale * ((s0.y + s1.y) + (s2.y + s3.y)));
+    }
+  }
 }
 
 // States of a sequence in a layer, copied: a workgroup per (pair, layer, 16 KB).
@@ -196,10 +187,10 @@ __global__ __launch_bounds__(kThreads) void state_reorder_kernel(ReorderArgs a) 
 
 hipError_t launch_linear_step(const StepArgs& a, hipStream_t stream) {
   const int64_t units = int64_t(a.geo.n) * a.geo.kv_heads;
-  if (units < 256)
-    linear_step_kernel<32><<<dim3(unsigned(units * 4)), kThreads, 0, stream>>>(a);
+  if (units < 256 && int64_t(a.longest) * a.geo.group <= kSums)
+    linear_step_kernel<true><<<dim3(unsigned(units * 4)), kThreads, 0, stream>>>(a);
   else
-    linear_step_kernel<128><<<dim3(unsigned(units)), kThreads, 0, stream>>>(a);
+    linear_step_kernel<false><<<dim3(unsigned(units)), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -68,17 +68,18 @@ int check_work(const void* work, size_t bytes, size_t need) {
 // of 2 / 4 / 8 chunks: 1 x 256 tokens, 16 heads, 20 / 20.5 / 24 / -, backward 20 / 31 / 32 / -; 1 x 1,024 68 / 29 / 30 / 37, backward
 // 66 / 61 / 48 / 47.  1 x 16,384 tokens in 1 / 4 / 8 parts, 64 heads: - / 424 / 395, backward 996 / 878 / 902; of 4 heads in 43 / 64 / 128
 // parts 61 / 53 / 62, backward 79 / 86 / 108.
-int32_t part_chunks(int64_t all, int64_t longest, int64_t n, int64_t heads, int walks) {
+int32_t part_chunks(int64_t all, int64_t longest, int64_t n, int64_t heads, int walks, int group) {
   const int sums = walks > 1 ? 2 : 1;
+  const double item = 0.35 + 0.65 * group, sum = walks > 1 ? 0.5 + 0.5 * group : 1.0;   // of a group's heads, for one's
   auto time = [&](int64_t c) {
     const double parts = double((longest + c - 1) / c);
     const double groups = double(heads) * (c < longest ? std::ceil(double(all) / double(c)) + 0.5 * double(n - 1) : double(n));
     // rounds of two workgroups a CU, and what is left
     const double all_walks = walks * groups, whole = std::floor(all_walks / 512.0), rest = all_walks - 512.0 * whole;
-    const double walk = double(c) * (walks > 1 ? std::max(1.9, all_walks / 155.0)
+    const double walk = item * double(c) * (walks > 1 ? std::max(1.9, all_walks / 155.0)
                                                : whole * 5.05 + (rest > 0.0 ? std::max(2.0, 0.6 + rest / 115.0) : 0.0));
     if (c >= longest) return 4.0 + walk;
-    return (walks > 1 ? 18.0 : 13.0) + walk + double(c) * std::max(0.9, sums * groups / (walks > 1 ? 310.0 : 250.0)) +
+    return (walks > 1 ? 18.0 : 13.0) + walk + sum * double(c) * std::max(0.9, sums * groups / (walks > 1 ? 310.0 : 250.0)) +
            std::max(0.12 * parts, 0.026 * sums * groups);
   };
   int64_t best = std::max<int64_t>(longest, 1);
@@ -117,7 +118,7 @@ int check_linear(const ufs_linear_desc* d, int walks, lin::Geo* g) {
   const int64_t chunks = (int64_t(d->tokens) + lin::kChunk - 1) / lin::kChunk;
   const double units = double(d->batch) * d->kv_heads;
   if (units * 8 * 2 > kMostGroups) return fail(UF_ERR_ARG, "shape too large: batch * kv_heads");
-  g->chunks = part_chunks(chunks * d->batch, chunks, d->batch, d->kv_heads, walks);
+  g->chunks = part_chunks(chunks * d->batch, chunks, d->batch, d->kv_heads, walks, g->group);
   g->parts = int32_t((chunks + g->chunks - 1) / g->chunks);
   if ((units * g->parts + 8) * 3 > kMostGroups || double(chunks) * g->group > 2.0e9)
     return fail(UF_ERR_ARG, "shape too large: batch * q_heads * tokens");
@@ -383,7 +384,7 @@ int ufs_extend(ufs_cache* c, int32_t n, const int32_t* seqs, const int32_t* coun
       longest = std::max(longest, counts[i]);
     }
     if (total > (1 << 30)) return fail(UF_ERR_ARG, "more than 2^30 new tokens");
-    const int32_t part = part_chunks(chunks, (int64_t(longest) + lin::kChunk - 1) / lin::kChunk, n, c->d.kv_heads, 1);
+    const int32_t part = part_chunks(chunks, (int64_t(longest) + lin::kChunk - 1) / lin::kChunk, n, c->d.kv_heads, 1, 1);
     std::vector<Entry> step;
     std::vector<int32_t> words = {n, int32_t(total), 0, part};
     step.reserve(size_t(n));
