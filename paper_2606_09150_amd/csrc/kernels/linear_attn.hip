@@ -190,10 +190,10 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   const Powers<6> power(double(geo.decay[h]));
   const float scale = geo.scale;
   // M is multiplied by L^32 not chunk by chunk, but for a period of four at once at its beginning; meanwhile it stands for the
-  // period's end: parts join it with their weights there, and it is read with L^-32 for each chunk that is to come (e^60 at
-  // most: heads that forget faster have periods of one chunk).
+  // period's end: parts join it with their weights there, and it is read with L^-32 for each chunk that is to come (1e10 at
+  // most, so that what small gradients leave there stays in fp32's range: heads that forget faster have periods of one chunk).
   const double dw = power.square[5], dw4 = (dw * dw) * (dw * dw);
-  const int period = __builtin_amdgcn_readfirstlane(OUT && dw4 > 1e-26 ? kPeriod : 1);
+  const int period = __builtin_amdgcn_readfirstlane(OUT && dw4 > 1e-13 ? kPeriod : 1);
   if (tid < 33) tab[tid] = float(power(tid));
   if (tid < kWeights) {
     const int k = tid / kChunk, j = tid % kChunk, n = k < kPeriod ? kChunk : rest;
@@ -528,10 +528,9 @@ __device__ __forceinline__ void run_walk(const Geo& geo, const Walk& w, int idx,
   walk<BACK, true, PARTS>(geo, p, w.x, w.y, w.z, w.out, begin, w.trans != 0, ends && w.last != nullptr ? w.last + at : nullptr, smem);
 }
 
-template <int PARTS>
 __global__ __launch_bounds__(256, 2) void linear_fwd_kernel(WalkArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kShared];
-  run_walk<false, PARTS>(a.geo, a.walk[0], blockIdx.x, smem);
+  run_walk<false, 3>(a.geo, a.walk[0], blockIdx.x, smem);
 }
 
 // dk, dv and dq of eight workgroups' places one after the other: a place's three lie on one XCD, and share their reads there.
@@ -561,12 +560,13 @@ __global__ __launch_bounds__(256, 2) void linear_parts_kernel(PartArgs a, int gr
 
 // Parts' beginnings from their own M, part by part, kAhead of them read at once.  A workgroup per (sequence, key head,
 // sixteenth of M).
-constexpr int kSlices = kState / 1024, kAhead = 16;
+constexpr int kAhead = 16;
+static_assert(kScanSlices * 1024 == kState);
 __global__ __launch_bounds__(256) void linear_scan_kernel(PartArgs a) {
   const Geo& geo = a.geo;
   int k = blockIdx.x;
-  const int slice = k % kSlices;
-  k /= kSlices;
+  const int slice = k % kScanSlices;
+  k /= kScanSlices;
   const int h = k % geo.kv_heads;
   k /= geo.kv_heads;
   const int e = k % geo.n;
@@ -629,13 +629,12 @@ hipError_t launch_linear_parts(const PartArgs& a, int32_t groups, bool exact, hi
 }
 
 hipError_t launch_linear_scan(const PartArgs& a, hipStream_t stream) {
-  linear_scan_kernel<<<dim3(unsigned(kSlices * a.geo.kv_heads) * a.geo.n * a.n), 256, 0, stream>>>(a);
+  linear_scan_kernel<<<dim3(unsigned(kScanSlices * a.geo.kv_heads) * a.geo.n * a.n), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, bool exact, hipStream_t stream) {
-  if (exact) linear_fwd_kernel<3><<<dim3(unsigned(groups)), 256, 0, stream>>>(a);
-  else linear_fwd_kernel<2><<<dim3(unsigned(groups)), 256, 0, stream>>>(a);
+hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, hipStream_t stream) {
+  linear_fwd_kernel<<<dim3(unsigned(groups)), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

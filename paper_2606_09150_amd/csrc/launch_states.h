@@ -65,10 +65,11 @@ struct PartArgs {
   int32_t n;
 };
 
-// exact: states are wanted in fp32, not only what bf16 results need of them
+constexpr int kScanSlices = 16;              // of a state, workgroups of the scan
+// exact: states are results in fp32, or bear on one
 hipError_t launch_linear_parts(const PartArgs& a, int32_t groups, bool exact, hipStream_t stream);
 hipError_t launch_linear_scan(const PartArgs& a, hipStream_t stream);
-hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, bool exact, hipStream_t stream);
+hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, hipStream_t stream);
 hipError_t launch_linear_bwd(const WalkArgs& a, int32_t groups, bool exact, hipStream_t stream);
 
 // Few tokens a sequence: token by token.

@@ -117,10 +117,9 @@ int check_linear(const ufs_linear_desc* d, int walks, lin::Geo* g) {
   g->scale = d->scale;
   const int64_t chunks = (int64_t(d->tokens) + lin::kChunk - 1) / lin::kChunk;
   const double units = double(d->batch) * d->kv_heads;
-  if (units * 8 * 2 > kMostGroups) return fail(UF_ERR_ARG, "shape too large: batch * kv_heads");
   g->chunks = part_chunks(chunks * d->batch, chunks, d->batch, d->kv_heads, walks, g->group);
   g->parts = int32_t((chunks + g->chunks - 1) / g->chunks);
-  if ((units * g->parts + 8) * 3 > kMostGroups || double(chunks) * g->group > 2.0e9)
+  if ((units * std::max(g->parts, g->parts > 1 ? lin::kScanSlices : 1) + 8) * 3 > kMostGroups || double(chunks) * g->group > 2.0e9)
     return fail(UF_ERR_ARG, "shape too large: batch * q_heads * tokens");
   return UF_OK;
 }
@@ -172,7 +171,6 @@ int ufs_linear_fwd(const ufs_linear_desc* d, const void* d_q, const void* d_k, c
     a.geo.decay = d_decay;
     a.geo.lengths = d_lengths;
     const int32_t groups = a.geo.n * a.geo.parts * a.geo.kv_heads;
-    const bool exact = true;
     float* starts = nullptr;
     if (a.geo.parts > 1) {
       starts = static_cast<float*>(d_work);
@@ -180,12 +178,12 @@ int ufs_linear_fwd(const ufs_linear_desc* d, const void* d_q, const void* d_k, c
       p.geo = a.geo;
       p.n = 1;
       p.sum[0] = {src(d_k, d->k), src(d_v, d->v), d_state, starts, 0};
-      if (int s = check_hip(lin::launch_linear_parts(p, groups, exact, st), "linear attention")) return s;
+      if (int s = check_hip(lin::launch_linear_parts(p, groups, true, st), "linear attention")) return s;
       if (int s = check_hip(lin::launch_linear_scan(p, st), "linear attention")) return s;
     }
     a.n = 1;
     a.walk[0] = lin::Walk{src(d_q, d->q), src(d_k, d->k), src(d_v, d->v), static_cast<uint16_t*>(d_o), d_state, d_final, starts, 0};
-    if (int s = check_hip(lin::launch_linear_fwd(a, groups, exact, st), "linear attention")) return s;
+    if (int s = check_hip(lin::launch_linear_fwd(a, groups, st), "linear attention")) return s;
     return ok();
   });
 }
@@ -401,7 +399,7 @@ int ufs_extend(ufs_cache* c, int32_t n, const int32_t* seqs, const int32_t* coun
       cut = cut || own > part;
     }
     words[2] = parts;
-    if ((double(parts) + n) * c->d.kv_heads * 8 > kMostGroups) return fail(UF_ERR_ARG, "step too large for one launch");
+    if (double(std::max(parts, cut ? lin::kScanSlices * n : n)) * c->d.kv_heads > kMostGroups) return fail(UF_ERR_ARG, "step too large for one launch");
     if (!c->dry())
       for (size_t k = 0; k < words.size();) {
         tok::PokeArgs a;
@@ -494,7 +492,7 @@ int ufs_attn(const ufs_cache* c, int32_t layer, const ufs_attn_desc* d, const vo
     a.geo = g;
     a.n = 1;
     a.walk[0] = lin::Walk{src(d_q, d->q), src(d_k, d->k), src(d_v, d->v), static_cast<uint16_t*>(d_o), states, states, starts, 0};
-    if (int s = check_hip(lin::launch_linear_fwd(a, groups, true, st), "linear attention")) return s;
+    if (int s = check_hip(lin::launch_linear_fwd(a, groups, st), "linear attention")) return s;
     return ok();
   });
 }
