@@ -86,9 +86,10 @@ __device__ inline void stay() { asm volatile("" ::: "memory"); }
 // Sign bits of the halves that are not finite (junk in the others).
 __device__ inline uint32_t odd_halves(uint32_t u) { return (u & 0x7f807f80u) + 0x00800080u; }
 
-// Powers of L: squares of exp(g), and the product of those that an exponent is made of.
-template <int BITS>
+__device__ inline double power_of(float g, int e) { return e == 0 ? 1.0 : exp(double(g) * double(e)); }
+// The first powers of L: squares of exp(g), and the product of those that an exponent is made of (an exp costs as much as six of them).
 struct Powers {
+  static constexpr int BITS = 6;
   double square[BITS];
   __device__ explicit Powers(double g) {
     square[0] = exp(g);
@@ -109,7 +110,7 @@ struct Powers {
 // to put it at the end, or null.
 template <bool BACK, bool OUT, int PARTS>
 __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& xs, const Src& ys, const Src& zs, uint16_t* out,
-                                     const float* begin, bool trans, float* last, uint8_t* smem) {
+                                     const float* begin, const float* sums, bool trans, float* last, uint8_t* smem) {
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, hl = lane >> 5, ln = lane & 31, rp = lane & 15, gr = (lane >> 4) & 1;
@@ -169,25 +170,55 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   // M: y-dim 32 mt + 16 (r / 8) + 8 hl + r % 8, z-dim 32 wave + ln
   f32x16 S[4];
   const int zd = 32 * wave + ln;
+  auto get_rows = [&](f32x16& to, const float* from, int mt) {
+    if (trans) {
+      from += zd * kD + 8 * hl + 32 * mt;
 #pragma unroll
-  for (int mt = 0; mt < 4; ++mt) S[mt] = f32x16{};
-  if (begin != nullptr && trans) {
-    const float* const from = begin + zd * kD + 8 * hl;
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(from + 16 * (i >> 1) + 4 * (i & 1));
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(from + 16 * (i >> 1) + 4 * (i & 1));
+        for (int r = 0; r < 4; ++r) to[4 * i + r] = x[r];
+      }
+    } else {
+      from += (8 * hl + 32 * mt) * kD + zd;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) S[i >> 2][4 * (i & 3) + r] = x[r];
+      for (int r = 0; r < 16; ++r) to[r] = from[(16 * (r >> 3) + (r & 7)) * kD];
     }
-  } else if (begin != nullptr) {
-    const float* const from = begin + 8 * hl * kD + zd;
+  };
 #pragma unroll
-    for (int i = 0; i < 64; ++i) S[i >> 4][i & 15] = from[(16 * (i >> 3) + (i & 7)) * kD];
+  for (int mt = 0; mt < 4; ++mt) {
+    S[mt] = f32x16{};
+    if (begin != nullptr) get_rows(S[mt], begin, mt);
+  }
+  // and the parts that were walked before: each row's place is loaded anew as soon as it is used
+  const int before_me = OUT && sums != nullptr ? (BACK ? p.parts - 1 - p.part : p.part) : 0;
+  if (before_me > 0) {
+    const int64_t stride = int64_t(BACK ? -geo.kv_heads : geo.kv_heads) * kState;
+    const float* at = sums - before_me * stride;
+    const double whole = power_of(geo.decay[h], p.cut * kChunk);
+    double d = BACK ? power_of(geo.decay[h], p.tokens - (p.parts - 1) * p.cut * kChunk) : whole;
+    f32x16 T[4];
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt) get_rows(T[mt], at, mt);
+#pragma unroll 1
+    for (int i = 1;; ++i) {
+      const float hi = float(d), lo = float(d - double(hi));
+      d = whole;
+      at += stride;
+#pragma unroll
+      for (int mt = 0; mt < 4; ++mt) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[mt][r] = __builtin_fmaf(S[mt][r], hi, __builtin_fmaf(S[mt][r], lo, T[mt][r]));
+        if (i < before_me) get_rows(T[mt], at, mt);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (i == before_me) break;
+    }
   }
 
   // weights
   float* const tab = reinterpret_cast<float*>(smem + kTable);
-  const Powers<6> power(double(geo.decay[h]));
+  const Powers power(double(geo.decay[h]));
   const float scale = geo.scale;
   // M is multiplied by L^32 not chunk by chunk, but for a period of four at once at its beginning; meanwhile it stands for the
   // period's end: parts join it with their weights there, and it is read with L^-32 for each chunk that is to come (1e10 at
@@ -522,10 +553,12 @@ __device__ __forceinline__ void run_walk(const Geo& geo, const Walk& w, int idx,
   if (p.seq < 0) return;
   const size_t at = (size_t(p.seq) * geo.kv_heads + p.h) * kState;
   const bool ends = p.part == (BACK ? 0 : max(p.parts - 1, 0));
-  const float* begin = nullptr;
-  if (p.chunks > 0 && w.starts != nullptr) begin = w.starts + size_t(idx) * kState;
+  const float *begin = nullptr, *sums = nullptr;
+  const float* const start = p.chunks > 0 && w.starts != nullptr ? w.starts + size_t(idx) * kState : nullptr;
+  if (start != nullptr && geo.scanned) begin = start;
   else if (p.held && w.first != nullptr) begin = w.first + at;
-  walk<BACK, true, PARTS>(geo, p, w.x, w.y, w.z, w.out, begin, w.trans != 0, ends && w.last != nullptr ? w.last + at : nullptr, smem);
+  if (!geo.scanned) sums = start;
+  walk<BACK, true, PARTS>(geo, p, w.x, w.y, w.z, w.out, begin, sums, w.trans != 0, ends && w.last != nullptr ? w.last + at : nullptr, smem);
 }
 
 __global__ __launch_bounds__(256, 2) void linear_fwd_kernel(WalkArgs a) {
@@ -552,9 +585,9 @@ __global__ __launch_bounds__(256, 2) void linear_parts_kernel(PartArgs a, int gr
   if (p.seq < 0 || p.chunks == 0) return;
   float* const to = s.starts + size_t(idx) * kState;
   if (s.back) {
-    if (p.part > 0) walk<true, false, PARTS>(a.geo, p, s.y, s.y, s.z, nullptr, nullptr, false, to, smem);
+    if (p.part > 0) walk<true, false, PARTS>(a.geo, p, s.y, s.y, s.z, nullptr, nullptr, nullptr, false, to, smem);
   } else if (p.part < p.parts - 1) {
-    walk<false, false, PARTS>(a.geo, p, s.y, s.y, s.z, nullptr, nullptr, false, to, smem);
+    walk<false, false, PARTS>(a.geo, p, s.y, s.y, s.z, nullptr, nullptr, nullptr, false, to, smem);
   }
 }
 
@@ -583,18 +616,16 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(PartArgs a) {
     if (e >= head[0]) return;
     entry_of(geo, e, p);
     if (p.seq < 0) return;
-    cut(p, max(1, head[3]));
+    cut_into(p, max(1, head[3]));
     first = head[kHeader + kEntry * e + 4];
     if (first < 0 || first + p.parts > geo.parts) return;
   }
-  const int chunks = geo.step == nullptr ? geo.chunks : max(1, ((const const_i32*)geo.step)[3]);
-  const Powers<31> power(double(geo.decay[h]));
   const int at = slice * 1024 + threadIdx.x * 4;
   float4 m = make_float4(0.f, 0.f, 0.f, 0.f);
   if (s.first != nullptr && p.held)
     m = *reinterpret_cast<const float4*>(s.first + (size_t(p.seq) * geo.kv_heads + h) * kState + at);
-  const int tail = p.tokens - (p.parts - 1) * chunks * kChunk;
-  const double whole = power(chunks * kChunk), part = power(max(tail, 0));
+  const int tail = p.tokens - (p.parts - 1) * p.cut * kChunk;
+  const double whole = power_of(geo.decay[h], p.cut * kChunk), part = power_of(geo.decay[h], max(tail, 0));
   auto slot = [&](int i) {
     const int q = s.back ? p.parts - 1 - i : i;
     return reinterpret_cast<float4*>(s.starts + (size_t(first + q) * geo.kv_heads + h) * kState + at);

@@ -13,13 +13,15 @@ struct Place {
   int64_t row;          // first token: plain, of the sequence's tensors; a step, of the step's
   int tokens;           // of the sequence
   int chunk0, chunks;   // of the part
+  int cut;              // chunks of the parts before the last one
   int rows;             // rows of the sequence in the outputs (with padding)
   bool held;            // the state before the walk counts
 };
 
 // Whole parts cover the same number of chunks; the last one has the rest.
-__device__ inline void cut(Place& p, int chunks) {
+__device__ inline void cut_into(Place& p, int chunks) {
   const int all = (p.tokens + kChunk - 1) / kChunk;
+  p.cut = chunks;
   p.parts = (all + chunks - 1) / chunks;
   p.chunk0 = p.part * chunks;
   p.chunks = min(chunks, max(0, all - p.chunk0));
@@ -49,7 +51,7 @@ __device__ inline Place place(const Geo& g, int idx) {
     p.tokens = g.lengths != nullptr ? min(max(((words)g.lengths)[p.seq], 0), g.tokens) : g.tokens;
     p.rows = g.tokens;
     p.held = true;
-    cut(p, g.chunks);
+    cut_into(p, g.chunks);
     return p;
   }
   const words head = (words)g.step;
@@ -64,7 +66,7 @@ __device__ inline Place place(const Geo& g, int idx) {
   if (n < 1 || k >= head[2]) return p;
   entry_of(g, lo, p);
   p.part = k - head[kHeader + kEntry * lo + 4];
-  cut(p, chunks);
+  cut_into(p, chunks);
   if (p.part >= p.parts) p.seq = -1;
   return p;
 }

@@ -29,6 +29,7 @@ struct Geo {
   int32_t kv_heads, group;
   int32_t parts, chunks;      // plain: parts of a sequence, a step: of all; chunks of a part (plain)
   int32_t max_seqs;           // a step: states of the pool
+  int32_t scanned;            // the parts' own M were carried on by a launch of their own
   float scale;
 };
 
@@ -44,7 +45,7 @@ struct Walk {
   uint16_t* out;
   const float* first;         // M where the walk begins, or null
   float* last;                // M where it ends, or null
-  const float* starts;        // M where each part begins, or null: the only part begins with `first`
+  const float* starts;        // M where each part begins (scanned), or the parts' own; null: the only part begins with `first`
   int32_t trans;              // first and starts hold M transposed
 };
 constexpr int kWalks = 3;

@@ -60,14 +60,20 @@ int check_work(const void* work, size_t bytes, size_t need) {
   return UF_OK;
 }
 
-// Chunks of a part: of n sequences with `all` chunks, the longest with `longest`, of `heads` key heads each; `walks` 1, or
-// the backward's 3 beside two sums.  Parts are walked side by side, and pay with a sum of each, two launches and their states'
-// way through memory.  The time of either is estimated from what these launches took (us; c chunks a part, P parts of
-// a sequence, W workgroups): walks 2.0 c on a CU of their own (W up to 160), 2.8 c where W = 256, 5.1 c at 512, the backward's 1.9 c
-// and W c / 155; sums 0.9 c, and 2.05 c at 512; the states carried on 0.12 P, or 13 us for 512 of them.  Whole / in parts
-// of 2 / 4 / 8 chunks: 1 x 256 tokens, 16 heads, 20 / 20.5 / 24 / -, backward 20 / 31 / 32 / -; 1 x 1,024 68 / 29 / 30 / 37, backward
-// 66 / 61 / 48 / 47.  1 x 16,384 tokens in 1 / 4 / 8 parts, 64 heads: - / 424 / 395, backward 996 / 878 / 902; of 4 heads in 43 / 64 / 128
-// parts 61 / 53 / 62, backward 79 / 86 / 108.
+// Whether a launch of its own carries the states on from part to part, or each walk sums those of the parts before it.  `groups`:
+// parts of all sequences' key heads.  Carried on / summed (us; one sequence, parts of 4 chunks): 2 / 4 / 8 parts of 4 heads
+// 23.6 / 24.1 / 25.4, 22.0 / 24.6 / 30.3; of 64 heads 32.0 / 33.2 / 50.9, 22.3 / 28.8 / 44.0, and 16 parts 96 and 99.  Backward 3
+// / 4 / 6 parts of 4 heads 24.9 / 25.5 / 26.8, 24.2 / 26.3 / 30.5; 4 / 8 of 64 heads 58.6 / 102, 58.4 / 116.
+bool scanned(int64_t parts, double groups, int walks) { return parts > 4 && (walks > 1 || parts > 8 || groups < 256.0); }
+
+// Chunks of a part: of n sequences with `all` chunks, the longest with `longest`, of `heads` key heads with `group` query heads
+// each; `walks` 1, or the backward's 3 beside two sums.  Parts are walked side by side, and pay with a sum of each, a launch or two
+// and their states' way through memory.  The time of either is estimated from what these launches took (us; c chunks a part, P
+// parts of a sequence, W workgroups): walks 2.0 c on a CU of their own (W up to 160), 2.8 c where W = 256, 5.1 c at 512, the
+// backward's 1.9 c and W c / 155; sums 0.9 c, and 2.05 c at 512; the states carried on 0.12 P, or 13 us for 512 of them, or summed
+// 1.3 P (backward 1.5 P) with a launch less.  Whole / in parts of 2 / 4 / 8 chunks, carried on: 1 x 256 tokens, 16 heads, 20 / 20.5 /
+// 24 / -, backward 20 / 31 / 32 / -; 1 x 1,024 68 / 29 / 30 / 37, backward 66 / 61 / 48 / 47.  1 x 16,384 tokens in 1 / 4 / 8 parts,
+// 64 heads: - / 424 / 395, backward 996 / 878 / 902; of 4 heads in 43 / 64 / 128 parts 61 / 53 / 62, backward 79 / 86 / 108.
 int32_t part_chunks(int64_t all, int64_t longest, int64_t n, int64_t heads, int walks, int group) {
   const int sums = walks > 1 ? 2 : 1;
   const double item = 0.35 + 0.65 * group, sum = walks > 1 ? 0.5 + 0.5 * group : 1.0;   // of a group's heads, for one's
@@ -79,8 +85,9 @@ int32_t part_chunks(int64_t all, int64_t longest, int64_t n, int64_t heads, int 
     const double walk = item * double(c) * (walks > 1 ? std::max(1.9, all_walks / 155.0)
                                                : whole * 5.05 + (rest > 0.0 ? std::max(2.0, 0.6 + rest / 115.0) : 0.0));
     if (c >= longest) return 4.0 + walk;
-    return (walks > 1 ? 18.0 : 13.0) + walk + sum * double(c) * std::max(0.9, sums * groups / (walks > 1 ? 310.0 : 250.0)) +
-           std::max(0.12 * parts, 0.026 * sums * groups);
+    const double carry = scanned(int64_t(parts), groups, walks) ? std::max(0.12 * parts, 0.026 * sums * groups)
+                                                                : (walks > 1 ? 1.5 * parts - 5.2 : 1.3 * parts - 4.5);
+    return (walks > 1 ? 18.0 : 13.0) + walk + sum * double(c) * std::max(0.9, sums * groups / (walks > 1 ? 310.0 : 250.0)) + carry;
   };
   int64_t best = std::max<int64_t>(longest, 1);
   for (int64_t c = 1; c < longest; c += std::max<int64_t>(1, c / 8))
@@ -119,6 +126,7 @@ int check_linear(const ufs_linear_desc* d, int walks, lin::Geo* g) {
   const double units = double(d->batch) * d->kv_heads;
   g->chunks = part_chunks(chunks * d->batch, chunks, d->batch, d->kv_heads, walks, g->group);
   g->parts = int32_t((chunks + g->chunks - 1) / g->chunks);
+  g->scanned = scanned(g->parts, units * g->parts, walks);
   if ((units * std::max(g->parts, g->parts > 1 ? lin::kScanSlices : 1) + 8) * 3 > kMostGroups || double(chunks) * g->group > 2.0e9)
     return fail(UF_ERR_ARG, "shape too large: batch * q_heads * tokens");
   return UF_OK;
@@ -179,7 +187,8 @@ int ufs_linear_fwd(const ufs_linear_desc* d, const void* d_q, const void* d_k, c
       p.n = 1;
       p.sum[0] = {src(d_k, d->k), src(d_v, d->v), d_state, starts, 0};
       if (int s = check_hip(lin::launch_linear_parts(p, groups, true, st), "linear attention")) return s;
-      if (int s = check_hip(lin::launch_linear_scan(p, st), "linear attention")) return s;
+      if (a.geo.scanned)
+        if (int s = check_hip(lin::launch_linear_scan(p, st), "linear attention")) return s;
     }
     a.n = 1;
     a.walk[0] = lin::Walk{src(d_q, d->q), src(d_k, d->k), src(d_v, d->v), static_cast<uint16_t*>(d_o), d_state, d_final, starts, 0};
@@ -223,7 +232,8 @@ int ufs_linear_bwd(const ufs_linear_desc* d, const void* d_q, const void* d_k, c
       p.sum[0] = {k, v, d_state, forth, 0};
       p.sum[1] = {q, g, d_dfinal, back, 1};
       if (int s = check_hip(lin::launch_linear_parts(p, groups, exact, st), "linear attention backward")) return s;
-      if (int s = check_hip(lin::launch_linear_scan(p, st), "linear attention backward")) return s;
+      if (a.geo.scanned)
+        if (int s = check_hip(lin::launch_linear_scan(p, st), "linear attention backward")) return s;
     }
     a.n = 3;
     a.walk[0] = lin::Walk{v, g, q, static_cast<uint16_t*>(d_dk), d_dfinal, nullptr, back, 1};
@@ -252,8 +262,7 @@ struct ufs_cache {
   int32_t* table;
   std::vector<int32_t> tokens;  // of each sequence
   std::vector<Entry> step;
-  int32_t step_tokens = 0, step_longest = 0, step_parts = 0;
-  bool step_cut = false;        // some sequence has several parts
+  int32_t step_tokens = 0, step_longest = 0, step_parts = 0, step_most = 0;   // (parts: of all, and of a sequence at most)
   std::vector<uint8_t> seen;    // scratch of the checks, all 0 between calls
 
   bool dry() const { return (d.flags & UF_F_DRYRUN) != 0; }
@@ -306,13 +315,12 @@ void leave_step(ufs_cache* c, int64_t n, const int32_t* seqs) {
   for (int64_t i = 0; i < n; ++i) c->seen[size_t(seqs[i])] = 0;
   if (!found) return;
   c->step.clear();
-  c->step_tokens = c->step_longest = c->step_parts = 0;
-  c->step_cut = false;
+  c->step_tokens = c->step_longest = c->step_parts = c->step_most = 0;
 }
 
 bool few(const ufs_cache* c) { return c->step_longest <= lin::kFewTokens; }
 size_t step_bytes(const ufs_cache* c) {
-  return !few(c) && c->step_cut ? size_t(c->step_parts) * c->d.kv_heads * kStateBytes : 0;
+  return !few(c) && c->step_most > 1 ? size_t(c->step_parts) * c->d.kv_heads * kStateBytes : 0;
 }
 
 }  // namespace
@@ -387,8 +395,7 @@ int ufs_extend(ufs_cache* c, int32_t n, const int32_t* seqs, const int32_t* coun
     std::vector<int32_t> words = {n, int32_t(total), 0, part};
     step.reserve(size_t(n));
     words.reserve(size_t(lin::kHeader) + size_t(n) * lin::kEntry);
-    int32_t at = 0, parts = 0;
-    bool cut = false;
+    int32_t at = 0, parts = 0, most = 0;
     for (int32_t i = 0; i < n; ++i) {
       const int32_t held = c->tokens[size_t(seqs[i])];
       step.push_back(Entry{seqs[i], at, counts[i], held, parts});
@@ -396,10 +403,10 @@ int ufs_extend(ufs_cache* c, int32_t n, const int32_t* seqs, const int32_t* coun
       at += counts[i];
       const int32_t own = (counts[i] + lin::kChunk - 1) / lin::kChunk;   // (counts <= 2^30)
       parts += (own + part - 1) / part;
-      cut = cut || own > part;
+      most = std::max(most, (own + part - 1) / part);
     }
     words[2] = parts;
-    if (double(std::max(parts, cut ? lin::kScanSlices * n : n)) * c->d.kv_heads > kMostGroups) return fail(UF_ERR_ARG, "step too large for one launch");
+    if (double(std::max(parts, most > 1 ? lin::kScanSlices * n : n)) * c->d.kv_heads > kMostGroups) return fail(UF_ERR_ARG, "step too large for one launch");
     if (!c->dry())
       for (size_t k = 0; k < words.size();) {
         tok::PokeArgs a;
@@ -416,7 +423,7 @@ int ufs_extend(ufs_cache* c, int32_t n, const int32_t* seqs, const int32_t* coun
     c->step_tokens = int32_t(total);
     c->step_longest = longest;
     c->step_parts = parts;
-    c->step_cut = cut;
+    c->step_most = most;
     return ok();
   });
 }
@@ -465,6 +472,7 @@ int ufs_attn(const ufs_cache* c, int32_t layer, const ufs_attn_desc* d, const vo
     g.kv_heads = c->d.kv_heads;
     g.group = group;
     g.parts = c->step_parts;
+    g.scanned = scanned(c->step_most, double(c->step_parts) * g.kv_heads, 1);
     g.max_seqs = c->d.max_seqs;
     g.scale = d->scale;
     if (few(c)) {
@@ -486,7 +494,8 @@ int ufs_attn(const ufs_cache* c, int32_t layer, const ufs_attn_desc* d, const vo
       p.n = 1;
       p.sum[0] = {src(d_k, d->k), src(d_v, d->v), states, starts, 0};
       if (int s = check_hip(lin::launch_linear_parts(p, groups, true, st), "linear attention")) return s;
-      if (int s = check_hip(lin::launch_linear_scan(p, st), "linear attention")) return s;
+      if (g.scanned)
+        if (int s = check_hip(lin::launch_linear_scan(p, st), "linear attention")) return s;
     }
     lin::WalkArgs a{};
     a.geo = g;
