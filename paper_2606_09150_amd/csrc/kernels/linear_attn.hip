@@ -170,8 +170,8 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   // M: y-dim 32 mt + 16 (r / 8) + 8 hl + r % 8, z-dim 32 wave + ln
   f32x16 S[4];
   const int zd = 32 * wave + ln;
-  auto get_rows = [&](f32x16& to, const float* from, int mt) {
-    if (trans) {
+  auto get_rows = [&](auto turned, f32x16& to, const float* from, int mt) {
+    if (decltype(turned)::value) {
       from += zd * kD + 8 * hl + 32 * mt;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -186,35 +186,41 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     }
   };
 #pragma unroll
-  for (int mt = 0; mt < 4; ++mt) {
-    S[mt] = f32x16{};
-    if (begin != nullptr) get_rows(S[mt], begin, mt);
-  }
+  for (int mt = 0; mt < 4; ++mt) S[mt] = f32x16{};
   // and the parts that were walked before: each row's place is loaded anew as soon as it is used
-  const int before_me = OUT && sums != nullptr ? (BACK ? p.parts - 1 - p.part : p.part) : 0;
-  if (before_me > 0) {
-    const int64_t stride = int64_t(BACK ? -geo.kv_heads : geo.kv_heads) * kState;
-    const float* at = sums - before_me * stride;
-    const double whole = power_of(geo.decay[h], p.cut * kChunk);
-    double d = BACK ? power_of(geo.decay[h], p.tokens - (p.parts - 1) * p.cut * kChunk) : whole;
-    f32x16 T[4];
+  auto get_state = [&](auto turned) {
+    if (begin != nullptr)
 #pragma unroll
-    for (int mt = 0; mt < 4; ++mt) get_rows(T[mt], at, mt);
+      for (int mt = 0; mt < 4; ++mt) get_rows(turned, S[mt], begin, mt);
+    const int before_me = OUT && sums != nullptr ? (BACK ? p.parts - 1 - p.part : p.part) : 0;
+    if (before_me > 0) {
+      const int64_t stride = int64_t(BACK ? -geo.kv_heads : geo.kv_heads) * kState;
+      const float* at = sums - before_me * stride;
+      const double whole = power_of(geo.decay[h], p.cut * kChunk);
+      double d = BACK ? power_of(geo.decay[h], p.tokens - (p.parts - 1) * p.cut * kChunk) : whole;
+      f32x16 T[4];
+#pragma unroll
+      for (int mt = 0; mt < 4; ++mt) get_rows(turned, T[mt], at, mt);
+      auto add = [&](bool more) {
+        const float hi = float(d), lo = float(d - double(hi));
+        d = whole;
+        at += stride;
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) S[mt][r] = __builtin_fmaf(S[mt][r], hi, __builtin_fmaf(S[mt][r], lo, T[mt][r]));
+          if (more) get_rows(turned, T[mt], at, mt);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
 #pragma unroll 1
-    for (int i = 1;; ++i) {
-      const float hi = float(d), lo = float(d - double(hi));
-      d = whole;
-      at += stride;
-#pragma unroll
-      for (int mt = 0; mt < 4; ++mt) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) S[mt][r] = __builtin_fmaf(S[mt][r], hi, __builtin_fmaf(S[mt][r], lo, T[mt][r]));
-        if (i < before_me) get_rows(T[mt], at, mt);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if (i == before_me) break;
+      for (int i = 1; i < before_me; ++i) add(true);
+      add(false);
     }
-  }
+  };
+  // (either way as a whole: branches between the loads would wait for them one by one)
+  if (trans) get_state(std::true_type{});
+  else get_state(std::false_type{});
 
   // weights
   float* const tab = reinterpret_cast<float*>(smem + kTable);
@@ -548,7 +554,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
 }
 
 template <bool BACK, int PARTS>
-__device__ __forceinline__ void run_walk(const Geo& geo, const Walk& w, int idx, uint8_t* smem) {
+__device__ __forceinline__ void run_walk(const Geo& geo, const Walk& w, bool trans, int idx, uint8_t* smem) {
   const Place p = place(geo, idx);
   if (p.seq < 0) return;
   const size_t at = (size_t(p.seq) * geo.kv_heads + p.h) * kState;
@@ -558,22 +564,22 @@ __device__ __forceinline__ void run_walk(const Geo& geo, const Walk& w, int idx,
   if (start != nullptr && geo.scanned) begin = start;
   else if (p.held && w.first != nullptr) begin = w.first + at;
   if (!geo.scanned) sums = start;
-  walk<BACK, true, PARTS>(geo, p, w.x, w.y, w.z, w.out, begin, sums, w.trans != 0, ends && w.last != nullptr ? w.last + at : nullptr, smem);
+  walk<BACK, true, PARTS>(geo, p, w.x, w.y, w.z, w.out, begin, sums, trans, ends && w.last != nullptr ? w.last + at : nullptr, smem);
 }
 
 __global__ __launch_bounds__(256, 2) void linear_fwd_kernel(WalkArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kShared];
-  run_walk<false, 3>(a.geo, a.walk[0], blockIdx.x, smem);
+  run_walk<false, 3>(a.geo, a.walk[0], false, blockIdx.x, smem);
 }
 
-// dk, dv and dq of eight workgroups' places one after the other: a place's three lie on one XCD, and share their reads there.
+// dk, dv and dq (dk's and dq's M are what is given transposed) of eight workgroups' places one after the other: a place's three lie on one XCD, and share their reads there.
 template <int PARTS>
 __global__ __launch_bounds__(256, 2) void linear_bwd_kernel(WalkArgs a, int groups) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kShared];
   const int b = blockIdx.x / 24, r = blockIdx.x % 24, idx = 8 * b + r % 8;
   if (idx >= groups) return;
-  if (r < 16) run_walk<true, PARTS>(a.geo, a.walk[r / 8], idx, smem);
-  else run_walk<false, 2>(a.geo, a.walk[2], idx, smem);
+  if (r < 16) run_walk<true, PARTS>(a.geo, a.walk[r / 8], r < 8, idx, smem);
+  else run_walk<false, 2>(a.geo, a.walk[2], true, idx, smem);
 }
 
 template <int PARTS>

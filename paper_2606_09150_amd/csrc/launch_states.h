@@ -39,14 +39,14 @@ struct Src {
 };
 
 // out_t = row weight x_t . M + sum of weights (x_t . y_j) z_j, M = sum of key weights y_j z_j^T: forwards over j <= t (o
-// from q, k, v; dq from do, v, k), or backwards over j >= t (dk from v, do, q; dv from k, q, do).
+// from q, k, v; dq from do, v, k), or backwards over j >= t (dk from v, do, q; dv from k, q, do).  dq and dk: first and starts
+// hold M transposed.
 struct Walk {
   Src x, y, z;
   uint16_t* out;
   const float* first;         // M where the walk begins, or null
   float* last;                // M where it ends, or null
   const float* starts;        // M where each part begins (scanned), or the parts' own; null: the only part begins with `first`
-  int32_t trans;              // first and starts hold M transposed
 };
 constexpr int kWalks = 3;
 struct WalkArgs {

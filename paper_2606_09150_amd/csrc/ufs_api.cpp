@@ -191,7 +191,7 @@ int ufs_linear_fwd(const ufs_linear_desc* d, const void* d_q, const void* d_k, c
         if (int s = check_hip(lin::launch_linear_scan(p, st), "linear attention")) return s;
     }
     a.n = 1;
-    a.walk[0] = lin::Walk{src(d_q, d->q), src(d_k, d->k), src(d_v, d->v), static_cast<uint16_t*>(d_o), d_state, d_final, starts, 0};
+    a.walk[0] = lin::Walk{src(d_q, d->q), src(d_k, d->k), src(d_v, d->v), static_cast<uint16_t*>(d_o), d_state, d_final, starts};
     if (int s = check_hip(lin::launch_linear_fwd(a, groups, st), "linear attention")) return s;
     return ok();
   });
@@ -236,9 +236,9 @@ int ufs_linear_bwd(const ufs_linear_desc* d, const void* d_q, const void* d_k, c
         if (int s = check_hip(lin::launch_linear_scan(p, st), "linear attention backward")) return s;
     }
     a.n = 3;
-    a.walk[0] = lin::Walk{v, g, q, static_cast<uint16_t*>(d_dk), d_dfinal, nullptr, back, 1};
-    a.walk[1] = lin::Walk{k, q, g, static_cast<uint16_t*>(d_dv), d_dfinal, d_dstate, back, 0};
-    a.walk[2] = lin::Walk{g, v, k, static_cast<uint16_t*>(d_dq), d_state, nullptr, forth, 1};
+    a.walk[0] = lin::Walk{v, g, q, static_cast<uint16_t*>(d_dk), d_dfinal, nullptr, back};
+    a.walk[1] = lin::Walk{k, q, g, static_cast<uint16_t*>(d_dv), d_dfinal, d_dstate, back};
+    a.walk[2] = lin::Walk{g, v, k, static_cast<uint16_t*>(d_dq), d_state, nullptr, forth};
     if (int s = check_hip(lin::launch_linear_bwd(a, groups, exact, st), "linear attention backward")) return s;
     return ok();
   });
@@ -500,7 +500,7 @@ int ufs_attn(const ufs_cache* c, int32_t layer, const ufs_attn_desc* d, const vo
     lin::WalkArgs a{};
     a.geo = g;
     a.n = 1;
-    a.walk[0] = lin::Walk{src(d_q, d->q), src(d_k, d->k), src(d_v, d->v), static_cast<uint16_t*>(d_o), states, states, starts, 0};
+    a.walk[0] = lin::Walk{src(d_q, d->q), src(d_k, d->k), src(d_v, d->v), static_cast<uint16_t*>(d_o), states, states, starts};
     if (int s = check_hip(lin::launch_linear_fwd(a, groups, st), "linear attention")) return s;
     return ok();
   });
