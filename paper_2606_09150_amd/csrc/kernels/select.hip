@@ -28,6 +28,7 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr int kEach = 16;                              // values of a lane and block
 constexpr int kBlock = 64 * kEach;                     // of a wave and block
 constexpr int kRoom = kBlock + 128, kMine = kRoom / 64;   // keys of a wave's list; of a lane
+constexpr int kSplits = 32;                            // slices of a row at most
 constexpr int kFew = 128;                              // keys of a list that are put in order by counting
 constexpr float kLog2e = 1.44269504f;
 constexpr uint32_t kNone = 0x007fffffu;                // -inf in the order of integers: nothing at or below it is taken
@@ -67,12 +68,14 @@ struct List {
   __device__ void begin(uint32_t top) {
     bar = max(nth(n, 16, [&](uint32_t c) { return int(__popcll(__ballot(top >= c))); }), kNone + 1) - 1;
   }
-  __device__ void push(uint32_t order, uint32_t place) {
+  // Whether any of them passed.
+  __device__ bool push(uint32_t order, uint32_t place) {
     const bool in = order > bar;
     const uint64_t mask = __ballot(in);
-    if (mask == 0) return;
+    if (mask == 0) return false;
     if (in) keys[count + below_me(mask)] = (uint64_t(order) << 32) | uint32_t(~place);
     count += __popcll(mask);
+    return true;
   }
   // The bar up to the n-th largest of the list's values (2^-13 below it at most), and what is below it out of the list.
   __device__ void raise() {
@@ -314,30 +317,48 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
   auto slice_at = [&](int i) { return work + size_t(i) * slice_bytes(a.k); };
   const int n = listed_of(a.k), slices = W * a.splits, listed = slices * n;
 
-  // the first of this thread's entries of the lists come while the sums are joined
+  // A wave takes a quarter of the slices, their first entries before their second ones and so on: none of a slice's passes once one
+  // has not, so that it is through when none of as many as it has slices did.  The first of them come while the sums are joined.
   constexpr int kHeld = 4;
+  const int own = (slices + kWaves - 1) / kWaves;
   uint64_t held[kHeld];
-  auto entry = [&](int i) { return i < listed ? reinterpret_cast<const uint64_t*>(slice_at(i / n) + 16)[i % n] : 0; };
+  int from[kHeld];
+  auto fetch = [&](int i0) {
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) held[i] = entry(tid + i * kThreads);
-  if (tid < W) {
-    const float score = a.scores[g * W + tid];
-    int kind = score > -INFINITY ? 1 : 0;
-    if (a.done != nullptr && a.done[g * W + tid] != 0) kind *= 2;
-    float lse = 0.f;
-    if (kind == 1) {
-      float top = -INFINITY;
-      for (int i = 0; i < a.splits; ++i) top = fmaxf(top, *reinterpret_cast<const float*>(slice_at(tid * a.splits + i)));
-      double sum = 0.0;
-      for (int i = 0; i < a.splits; ++i) {
-        const float2 t = *reinterpret_cast<const float2*>(slice_at(tid * a.splits + i));
-        sum += t.y != 0.f ? double(t.y * __builtin_amdgcn_exp2f((t.x - top) * kLog2e)) : 0.0;
-      }
-      lse = float(double(top) + log(sum));
+    for (int u = 0; u < kHeld; ++u) {
+      const int i = i0 + lane + 64 * u, level = i / own;
+      from[u] = (i - level * own) * kWaves + wave;
+      held[u] = level < n && from[u] < slices ? reinterpret_cast<const uint64_t*>(slice_at(from[u]) + 16)[level] : 0;
     }
-    slse[tid] = lse;
-    sscore[tid] = score;
-    skind[tid] = uint8_t(kind);
+  };
+  fetch(0);
+  // eight lanes a row
+  for (int w0 = 0; w0 < W; w0 += kThreads / 8) {
+    const int w = w0 + tid / 8, part = tid % 8;
+    const float score = w < W ? a.scores[g * W + w] : -INFINITY;
+    int kind = score > -INFINITY ? 1 : 0;
+    if (w < W && a.done != nullptr && a.done[g * W + w] != 0) kind *= 2;
+    float2 t[kSplits / 8];
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kSplits / 8; ++i) {
+      t[i] = make_float2(-INFINITY, 0.f);
+      if (kind == 1 && part + 8 * i < a.splits) t[i] = *reinterpret_cast<const float2*>(slice_at(w * a.splits + part + 8 * i));
+    }
+#pragma unroll
+    for (int i = 0; i < kSplits / 8; ++i) top = fmaxf(top, t[i].x);
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kSplits / 8; ++i) sum += t[i].y != 0.f ? double(t[i].y * __builtin_amdgcn_exp2f((t[i].x - top) * kLog2e)) : 0.0;
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor(sum, d);
+    if (part == 0 && w < W) {
+      slse[w] = kind == 1 ? float(double(top) + log(sum)) : 0.f;
+      sscore[w] = score;
+      skind[w] = uint8_t(kind);
+    }
   }
   __syncthreads();
   auto score_of = [&](int w, float logit) { return sscore[w] + (logit - slse[w]); };   // (float32 each)
@@ -351,10 +372,10 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
     const float x = value_of(uint32_t(last >> 32)), score = score_of(w, x);
     return order_of(score) > kNone && order_of(score) >= limit && score_of(w, L::below(x)) == score;
   };
-  // Entry i of the lists as a candidate: its score, and its place.
-  auto candidate = [&](int i, uint64_t key, uint32_t* place) {
-    const int w = i / n / a.splits;
-    if (i >= listed || skind[w] != 1 || uint32_t(key >> 32) <= kNone) return 0u;
+  // An entry of a slice as a candidate: its score, and its place.
+  auto candidate = [&](int slice, uint64_t key, uint32_t* place) {
+    const int w = min(slice / a.splits, W - 1);
+    if (uint32_t(key >> 32) <= kNone || skind[w] != 1) return 0u;
     *place = uint32_t(w) * uint32_t(a.vocab) + uint32_t(~uint32_t(key));
     return order_of(score_of(w, value_of(uint32_t(key >> 32))));
   };
@@ -368,19 +389,21 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
 
   {
     List list(s.keys[wave], a.k, false);
-    uint32_t place = 0, order[kHeld], places[kHeld], top = 0;
+    uint32_t order[kHeld], places[kHeld];
+    int last = 0;                                      // behind the last that passed
+    for (int i0 = 0; i0 < n * own && i0 - last < own; i0 += 64 * kHeld) {
+      if (i0 > 0) fetch(i0);
+      uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-      order[i] = candidate(tid + i * kThreads, held[i], &places[i]);
-      top = max(top, order[i]);
-    }
-    list.begin(top);
+      for (int u = 0; u < kHeld; ++u) {
+        order[u] = candidate(from[u], held[u], &places[u]);
+        top = max(top, order[u]);
+      }
+      if (i0 == 0) list.begin(top);
+      list.room(64 * kHeld, false);
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) list.push(order[i], places[i]);
-    for (int i0 = kHeld * kThreads; i0 < listed; i0 += kThreads) {
-      const uint32_t o = candidate(i0 + tid, entry(i0 + tid), &place);
-      list.room(64, false);
-      list.push(o, place);
+      for (int u = 0; u < kHeld; ++u)
+        if (list.push(order[u], places[u])) last = i0 + 64 * (u + 1);
     }
     finished(list);
     list.raise();
@@ -393,7 +416,8 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
     List list(s.keys[wave], a.k, false);
     for (int i0 = 0; i0 < listed; i0 += kThreads) {
       const int i = i0 + tid;
-      uint32_t place = 0, o = candidate(i, entry(i), &place);
+      uint32_t place = 0, o = 0;
+      if (i < listed) o = candidate(i / n, reinterpret_cast<const uint64_t*>(slice_at(i / n) + 16)[i % n], &place);
       if (o != 0 && again(i / n, limit)) o = 0;
       list.room(64, false);
       list.push(o, place);
@@ -442,7 +466,7 @@ void plan_select(SelectArgs* a) {
   const int e = a->type == UFS_FP32 ? 4 : 8, block = kWaves * kBlock / e;
   const int64_t vectors = (int64_t(a->vocab) + e - 1) / e, rows = int64_t(a->groups) * a->beams;
   const int64_t blocks = (vectors + block - 1) / block;
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({blocks, 32, (1024 + rows - 1) / rows}));
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({blocks, kSplits, (1024 + rows - 1) / rows}));
   a->slice = int32_t((blocks + splits - 1) / splits * block);
   a->splits = int32_t((vectors + a->slice - 1) / a->slice);
 }
