@@ -64,9 +64,20 @@ struct List {
   uint32_t bar = kNone;                                // values above it pass
 
   __device__ List(uint64_t* keys_, int n_, bool ascending_) : keys(keys_), n(n_), ascending(ascending_) {}
-  // A bar that at least n of the values in `top`, one a lane, are above.
-  __device__ void begin(uint32_t top) {
-    bar = max(nth(n, 16, [&](uint32_t c) { return int(__popcll(__ballot(top >= c))); }), kNone + 1) - 1;
+  // A bar that at least n of the values in a and b, one a lane each, are above.
+  __device__ void begin(uint32_t a, uint32_t b) {
+    bar = max(nth(n, 16, [&](uint32_t c) { return int(__popcll(__ballot(a >= c))) + int(__popcll(__ballot(b >= c))); }), kNone + 1) - 1;
+  }
+  // Places for `mine` keys of this lane, 31 at most: the first one.
+  __device__ int claim(int mine) {
+    int at = count;
+#pragma unroll
+    for (int b = 0; b < 5; ++b) {
+      const uint64_t mask = __ballot((mine >> b) & 1);
+      at += below_me(mask) << b;
+      count += __popcll(mask) << b;
+    }
+    return at;
   }
   // Whether any of them passed.
   __device__ bool push(uint32_t order, uint32_t place) {
@@ -111,7 +122,7 @@ struct List {
   }
   // Room for the next block, which may all pass; `now`: the bar in any case.
   __device__ void room(int most, bool now) {
-    if (!now && count <= seen + 64 && count + most <= kRoom) return;
+    if (!now && count <= seen + 2 * n + 32 && count + most <= kRoom) return;
     raise();
     if (count + most > kRoom) cut();
   }
@@ -250,11 +261,12 @@ __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
     float y[kVectors][kE];
 #pragma unroll
     for (int u = 0; u < kVectors; ++u) L::unpack(bits[u], y[u]);
-    float most = -INFINITY;
+    float half[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int u = 0; u < kVectors; ++u)
 #pragma unroll
-      for (int e = 0; e < kE; ++e) most = fmaxf(most, y[u][e]);
+      for (int e = 0; e < kE; ++e) half[2 * u / kVectors] = fmaxf(half[2 * u / kVectors], y[u][e]);
+    const float most = fmaxf(half[0], half[1]);
     if (most > top) {
       sum *= __builtin_amdgcn_exp2f((top - most) * kLog2e);
       top = most;
@@ -266,15 +278,21 @@ __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
 #pragma unroll
       for (int e = 0; e < kE; ++e) part[e & 3] += __builtin_amdgcn_exp2f((y[u][e] - off) * kLog2e);
     sum += (part[0] + part[1]) + (part[2] + part[3]);
-    if (v == v0) list.begin(ordered(most));
+    if (v == v0) list.begin(ordered(half[0]), ordered(half[1]));
     // the bar as a value: -inf where all pass; the place between 0 and the largest value below it is no other value's
     const float bar = value_of(list.bar == 0x7fffffffu ? 0x7ffffffeu : list.bar);
     if (__ballot(most > bar) != 0) {
+      int passed = 0;
+#pragma unroll
+      for (int u = 0; u < kVectors; ++u)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) passed += y[u][e] > bar;
+      uint64_t* to = list.keys + list.claim(passed);
 #pragma unroll
       for (int u = 0; u < kVectors; ++u)
 #pragma unroll
         for (int e = 0; e < kE; ++e)
-          if (__ballot(y[u][e] > bar) != 0) list.push(ordered(y[u][e]), uint32_t((v + 64 * u + lane) * kE + e));
+          if (y[u][e] > bar) *to++ = (uint64_t(ordered(y[u][e])) << 32) | uint32_t(~uint32_t((v + 64 * u + lane) * kE + e));
     }
     list.room(kBlock, v + step >= v1 && list.count > max(2 * list.n, 24));
   };
@@ -393,13 +411,13 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
     int last = 0;                                      // behind the last that passed
     for (int i0 = 0; i0 < n * own && i0 - last < own; i0 += 64 * kHeld) {
       if (i0 > 0) fetch(i0);
-      uint32_t top = 0;
+      uint32_t top[2] = {0, 0};
 #pragma unroll
       for (int u = 0; u < kHeld; ++u) {
         order[u] = candidate(from[u], held[u], &places[u]);
-        top = max(top, order[u]);
+        top[2 * u / kHeld] = max(top[2 * u / kHeld], order[u]);
       }
-      if (i0 == 0) list.begin(top);
+      if (i0 == 0) list.begin(top[0], top[1]);
       list.room(64 * kHeld, false);
 #pragma unroll
       for (int u = 0; u < kHeld; ++u)
