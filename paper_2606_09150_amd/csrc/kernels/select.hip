@@ -15,6 +15,7 @@
 // first of the first block's, later of the list's (n values are at or above it, and what comes
 // later has a higher place).  A list that might not hold the next block is cut down to its n largest.
 #include <algorithm>
+#include <type_traits>
 
 #include "../launch_states.h"
 
@@ -42,13 +43,28 @@ __device__ inline float value_of(uint32_t o) { return __uint_as_float(o ^ (uint3
 __device__ inline int below_me(uint64_t mask) {        // lanes of the mask before this one
   return __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
 }
-// A t that n values are at or above, the largest whose last `rest` bits are 0, bit by bit; `above` counts them over the wave.  (Loops over bits stay loops
-// here: a workgroup goes through this code once, and waits for every line of it to be fetched.)
+// The largest of the lanes' values.
+__device__ inline uint32_t wave_max(uint32_t x) {
+  auto step = [&](auto control) {
+    x = max(x, uint32_t(__builtin_amdgcn_update_dpp(0, int(x), decltype(control)::value, 0xf, 0xf, false)));
+  };
+  step(std::integral_constant<int, 0x111>{});       // from 1, 2, 4 and 8 lanes below in a row of 16
+  step(std::integral_constant<int, 0x112>{});
+  step(std::integral_constant<int, 0x114>{});
+  step(std::integral_constant<int, 0x118>{});
+  const uint32_t a = __builtin_amdgcn_readlane(x, 15), b = __builtin_amdgcn_readlane(x, 31), c = __builtin_amdgcn_readlane(x, 47),
+                 d = __builtin_amdgcn_readlane(x, 63);
+  return max(max(a, b), max(c, d));
+}
+// A t that n values are at or above, the largest whose last `rest` bits are 0, bit by bit from the first in which `low` and `high` differ: the
+// n-th largest lies between them, or there are fewer than n above `low`, and t is at most `low`.  `above` counts over the wave.
+// (Loops over bits stay loops here: a workgroup goes through this code once, and waits for every line of it to be fetched.)
 template <class Above>
-__device__ inline uint32_t nth(int n, int rest, Above above) {
-  uint32_t t = 0;
+__device__ inline uint32_t nth(int n, uint32_t low, uint32_t high, int rest, Above above) {
+  const int first = low == high ? -1 : 31 - __clz(low ^ high);
+  uint32_t t = first < 0 ? low : first == 31 ? 0 : low >> (first + 1) << (first + 1);
 #pragma unroll 1
-  for (int bit = 31; bit >= rest; --bit) {
+  for (int bit = first; bit >= rest; --bit) {
     const uint32_t c = t | (1u << bit);
     if (above(c) >= n) t = c;
   }
@@ -60,13 +76,15 @@ struct List {
   uint64_t* keys;
   int n;
   bool ascending;                                      // blocks come in the order of their places
+  int rest;                                            // last bits that bars do not go by
   int count = 0, seen = 0;                             // keys; of them when the bar was last raised
   uint32_t bar = kNone;                                // values above it pass
 
-  __device__ List(uint64_t* keys_, int n_, bool ascending_) : keys(keys_), n(n_), ascending(ascending_) {}
+  __device__ List(uint64_t* keys_, int n_, bool ascending_, int rest_) : keys(keys_), n(n_), ascending(ascending_), rest(rest_) {}
   // A bar that at least n of the values in a and b, one a lane each, are above.
   __device__ void begin(uint32_t a, uint32_t b) {
-    bar = max(nth(n, 16, [&](uint32_t c) { return int(__popcll(__ballot(a >= c))) + int(__popcll(__ballot(b >= c))); }), kNone + 1) - 1;
+    const uint32_t low = ~wave_max(~min(a, b)), high = wave_max(max(a, b));
+    bar = max(nth(n, low, high, rest, [&](uint32_t c) { return int(__popcll(__ballot(a >= c))) + int(__popcll(__ballot(b >= c))); }), kNone + 1) - 1;
   }
   // Places for `mine` keys of this lane, 31 at most: the first one.
   __device__ int claim(int mine) {
@@ -88,13 +106,19 @@ struct List {
     count += __popcll(mask);
     return true;
   }
-  // The bar up to the n-th largest of the list's values (2^-13 below it at most), and what is below it out of the list.
+  // The bar up to the n-th largest of the list's values, but for its last bits, and what is below it out of the list.
   __device__ void raise() {
     const int lane = threadIdx.x & 63, m = (count + 63) / 64;
     uint32_t mine[kMine];
+    uint32_t high = bar;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) mine[i] = lane + 64 * i < count ? uint32_t(keys[lane + 64 * i] >> 32) : 0;
-    const uint32_t t = nth(n, 10, [&](uint32_t c) {
+    for (int i = 0; i < kMine; ++i) {
+      mine[i] = 0;
+      if (i >= m) break;
+      if (lane + 64 * i < count) mine[i] = uint32_t(keys[lane + 64 * i] >> 32);
+      high = max(high, mine[i]);
+    }
+    const uint32_t t = nth(n, bar, wave_max(high), rest, [&](uint32_t c) {
       int found = 0;
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
@@ -153,25 +177,41 @@ struct Shared {
 };
 __device__ inline void join(Shared& s, List& list) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  // what is below any wave's n-th largest is left out
-  if (lane == 0) s.low[wave] = list.bar;
-  __syncthreads();
-  const uint32_t low = max(max(s.low[0], s.low[1]), max(s.low[2], s.low[3]));
-  uint64_t* const keys = s.keys[wave];
-  list.keep(uint64_t(low) << 32);                      // (a list's own n-th may equal its bar)
-  if (list.count > kFew) list.cut();
-  if (lane == 0) s.count[wave] = list.count;
+  if (lane == 0) s.low[wave] = list.bar, s.count[wave] = list.count;
   for (int i = threadIdx.x; i < list.n; i += kThreads) s.out[i] = 0;
   __syncthreads();
-  for (int i = lane; i < list.count; i += 64) {
-    const uint64_t mine = keys[i];
-    int rank = 0;
+  // what is below any wave's n-th largest is left out (a list's own n-th may equal its bar)
+  const uint32_t low = max(max(s.low[0], s.low[1]), max(s.low[2], s.low[3]));
+  const bool many = s.count[0] > kFew || s.count[1] > kFew || s.count[2] > kFew || s.count[3] > kFew;
+  if (many) {
+    list.keep(uint64_t(low) << 32);
+    if (list.count > kFew) list.cut();
+    if (lane == 0) s.count[wave] = list.count;
+    __syncthreads();
+  }
+  if (wave == 0) {                                     // the others' into the first list
+    list.keep(uint64_t(low) << 32);
+    list.bar = low - 1;
 #pragma unroll 1
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 1; w < kWaves; ++w) {
       const int c = s.count[w];
-#pragma unroll 4
-      for (int k = 0; k < c; ++k) rank += s.keys[w][k] > mine;
+#pragma unroll 1
+      for (int i = lane; i - lane < c; i += 64) {
+        const uint64_t key = i < c ? s.keys[w][i] : 0;
+        list.push(uint32_t(key >> 32), ~uint32_t(key));
+      }
     }
+    if (list.count > kFew) list.raise();
+    if (list.count > kFew) list.cut();
+    if (lane == 0) s.count[0] = list.count;
+  }
+  __syncthreads();
+  const int all = s.count[0];                          // (at most kFew)
+  if (int(threadIdx.x) < all) {
+    const uint64_t mine = s.keys[0][threadIdx.x];
+    int rank = 0;
+#pragma unroll 8
+    for (int k = 0; k < all; ++k) rank += s.keys[0][k] > mine;
     if (rank < list.n) s.out[rank] = mine;
   }
   __syncthreads();
@@ -182,6 +222,7 @@ __device__ inline void join(Shared& s, List& list) {
 template <int TYPE>
 struct Logits {
   static constexpr int kSize = TYPE == UFS_FP32 ? 4 : 2, kE = 16 / kSize;
+  static constexpr int kRest = TYPE == UFS_BF16 ? 16 : TYPE == UFS_FP16 ? 13 : 10;   // last bits: none of the type, or 2^-13
   const uint8_t* row;
   int vocab;
   __device__ Logits(const SelectArgs& a, int w, int g) {
@@ -250,7 +291,7 @@ __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
   const int v1 = min((split + 1) * a.slice, (a.vocab + kE - 1) / kE), step = kWaves * 64 * kVectors;
   const int v0 = split * a.slice + wave * 64 * kVectors;
 
-  List list(s.keys[wave], listed_of(a.k), true);
+  List list(s.keys[wave], listed_of(a.k), true, L::kRest);
   float top = -INFINITY, sum = 0.f;
   uint4 next[2][kVectors];                             // two blocks ahead
   auto fetch = [&](uint4 (&to)[kVectors], int v) {
@@ -341,7 +382,7 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
   const int own = (slices + kWaves - 1) / kWaves;
   uint64_t held[kHeld];
   int from[kHeld];
-  auto fetch = [&](int i0) {
+  auto fetch = [&](uint64_t (&held)[kHeld], int (&from)[kHeld], int i0) {
 #pragma unroll
     for (int u = 0; u < kHeld; ++u) {
       const int i = i0 + lane + 64 * u, level = i / own;
@@ -349,7 +390,7 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
       held[u] = level < n && from[u] < slices ? reinterpret_cast<const uint64_t*>(slice_at(from[u]) + 16)[level] : 0;
     }
   };
-  fetch(0);
+  fetch(held, from, 0);
   // eight lanes a row
   for (int w0 = 0; w0 < W; w0 += kThreads / 8) {
     const int w = w0 + tid / 8, part = tid % 8;
@@ -406,11 +447,13 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
   };
 
   {
-    List list(s.keys[wave], a.k, false);
+    List list(s.keys[wave], a.k, false, 10);
     uint32_t order[kHeld], places[kHeld];
     int last = 0;                                      // behind the last that passed
     for (int i0 = 0; i0 < n * own && i0 - last < own; i0 += 64 * kHeld) {
-      if (i0 > 0) fetch(i0);
+      uint64_t next[kHeld];
+      int next_from[kHeld];
+      fetch(next, next_from, i0 + 64 * kHeld);
       uint32_t top[2] = {0, 0};
 #pragma unroll
       for (int u = 0; u < kHeld; ++u) {
@@ -422,6 +465,8 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
 #pragma unroll
       for (int u = 0; u < kHeld; ++u)
         if (list.push(order[u], places[u])) last = i0 + 64 * (u + 1);
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u) held[u] = next[u], from[u] = next_from[u];
     }
     finished(list);
     list.raise();
@@ -431,7 +476,7 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
   int reads = 0;
   for (int i = tid; i < slices; i += kThreads) reads |= again(i, limit);
   if (__syncthreads_or(reads)) {                       // those slices by their scores, and the others' lists
-    List list(s.keys[wave], a.k, false);
+    List list(s.keys[wave], a.k, false, 10);
     for (int i0 = 0; i0 < listed; i0 += kThreads) {
       const int i = i0 + tid;
       uint32_t place = 0, o = 0;
