@@ -45,6 +45,7 @@ using tok::lds_row;
 using tok::lds_tr2;
 using tok::swz_k;
 
+constexpr int kThreads = 512;
 constexpr uint32_t kTile = 8192, kHalf = 4096, kStage = 3 * kTile;
 constexpr int kStages = 3;
 // LDS behind the stages: P, a row of 32 values in two parts (and 16 bytes, so that rows begin in banks of their own) for each
@@ -113,13 +114,13 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
                                      const float* begin, const float* sums, bool trans, float* last, uint8_t* smem) {
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lane = tid & 63, hl = lane >> 5, ln = lane & 31, rp = lane & 15, gr = (lane >> 4) & 1;
+  const int lane = tid & 63, q = lane >> 4, rp = lane & 15;
   const int h = p.h, G = geo.group;
   const int rest = min(kChunk, p.tokens - (p.chunk0 + p.chunks - 1) * kChunk);   // tokens of the part's last chunk (by time)
   const uint32_t lds0 = lds_addr(smem);
 
-  // copies: rows 8 wave + lane / 8 of each tile
-  const int crow = 8 * wave + (lane >> 3);
+  // copies: rows 8 (wave % 4) + lane / 8 of a half of each tile
+  const int crow = 8 * (wave & 3) + (lane >> 3), half = wave >> 2;
   const uint32_t cchunk = uint32_t(16 * ((lane & 7) ^ swz_k(crow & 15)));
   const int heads = OUT || BACK ? G : 1;               // items of a chunk
   constexpr bool kDown = OUT == BACK;                  // from the last chunk to the first
@@ -133,21 +134,18 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     Tile t;
     const int first = kDown ? p.chunk0 + p.chunks - 1 : p.chunk0;
     t.at = uniform_ptr(reinterpret_cast<const uint8_t*>(src.p + (geo.step == nullptr ? int64_t(p.seq) * src.batch : 0) +
-                                                        (p.row + first * kChunk) * src.token + int64_t(grouped ? h * G : h) * src.head));
+                                                        (p.row + first * kChunk) * src.token + int64_t(grouped ? h * G : h) * src.head + 64 * half));
     t.head = grouped ? 2 * src.head : 0;
     t.token = int32_t(2 * src.token);                  // (at most 2^25)
     return t;
   };
   Tile tx = OUT ? tile(xs, !BACK) : Tile{}, ty = tile(ys, BACK), tz = tile(zs, BACK);
   int next_t = (kDown ? p.chunk0 + p.chunks - 1 : p.chunk0) * kChunk, next_c = 0, next_g = 0;   // the next item to copy
+  const uint32_t mine = uint32_t(half) * kHalf + uint32_t(wave & 3) * 1024u;   // of a tile
   auto issue = [&](uint32_t stage) {
     const int row = min(crow, p.tokens - 1 - next_t);
-    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + stage * kStage + uint32_t(wave) * 1024u);
-    auto copy = [&](const Tile& t, uint32_t at) {
-      const uint32_t off = uint32_t(row) * uint32_t(t.token) + cchunk;
-      dma16(t.at, off, dst + at);
-      dma16(t.at + 128, off, dst + at + kHalf);
-    };
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + stage * kStage + mine);
+    auto copy = [&](const Tile& t, uint32_t at) { dma16(t.at, uint32_t(row) * uint32_t(t.token) + cchunk, dst + at); };
     if (OUT) copy(tx, 0);
     copy(ty, kTile);
     copy(tz, 2 * kTile);
@@ -167,49 +165,41 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     issue(1);
   }
 
-  // M: y-dim 32 mt + 16 (r / 8) + 8 hl + r % 8, z-dim 32 wave + ln
-  f32x16 S[4];
-  const int zd = 32 * wave + ln;
-  auto get_rows = [&](auto turned, f32x16& to, const float* from, int mt) {
-    if (decltype(turned)::value) {
-      from += zd * kD + 8 * hl + 32 * mt;
+  // M: y-dim 32 (b / 2) + 8 q + 4 (b % 2) + r, z-dim 16 wave + rp
+  f32x4 S[8];
+  const int zd = 16 * wave + rp;
+  auto get_rows = [&](auto turned, f32x4& to, const float* from, int b) {
+    const int y = 32 * (b >> 1) + 8 * q + 4 * (b & 1);
+    if (decltype(turned)::value) to = *reinterpret_cast<const f32x4*>(from + zd * kD + y);
+    else
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(from + 16 * (i >> 1) + 4 * (i & 1));
-#pragma unroll
-        for (int r = 0; r < 4; ++r) to[4 * i + r] = x[r];
-      }
-    } else {
-      from += (8 * hl + 32 * mt) * kD + zd;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) to[r] = from[(16 * (r >> 3) + (r & 7)) * kD];
-    }
+      for (int r = 0; r < 4; ++r) to[r] = from[(y + r) * kD + zd];
   };
 #pragma unroll
-  for (int mt = 0; mt < 4; ++mt) S[mt] = f32x16{};
+  for (int b = 0; b < 8; ++b) S[b] = f32x4{};
   // and the parts that were walked before: each row's place is loaded anew as soon as it is used
   auto get_state = [&](auto turned) {
     if (begin != nullptr)
 #pragma unroll
-      for (int mt = 0; mt < 4; ++mt) get_rows(turned, S[mt], begin, mt);
+      for (int b = 0; b < 8; ++b) get_rows(turned, S[b], begin, b);
     const int before_me = OUT && sums != nullptr ? (BACK ? p.parts - 1 - p.part : p.part) : 0;
     if (before_me > 0) {
       const int64_t stride = int64_t(BACK ? -geo.kv_heads : geo.kv_heads) * kState;
       const float* at = sums - before_me * stride;
       const double whole = power_of(geo.decay[h], p.cut * kChunk);
       double d = BACK ? power_of(geo.decay[h], p.tokens - (p.parts - 1) * p.cut * kChunk) : whole;
-      f32x16 T[4];
+      f32x4 T[8];
 #pragma unroll
-      for (int mt = 0; mt < 4; ++mt) get_rows(turned, T[mt], at, mt);
+      for (int b = 0; b < 8; ++b) get_rows(turned, T[b], at, b);
       auto add = [&](bool more) {
         const float hi = float(d), lo = float(d - double(hi));
         d = whole;
         at += stride;
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
+        for (int b = 0; b < 8; ++b) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) S[mt][r] = __builtin_fmaf(S[mt][r], hi, __builtin_fmaf(S[mt][r], lo, T[mt][r]));
-          if (more) get_rows(turned, T[mt], at, mt);
+          for (int r = 0; r < 4; ++r) S[b][r] = __builtin_fmaf(S[b][r], hi, __builtin_fmaf(S[b][r], lo, T[b][r]));
+          if (more) get_rows(turned, T[b], at, b);
           __builtin_amdgcn_sched_barrier(0);
         }
       };
@@ -248,71 +238,57 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   const double dp = period == kPeriod ? dw4 : dw;
   const float whole_hi = float(dp), whole_lo = float(dp - double(whole_hi)), rest_dec = float(power(max(rest, 0)));
   meet_lds();                                          // (M and the first copies are on their way)
-  // P: this wave's quarter, x_t.y_j for j = pj .. pj + 3 and t = pt
-  const int pq = lane >> 4, pj = 16 * (wave >> 1) + 4 * pq, pt = 16 * (wave & 1) + rp;
+  // P: a quarter for each of the first four waves, x_t.y_j for j = pj .. pj + 3 and t = pt
+  const bool scores = OUT && wave < 4;
+  const int pj = 16 * (wave >> 1) + 4 * q, pt = 16 * (wave & 1) + rp;
   float pw[4];
   bool seen[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int age = BACK ? pj + r - pt : pt - pj - r;
-    pw[r] = scale * tab[max(age, 0)];
+    pw[r] = scale * tab[min(max(age, 0), 32)];
     seen[r] = age >= 0;
   }
-  const float row_whole = BACK ? tab[31 - ln] : scale * tab[ln + 1];
-  const float row_rest = BACK ? tab[max(rest - 1 - ln, 0)] : row_whole;
-
-  // operand addresses within a stage
-  uint32_t kr[4], yt[2][2], zt[2], py[2], px[2], put[4];   // (of the present stage)
+  float row_whole[2], row_rest[2];                     // of tokens rp and 16 + rp
 #pragma unroll
-  for (int k = 0; k < 4; ++k) kr[k] = lds0 + uint32_t(ln * 128 + 16 * ((2 * k + hl) ^ swz_k(ln & 15)));
-#pragma unroll
-  for (int hh = 0; hh < 2; ++hh) {
-    const int r = 8 * hh + 4 * hl + (rp >> 2);
-#pragma unroll
-    for (int m = 0; m < 2; ++m)                        // (units of four dimensions with bits 2 and 3 swapped)
-      yt[hh][m] = lds0 + kTile + uint32_t(r * 128 + 16 * ((4 * m + 2 * gr + (rp & 1)) ^ swz_k(r)) + 8 * ((rp >> 1) & 1));
-    zt[hh] = lds0 + 2 * kTile + uint32_t(wave >> 1) * kHalf +
-             uint32_t(r * 128 + 16 * ((4 * (wave & 1) + 2 * gr + ((rp >> 1) & 1)) ^ swz_k(r)) + 8 * (rp & 1));
+  for (int tb = 0; tb < 2; ++tb) {
+    const int t = 16 * tb + rp;
+    row_whole[tb] = BACK ? tab[31 - t] : scale * tab[t + 1];
+    row_rest[tb] = BACK ? tab[max(rest - 1 - t, 0)] : row_whole[tb];
   }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {                        // rows 16 .. of Y and X, dims 32 k + 8 pq ..
-    const uint32_t c = 16 * ((4 * k + pq) ^ swz_k(rp));
-    py[k] = lds0 + kTile + uint32_t((16 * (wave >> 1) + rp) * 128) + c;
-    px[k] = lds0 + uint32_t((16 * (wave & 1) + rp) * 128) + c;
-  }
-  // P's places of j within 16 have bits 2 and 3 swapped, as the k-slots of Z^T
-  const uint32_t pput = lds0 + kP + uint32_t(pt) * kRow + 2 * (16 * (wave >> 1) + 4 * (2 * (pq & 1) + (pq >> 1)));
-  const uint32_t pget = lds0 + kP + uint32_t(ln) * kRow + 16 * hl;
-  const uint32_t kwt = lds0 + kTable + 4 * (kPowers + 4 * hl);
 
-  f32x16 os = f32x16{}, op = f32x16{};                  // O^T: of M, without the row's weight, and of P
+  // operand addresses within a stage (16 rows further: 2,048 bytes)
+  uint32_t px[2], yt[2], zt, put;                      // (of the present stage)
+  const int r0 = 4 * q + (rp >> 2);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    px[k] = lds0 + uint32_t(rp * 128 + 16 * ((4 * k + q) ^ swz_k(rp)));
+    yt[k] = lds0 + kTile + uint32_t(r0 * 128 + 16 * ((4 * k + (rp & 3)) ^ swz_k(r0)));
+  }
+  zt = lds0 + 2 * kTile + uint32_t(half) * kHalf + uint32_t(r0 * 128 + 16 * ((2 * (wave & 3) + ((rp >> 1) & 1)) ^ swz_k(r0)) + 8 * (rp & 1));
+  const uint32_t py_at = kTile + 2048 * uint32_t((wave >> 1) & 1), px_at = 2048 * uint32_t(wave & 1);
+  // P's place of j: 8 (j % 16 / 4) + 4 (j / 16) + j % 4, as the k-slots of Z^T
+  const uint32_t pput = lds0 + kP + uint32_t(pt) * kRow + 2 * (8 * q + 4 * ((wave >> 1) & 1));
+  const uint32_t pget = lds0 + kP + uint32_t(rp) * kRow + 16 * q;
+  const uint32_t kwt = lds0 + kTable + 4 * (kPowers + 4 * q);
+
+  f32x4 os[2], op[2];                                   // O^T of tokens rp and 16 + rp: of M, without the row's weight, and of P
   const int out_heads = geo.kv_heads * (BACK ? 1 : G);
   // a result on its way: through the place of x in LDS, from where whole rows are stored, by the wave that then copies the next
   // item's rows there
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    put[k] = lds0 + uint32_t(wave >> 1) * kHalf + uint32_t(ln * 128 + 8 * hl + 16 * ((4 * (wave & 1) + k) ^ swz_k(ln & 15)));
-  const uint32_t get = lds0 + uint32_t(rp >> 3) * kHalf;
-  uint16_t* const out_row = OUT ? out + (p.row + (geo.step == nullptr ? int64_t(p.seq) * p.rows : 0)) * out_heads * kD + 8 * rp : nullptr;
+  put = lds0 + uint32_t(half) * kHalf + uint32_t(rp * 128 + 16 * ((2 * (wave & 3) + (q >> 1)) ^ swz_k(rp)) + 8 * (q & 1));
+  const uint32_t get = lds0 + mine + 16 * lane;
+  uint16_t* const out_row = OUT ? out + (p.row + (geo.step == nullptr ? int64_t(p.seq) * p.rows : 0)) * out_heads * kD + 64 * half +
+                                      int64_t(crow) * out_heads * kD + cchunk / 2 : nullptr;
   int held_n = 0;                                      // its rows, or none
   int64_t held_at = 0;
-  bf16x8 going[2];
-  auto fetch = [&](uint32_t stage) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int row = 8 * wave + 4 * i + pq;
-      going[i] = lds_row(get + stage * kStage + uint32_t(row * 128 + 16 * ((rp & 7) ^ swz_k(row & 15))));
-    }
-  };
+  bf16x8 going;
+  auto fetch = [&](uint32_t stage) { going = lds_row(get + stage * kStage); };
   auto store = [&] {                                   // (waits for what was read: before the copies to its place)
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     __builtin_amdgcn_s_waitcnt(waitcnt_lds());
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int row = 8 * wave + 4 * i + pq;
-      if (row < held_n) *reinterpret_cast<bf16x8*>(out_row + held_at + int64_t(row) * out_heads * kD) = going[i];
-    }
+    if (crow < held_n) *reinterpret_cast<bf16x8*>(out_row + held_at) = going;
     held_n = 0;
   };
   float err = 0.f;                                     // of the factors so far, relative
@@ -320,7 +296,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   uint32_t stage = 0;
   int chunk = 0, n = 0, phase = 0;                     // the chunk, its tokens, and its place in the period
   bool full = true;
-  bf16x8 z[2];                                         // Z^T: z-dim zd, tokens 16 kk + 4 hl .. + 3 and 8 more
+  bf16x8 z;                                            // Z^T: z-dim zd, tokens 4 q .. + 3 and 16 more
   auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
   auto before = [&] { return stage == 0 ? 2 : stage - 1; };
 
@@ -328,23 +304,25 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   // has the other to run beside.
   auto result = [&](auto first, int g) {
     constexpr bool kOfM = decltype(first)::value || !BACK;   // (backwards the sum over the query heads begins)
-    // (its parts are formed anew for each query head: held, they would take 64 registers that are not there)
-    if (kOfM) asm volatile("" : "+v"(S[0]), "+v"(S[1]), "+v"(S[2]), "+v"(S[3]));
+    // (its parts are formed anew for each query head: held, they would take 32 registers that are not there)
+    if (kOfM) asm volatile("" : "+v"(S[0]), "+v"(S[1]), "+v"(S[2]), "+v"(S[3]), "+v"(S[4]), "+v"(S[5]), "+v"(S[6]), "+v"(S[7]));
     // this wave's quarter of P^T = Y X^T
     f32x4 s = f32x4{};
+    if (scores) {
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      const uint32_t c = (ks >> 1) * kHalf;
-      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row(py[ks & 1] + c), lds_row(px[ks & 1] + c), s, 0, 0, 0);
+      for (int ks = 0; ks < 4; ++ks) {
+        const uint32_t c = px[ks & 1] + (ks >> 1) * kHalf;
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row(c + py_at), lds_row(c + px_at), s, 0, 0, 0);
+      }
     }
-    auto row = [&](int ks) { return lds_row(kr[ks & 3] + (ks >> 2) * kHalf); };
-    bf16x8 x[3];
+    auto row = [&](int ks, int tb) { return lds_row(px[ks & 1] + (ks >> 1) * kHalf + 2048 * tb); };
+    bf16x8 x[2][2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) x[k] = row(k);
+    for (int tb = 0; tb < 2; ++tb) x[0][tb] = row(0, tb);
     fence();
     store();
     issue(before());
-    {
+    if (scores) {
       float w[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
@@ -362,67 +340,70 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
       *(lds_u32x2*)(uintptr_t)(pput + 64) = u32x2{low[0], low[1]};
     }
     if (kOfM) {
-      os = f32x16{};
-      op = f32x16{};
 #pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
+      for (int tb = 0; tb < 2; ++tb) os[tb] = f32x4{}, op[tb] = f32x4{};
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
         fence();
-        if (ks + 2 < 8) x[(ks + 2) % 3] = row(ks + 2);
+        if (ks + 1 < 4)
+#pragma unroll
+          for (int tb = 0; tb < 2; ++tb) x[(ks + 1) & 1][tb] = row(ks + 1, tb);
         float m[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m[e] = S[ks >> 1][8 * (ks & 1) + e];
+        for (int e = 0; e < 8; ++e) m[e] = S[2 * ks + (e >> 2)][e & 3];
         const bf16x8 hi = top_part(m), lo = last_part(m);
-        os = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, x[ks % 3], os, 0, 0, 0);
-        os = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, x[ks % 3], os, 0, 0, 0);
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) os[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, x[ks & 1][tb], os[tb], 0, 0, 0);
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) os[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, x[ks & 1][tb], os[tb], 0, 0, 0);
       }
     }
     fence();
-    bf16x8 zf[2] = {z[0], z[1]};
-    uint32_t bits = 0;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      const uint4 u = __builtin_bit_cast(uint4, z[kk]);
-      bits |= odd_halves(u.x) | odd_halves(u.y) | odd_halves(u.z) | odd_halves(u.w);
-    }
+    bf16x8 zf = z;
+    const uint4 u = __builtin_bit_cast(uint4, z);
+    const uint32_t bits = odd_halves(u.x) | odd_halves(u.y) | odd_halves(u.z) | odd_halves(u.w);
     const bool any_odd = __ballot((bits & 0x80008000u) != 0) != 0;
     int odd = BACK ? -1 : kChunk;                      // the first (last) token whose value zd is not finite
     if (seldom(any_odd)) {                             // weights of zero would carry it to tokens that do not see it
       stay();
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
+      for (int e = 0; e < 8; ++e)
+        if (tok::not_finite(float(z[e]))) {
+          const int j = 16 * (e >> 2) + 4 * q + (e & 3);
+          odd = BACK ? max(odd, j) : min(odd, j);
+          zf[e] = (__bf16)0.f;
+        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (tok::not_finite(float(z[kk][e]))) {
-            const int j = 16 * kk + 8 * (e >> 2) + 4 * hl + (e & 3);
-            odd = BACK ? max(odd, j) : min(odd, j);
-            zf[kk][e] = (__bf16)0.f;
-          }
-      const int other = __shfl_xor(odd, 32);
-      odd = BACK ? max(odd, other) : min(odd, other);
+      for (int d = 16; d < 64; d <<= 1) {
+        const int other = __shfl_xor(odd, d);
+        odd = BACK ? max(odd, other) : min(odd, other);
+      }
     }
     meet_lds();                                        // P is there, and nobody needs x any more
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      op = __builtin_amdgcn_mfma_f32_32x32x16_bf16(zf[kk], lds_row(pget + 32 * kk), op, 0, 0, 0);
-      op = __builtin_amdgcn_mfma_f32_32x32x16_bf16(zf[kk], lds_row(pget + 32 * kk + 64), op, 0, 0, 0);
-    }
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb)
+        op[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zf, lds_row(pget + 64 * k + 16 * kRow * tb), op[tb], 0, 0, 0);
     if (seldom(any_odd)) {
       stay();
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int of = __shfl(odd, 8 * (r >> 2) + 4 * hl + (r & 3));
-        if (BACK ? ln <= of : ln >= of) op[r] = __builtin_nanf("");
+      for (int r = 0; r < 4; ++r) {
+        const int of = __shfl(odd, 4 * q + r);
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+          if (BACK ? 16 * tb + rp <= of : 16 * tb + rp >= of) op[tb][r] = __builtin_nanf("");
       }
     }
   };
   auto keep = [&](int g) {                             // the result, to be stored behind the next barrier
-    const float weight = (full ? row_whole : row_rest) * tab[kPowers + kWeights + phase];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int tb = 0; tb < 2; ++tb) {
+      const float weight = (full ? row_whole[tb] : row_rest[tb]) * tab[kPowers + kWeights + phase];
       float r[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(os[4 * k + i], weight, op[4 * k + i]);
-      *(lds_u32x2*)(uintptr_t)(put[k]) = u32x2{pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
+      for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(os[tb][i], weight, op[tb][i]);
+      *(lds_u32x2*)(uintptr_t)(put + 2048 * tb) = u32x2{pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
     }
     held_n = n;
     held_at = (int64_t(chunk) * kChunk * out_heads + (BACK ? h : h * G + g)) * kD;
@@ -441,59 +422,53 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     if (forget) {
       stay();
 #pragma unroll
-      for (int mt = 0; mt < 4; ++mt) S[mt] *= dec;
+      for (int b = 0; b < 8; ++b) S[b] *= dec;
     }
-    auto operand = [&](int i) {                        // of tokens 16 (i / 4) .., y-dims 32 (i % 4) ..
-      const uint32_t ya = ((i & 3) >> 1) * kHalf + (i >> 2) * 2048;
-      return lds_tr2(yt[0][i & 1] + ya, yt[1][i & 1] + ya);
+    auto operand = [&](int b) {                        // of the chunk's tokens, y-dims of S[b]
+      const uint32_t a = yt[(b >> 1) & 1] + (b >> 2) * kHalf + 8 * (b & 1);
+      return lds_tr2(a, a + 2048);
     };
     bf16x8 part[PARTS], y[3];
-    auto split = [&](int kk) {
-      const float4 a = __builtin_bit_cast(float4, *(const tok::lds_u32x4*)(uintptr_t)(kw + 64 * kk));
-      const float4 b = __builtin_bit_cast(float4, *(const tok::lds_u32x4*)(uintptr_t)(kw + 64 * kk + 32));
+    y[0] = operand(0);
+    y[1] = operand(1);
+    {
+      const float4 a = __builtin_bit_cast(float4, *(const tok::lds_u32x4*)(uintptr_t)(kw));
+      const float4 b = __builtin_bit_cast(float4, *(const tok::lds_u32x4*)(uintptr_t)(kw + 64));
       const float c8[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
       float w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = float(z[kk][e]) * (OUT ? c8[e] : c8[e] * float(far));
+      for (int e = 0; e < 8; ++e) w[e] = float(z[e]) * (OUT ? c8[e] : c8[e] * float(far));
 #pragma unroll
       for (int k = 0; k < PARTS; ++k) part[k] = k == PARTS - 1 ? last_part(w) : top_part(w);
-    };
-    y[0] = operand(0);
-    y[1] = operand(1);
-    split(0);
+    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int b = 0; b < 8; ++b) {
       fence();
-      if (i + 2 < 8) y[(i + 2) % 3] = operand(i + 2);
-      if (i == 4) split(1);
+      if (b + 2 < 8) y[(b + 2) % 3] = operand(b + 2);
 #pragma unroll
-      for (int k = PARTS - 1; k >= 0; --k) S[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[i % 3], part[k], S[i & 3], 0, 0, 0);
-      if (i == 3) between();
+      for (int k = PARTS - 1; k >= 0; --k) S[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[b % 3], part[k], S[b], 0, 0, 0);
+      if (b == 3) between();
     }
     fence();
   };
   auto begin_item = [&] {
-    meet<OUT ? 6 : 4>();                               // this item has landed, and the last one's buffer is free
+    meet<OUT ? 3 : 2>();                               // this item has landed, and the last one's buffer is free
     if (OUT) fetch(before());
     else issue(before());
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) z[kk] = lds_tr2(zt[0] + kk * 2048, zt[1] + kk * 2048);
+    z = lds_tr2(zt, zt + 2048);
     if (seldom(!full)) {
       stay();
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (16 * kk + 8 * (e >> 2) + 4 * hl + (e & 3) >= n) z[kk][e] = (__bf16)0.f;
+      for (int e = 0; e < 8; ++e)
+        if (16 * (e >> 2) + 4 * q + (e & 3) >= n) z[e] = (__bf16)0.f;
     }
   };
   auto end_item = [&] {
     const uint32_t d = stage == 2 ? uint32_t(-2) * kStage : kStage;
     stage = stage == 2 ? 0 : stage + 1;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) kr[k] += d, yt[k >> 1][k & 1] += d, put[k] += d;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) zt[k] += d, py[k] += d, px[k] += d;
+    for (int k = 0; k < 2; ++k) px[k] += d, yt[k] += d;
+    zt += d, put += d;
   };
   const std::true_type yes;
   const std::false_type no;
@@ -535,18 +510,18 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   if (last != nullptr) {
     if (phase > 0)
 #pragma unroll
-      for (int mt = 0; mt < 4; ++mt) S[mt] *= tab[kPowers + kWeights + phase];
+      for (int b = 0; b < 8; ++b) S[b] *= tab[kPowers + kWeights + phase];
 #pragma unroll
-    for (int mt = 0; mt < 4; ++mt)
+    for (int b = 0; b < 8; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) last[(32 * mt + 16 * (r >> 3) + 8 * hl + (r & 7)) * kD + zd] = S[mt][r];
+      for (int r = 0; r < 4; ++r) last[(32 * (b >> 1) + 8 * q + 4 * (b & 1) + r) * kD + zd] = S[b][r];
   }
   if (OUT && geo.step == nullptr) {                    // padding
     const int from = max(p.tokens, p.part * geo.chunks * kChunk);
     const int to = p.part == geo.parts - 1 ? p.rows : min(p.rows, (p.part + 1) * geo.chunks * kChunk);
     const int own = BACK ? 1 : G;
     uint16_t* const row0 = out + int64_t(p.seq) * p.rows * out_heads * kD + int64_t(h) * own * kD;
-    for (int64_t k = tid; k < int64_t(max(to - from, 0)) * own * 16; k += 256) {
+    for (int64_t k = tid; k < int64_t(max(to - from, 0)) * own * 16; k += kThreads) {
       const int64_t t = k / (own * 16), w = k % (own * 16);
       *reinterpret_cast<uint4*>(row0 + (from + t) * out_heads * kD + w * 8) = make_uint4(0, 0, 0, 0);
     }
@@ -567,14 +542,14 @@ __device__ __forceinline__ void run_walk(const Geo& geo, const Walk& w, bool tra
   walk<BACK, true, PARTS>(geo, p, w.x, w.y, w.z, w.out, begin, sums, trans, ends && w.last != nullptr ? w.last + at : nullptr, smem);
 }
 
-__global__ __launch_bounds__(256, 2) void linear_fwd_kernel(WalkArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void linear_fwd_kernel(WalkArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kShared];
   run_walk<false, 3>(a.geo, a.walk[0], false, blockIdx.x, smem);
 }
 
 // dk, dv and dq (dk's and dq's M are what is given transposed) of eight workgroups' places one after the other: a place's three lie on one XCD, and share their reads there.
 template <int PARTS>
-__global__ __launch_bounds__(256, 2) void linear_bwd_kernel(WalkArgs a, int groups) {
+__global__ __launch_bounds__(kThreads, 4) void linear_bwd_kernel(WalkArgs a, int groups) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kShared];
   const int b = blockIdx.x / 24, r = blockIdx.x % 24, idx = 8 * b + r % 8;
   if (idx >= groups) return;
@@ -583,7 +558,7 @@ __global__ __launch_bounds__(256, 2) void linear_bwd_kernel(WalkArgs a, int grou
 }
 
 template <int PARTS>
-__global__ __launch_bounds__(256, 2) void linear_parts_kernel(PartArgs a, int groups) {
+__global__ __launch_bounds__(kThreads, 4) void linear_parts_kernel(PartArgs a, int groups) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kShared];
   const int idx = blockIdx.x % groups;
   const auto& s = a.sum[blockIdx.x / groups];
@@ -660,8 +635,8 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(PartArgs a) {
 }  // namespace
 
 hipError_t launch_linear_parts(const PartArgs& a, int32_t groups, bool exact, hipStream_t stream) {
-  if (exact) linear_parts_kernel<3><<<dim3(unsigned(groups) * a.n), 256, 0, stream>>>(a, groups);
-  else linear_parts_kernel<2><<<dim3(unsigned(groups) * a.n), 256, 0, stream>>>(a, groups);
+  if (exact) linear_parts_kernel<3><<<dim3(unsigned(groups) * a.n), kThreads, 0, stream>>>(a, groups);
+  else linear_parts_kernel<2><<<dim3(unsigned(groups) * a.n), kThreads, 0, stream>>>(a, groups);
   return hipGetLastError();
 }
 
@@ -671,14 +646,14 @@ hipError_t launch_linear_scan(const PartArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, hipStream_t stream) {
-  linear_fwd_kernel<<<dim3(unsigned(groups)), 256, 0, stream>>>(a);
+  linear_fwd_kernel<<<dim3(unsigned(groups)), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_linear_bwd(const WalkArgs& a, int32_t groups, bool exact, hipStream_t stream) {
   const unsigned grid = (unsigned(groups) + 7) / 8 * 24;
-  if (exact) linear_bwd_kernel<3><<<dim3(grid), 256, 0, stream>>>(a, groups);
-  else linear_bwd_kernel<2><<<dim3(grid), 256, 0, stream>>>(a, groups);
+  if (exact) linear_bwd_kernel<3><<<dim3(grid), kThreads, 0, stream>>>(a, groups);
+  else linear_bwd_kernel<2><<<dim3(grid), kThreads, 0, stream>>>(a, groups);
   return hipGetLastError();
 }
 
