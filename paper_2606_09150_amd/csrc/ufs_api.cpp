@@ -69,13 +69,13 @@ bool scanned(int64_t parts, double groups, int walks) { return parts > 4 && (wal
 // Chunks of a part: of n sequences with `all` chunks, the longest with `longest`, of `heads` key heads with `group` query heads
 // each; `walks` 1, or the backward's 3 beside two sums.  Parts are walked side by side, and pay with a sum of each, a launch or two
 // and their states' way through memory.  The time of either is estimated from what these launches took (us; c chunks a part, P
-// parts of a sequence, W workgroups).  Walks: 2.0 c where a workgroup has a CU of its own (2.35 c where W = 256), 3.1 c where the first two
-// share one, 4.05 c at W = 512, and rounds of these; the backward's 1.9 c, 2.1 c at 192, 3.6 c at 512, and less for what is left in
-// a second round.  Sums 0.95 c, 1.9 c at 512; the states carried on 0.12 P, or 13 us for 512 of them, or summed 1.3 P (backward
-// 1.5 P) with a launch less.  Measured (W: us): 1 x 32,768 tokens, 16 heads, 128: 397, 256: 235, 320: 260, 400: 259, 512: 216, 640: 252,
-// 1,024: 239; 4 x 2,048 tokens, 8 heads, 128: 60, 256: 42, 320: 54, 512: 54; 1 x 16,384, 8 heads of 4, 192: 176, 256: 148, 512: 138,
-// 592: 169.  Backward (W: of walks, us) 1 x 32,768, 16 heads, 384: 526, 576: 539, 768: 490, 960: 508, 1,536: 503; 4 x 2,048, 8 heads,
-// 192: 103, 384: 79, 576: 89, 768: 84; 2 x 8,192, 32 heads, 192 (whole): 531, 768: 468, 960: 480, 1,536: 492.
+// parts of a sequence, W workgroups).  Walks: 1.8 c where a workgroup has a CU of its own (2.15 c where W = 256), 3.1 c where the first two
+// share one, 3.8 c at W = 512, and rounds of these; the backward's 1.9 c, 2.1 c at 192, 3.75 c at 512, and less for what is left in a
+// second round.  Sums 0.8 c, 1.9 c at 512; the states carried on 0.12 P, or 13 us for 512 of them, or summed 1.3 P (backward 1.5 P)
+// with a launch less.  Measured (W: us): 1 x 32,768 tokens, 16 heads, 128: 336, 256: 221, 320: 254, 384: 234, 512: 211, 640: 238, 1,024: 238;
+// 4 x 2,048 tokens, 8 heads, 128: 53, 256: 39, 320: 53, 512: 51; 1 x 16,384, 8 heads of 4, 192: 162, 256: 138, 512: 138, 592: 161.
+// Backward (W: of walks, us) 2 x 8,192, 32 heads, 192 (whole): 547, 384: 502, 576: 521, 768: 509, 960: 489, 1,536: 502; 4 x 2,048, 8
+// heads, 192: 95, 384: 77, 576: 87, 768: 83.
 int32_t part_chunks(int64_t all, int64_t longest, int64_t n, int64_t heads, int walks, int group) {
   const int sums = walks > 1 ? 2 : 1;
   const double item = 0.35 + 0.65 * group, sum = walks > 1 ? 0.5 + 0.5 * group : 1.0;   // of a group's heads, for one's
@@ -88,13 +88,13 @@ int32_t part_chunks(int64_t all, int64_t longest, int64_t n, int64_t heads, int 
     const double all_walks = walks * groups, whole = std::floor(all_walks / 512.0), rest = all_walks - 512.0 * whole;
     double left = 0.0;
     if (walks > 1 && whole == 0.0) left = 1.9 + std::max(0.0, rest - 160.0) / 190.0;
-    else if (walks > 1 && rest > 0.0) left = rest <= 256.0 ? 0.7 + rest / 365.0 : 1.4 + (rest - 256.0) / 101.0;
-    else if (rest > 0.0) left = rest <= 256.0 ? std::max(2.0, 1.45 + rest / 285.0) : 3.1 + (rest - 256.0) / 270.0;
-    const double walk = item * double(c) * (whole * (walks > 1 ? 3.6 : 4.05) + left);
+    else if (walks > 1 && rest > 0.0) left = rest <= 256.0 ? 0.5 + rest / 183.0 : 1.9 + (rest - 256.0) / 160.0;
+    else if (rest > 0.0) left = rest <= 256.0 ? std::max(1.8, 1.25 + rest / 285.0) : 3.1 + (rest - 256.0) / 365.0;
+    const double walk = item * double(c) * (whole * (walks > 1 ? 3.75 : 3.8) + left);
     if (c >= longest) return 4.0 + walk;
     const double carry = scanned(int64_t(parts), groups, walks) ? std::max(0.12 * parts, 0.026 * sums * groups)
                                                                 : (walks > 1 ? 1.5 * parts - 5.2 : 1.3 * parts - 4.5);
-    return (walks > 1 ? 18.0 : 13.0) + walk + sum * double(c) * std::max(0.95, sums * groups / (walks > 1 ? 300.0 : 265.0)) + carry;
+    return (walks > 1 ? 18.0 : 13.0) + walk + sum * double(c) * std::max(0.8, sums * groups / (walks > 1 ? 300.0 : 265.0)) + carry;
   };
   int64_t best = std::max<int64_t>(longest, 1);
   for (int64_t c = 1; c < longest; c += std::max<int64_t>(1, c / 32))
