@@ -17,9 +17,9 @@
  *     S_t = L S_{t-1} + k_t v_t^T          [128 (of k), 128 (of v)], float32
  *     o_t = scale S_t^T q_t   =   scale ( sum_{j <= t} L^{t-j} (q_t.k_j) v_j + L^{t+1} S_-1^T q_t ).
  * Query head n reads key head n / (q_heads / kv_heads).  Scores, states and
- * accumulators are fp32; weights and states enter their products in two bf16 parts,
- * what is added to a state in three (or two where only bf16 results come of it), and every
- * bf16 result is rounded once.  A value that is not finite reaches its own token and those
+ * accumulators are fp32; weights and states enter their products in two bf16 parts (in
+ * steps of few tokens in fp32), what is added to a state in three (backwards in two where
+ * d_dstate is not wanted), and every bf16 result is rounded once.  A value that is not finite reaches its own token and those
  * after it (gradients: dk and dv before it), and no others.
  */
 #ifndef UFS_H
@@ -37,10 +37,10 @@ extern "C" {
 /* d_q [batch, tokens, q_heads, head_dim], d_k, d_v [batch, tokens, kv_heads,
  * head_dim] bf16 (16-byte aligned, strided), d_decay [kv_heads] fp32, d_o [batch,
  * tokens, q_heads, head_dim] bf16 contiguous.  d_lengths, NULL or int32 [batch]
- * (device): tokens from d_lengths[b] on are padding: not read, and their rows get zeros,
- * in o and in the gradients.  d_state, NULL (zeros) or fp32 [batch, kv_heads, head_dim,
+ * (device): tokens from d_lengths[b] on (brought into 0 .. tokens) are padding: not read,
+ * and their rows get zeros, in o and in the gradients.  d_state, NULL (zeros) or fp32 [batch, kv_heads, head_dim,
  * head_dim]: the states before the first token; d_final, NULL or the same: those behind
- * the last one (d_final may be d_state).
+ * the last one (d_final may be d_state; outputs overlap nothing else).
  *
  * Sequences are cut into parts where that fills the GPU; the states between them lie
  * in d_work (16-byte aligned, >= ufs_linear_work_bytes; 0 bytes: may be NULL).  scale:
@@ -125,7 +125,7 @@ int ufs_attn(const ufs_cache* cache, int32_t layer, const ufs_attn_desc* desc, c
              const void* d_v, const float* d_decay, void* d_o, void* d_work, size_t work_bytes, void* stream);
 
 /* Sequences dst[i], empty before, become continuations of src[i]: states are copied,
- * all layers.  Errors: UF_ERR_ARG (a dst twice, or not empty), UF_ERR_EMPTY (src has no
+ * all layers, as they are (so: behind a step's layers, as in ufs_reorder).  Errors: UF_ERR_ARG (a dst twice, or not empty), UF_ERR_EMPTY (src has no
  * token), UF_ERR_HIP. */
 int ufs_fork(ufs_cache* cache, int32_t n, const int32_t* src, const int32_t* dst, void* stream);
 

@@ -8,25 +8,32 @@
 // o is the walk of (q, k, v), dq that of (do, v, k) with M transposed, and backwards dk that of (v,
 // do, q) and dv that of (k, q, do), which add over the query heads of a key head.  Where
 // sequences are few they are cut into parts: one launch forms the parts' own M, one
-// carries them on from part to part, and the walks begin from those.
+// carries them on from part to part (or, of few parts, each walk sums those before it), and
+// the walks begin from those.
 //
-// Work split: a workgroup per (sequence, part, key head), four waves, each with 32
-// z-dims of M and of the result; P^T = Y X^T is formed by each of them for itself (8 of
-// 52 products a chunk), so that no wave waits for another but for the copies.  All products are
-// v_mfma_f32_32x32x16_bf16: O^T = M^T X^T + Z^T P^T and M += Y^T (c Z), X and Y rows and
-// transposed reads of Y and Z from LDS.  M stays in accumulators: its y-dims lie there as the
-// k-slots of the next product want them (Y^T's operand is read with bits 2 and 3 of its
-// dimensions swapped, which the accumulators swap back), so it is multiplied without leaving
-// registers.
+// Work split: a workgroup per (sequence, part, key head), eight waves, each with 16
+// z-dims of M and of the result; P^T = Y X^T is formed once, a quarter by each of four waves, and
+// shared through LDS.  All products are v_mfma_f32_16x16x32_bf16: O^T = M^T X^T + Z^T P^T and
+// M += Y^T (c Z), X and Y rows and transposed reads of Y and Z from LDS.  M stays in
+// accumulators: its y-dims lie there as the k-slots of the next product want them (Y^T's rows
+// are read in that order), so it is multiplied without leaving registers.  (Four waves of 32
+// z-dims, by 32x32x16: two waves a SIMD hide less; one sequence of 32,768 tokens, 16 heads, in 8 parts 397 us
+// for 336, in 32 216 for 207.  But all of Y is read by twice the waves now, and half of these reads'
+// cycles are bank conflicts, for a wave's rows have one 8-byte half of each 16: the backward pass
+// of 2 x 8,192 tokens, 32 heads, took 466 for 457 to 505.)
+//
+// What bounds it: of 2.4e5 cycles of a SIMD in the walk of 1 x 32,768 tokens, 16 heads (159 us), matrix
+// instructions take 0.94e5 and vector ones 1.34e5, a third of these M's parts, and they run beside
+// each other little; each chunk has two barriers.
 //
 // Rounding: M and P enter their products as two bf16 parts each (one alone would add as much
 // error as the result's own rounding), c Z in three, since M is a result in fp32 and carries
-// each error on (two where it is none).  L^32 in fp32 would be off by the same 2^-25 in each of
-// thousands of chunks: the part of it that fp32 drops is carried on and added to the next factor.
+// each error on (two backwards, where it is none).  L^32 in fp32 would be off by the same 2^-25 in each
+// of thousands of chunks: the part of it that fp32 drops is carried on and added to the next factor.
 //
 // Memory: three tiles of 8 KB an item (a chunk and query head), in two blocks of 64 dimensions in 128-byte
-// rows (swz_k), copied by global_load_lds two items ahead into three buffers; one barrier
-// an item.  Rows past the sequence's end take its last row, and weigh nothing.
+// rows (swz_k), copied by global_load_lds two items ahead into three buffers.  Rows past the
+// sequence's end take its last row, and weigh nothing.
 #include "linear_place.h"
 #include "token_common.h"
 

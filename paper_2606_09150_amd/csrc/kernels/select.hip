@@ -11,9 +11,14 @@
 // A list holds 64-bit keys, the value in an order of integers, then the place, lowest
 // first: all different, so that what is selected does not depend on the order in
 // which it was found.  In a slice each wave keeps a list of its own in LDS, without a
-// barrier: values above a bar join it, and the bar is the n-th largest of the lanes' maxima, at
-// first of the first block's, later of the list's (n values are at or above it, and what comes
-// later has a higher place).  A list that might not hold the next block is cut down to its n largest.
+// barrier: values above a bar join it, and the bar is the n-th largest, at first of the first
+// block's maxima (two of each lane), later of the list's values (n values are at or above it, and
+// what comes later has a higher place).  A list that might not hold the next block is cut down to its n largest.
+//
+// 32 requests of 8 beams over 131,072 tokens, bf16, k 16: 25 us of slices (67 MB at 2.7 TB/s) and 10 of joining.  A workgroup's
+// eight blocks take 1.2 each, at which rate the slices would be read in 10; before them lie 3 until its first one is there, behind
+// them and between, 5 of raising bars, summing and joining lists, at the same time in all workgroups.  One request of 32 beams
+// over 200,000, k 64: 42 us (190 with the lists' entries all read by the join).
 #include <algorithm>
 #include <type_traits>
 

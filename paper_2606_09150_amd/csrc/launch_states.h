@@ -73,7 +73,8 @@ hipError_t launch_linear_scan(const PartArgs& a, hipStream_t stream);
 hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, hipStream_t stream);
 hipError_t launch_linear_bwd(const WalkArgs& a, int32_t groups, bool exact, hipStream_t stream);
 
-// Few tokens a sequence: token by token.
+// Few tokens a sequence: token by token.  So / in chunks (us): 24 sequences of 8 key heads of 2, 2 tokens 7.4 / 12.6, 4 9.6 / 12.6,
+// 7 13.0 / 12.5; 64 of 8, 4 14.2 / 18.1, 8 20.3 / 18.3; 64 of 32, 2 41.8 / 58.4, 8 58.4 / 59.5; 1 of 8 heads of 8, 4 11.6 / 18.3.
 constexpr int kFewTokens = 8;
 struct StepArgs {
   Geo geo;                    // of a step
