@@ -544,7 +544,11 @@ __device__ __forceinline__ void run_walk(const Geo& geo, const Walk& w, bool tra
   const float *begin = nullptr, *sums = nullptr;
   const float* const start = p.chunks > 0 && w.starts != nullptr ? w.starts + size_t(idx) * kState : nullptr;
   if (start != nullptr && geo.scanned) begin = start;
-  else if (p.held && w.first != nullptr) begin = w.first + at;
+  else if (p.held && w.first != nullptr) {
+    // (forwards the last part's place has a copy: that part may end, and put its M over the first one, before others begin)
+    if (start != nullptr && !BACK) begin = start + int64_t(p.parts - 1 - p.part) * geo.kv_heads * kState;
+    else begin = w.first + at;
+  }
   if (!geo.scanned) sums = start;
   walk<BACK, true, PARTS>(geo, p, w.x, w.y, w.z, w.out, begin, sums, trans, ends && w.last != nullptr ? w.last + at : nullptr, smem);
 }
@@ -574,7 +578,11 @@ __global__ __launch_bounds__(kThreads, 4) void linear_parts_kernel(PartArgs a, i
   float* const to = s.starts + size_t(idx) * kState;
   if (s.back) {
     if (p.part > 0) walk<true, false, PARTS>(a.geo, p, s.y, s.y, s.z, nullptr, nullptr, nullptr, false, to, smem);
-  } else if (p.part < p.parts - 1) {
+  } else if (p.part == p.parts - 1) {
+    if (a.geo.scanned || s.first == nullptr || !p.held) return;
+    const float* const from = s.first + (size_t(p.seq) * a.geo.kv_heads + p.h) * kState;
+    for (int i = 4 * threadIdx.x; i < kState; i += 4 * kThreads) *reinterpret_cast<f32x4*>(to + i) = *reinterpret_cast<const f32x4*>(from + i);
+  } else {
     walk<false, false, PARTS>(a.geo, p, s.y, s.y, s.z, nullptr, nullptr, nullptr, false, to, smem);
   }
 }

@@ -54,7 +54,8 @@ struct WalkArgs {
   Walk walk[kWalks];
   int32_t n;
 };
-// Parts' own M without the parts before (after) them, in their places of `starts`.
+// Parts' own M without the parts before (after) them, in their places of `starts`; forwards, where they are not carried on, `first` in
+// the last part's, which no part comes after.
 struct PartArgs {
   Geo geo;
   struct {

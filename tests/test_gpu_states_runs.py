@@ -194,6 +194,28 @@ def test_other_streams():
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("B,n,Hk", [(3, 900, 11), (2, 2000, 32), (80, 700, 4), (1, 9000, 2)])
+def test_states_exchanged_in_place(B, n, Hk):
+    """Final states over the first ones, for few parts and for many, and more of them than run at once: no part's walk may read what
+    the last one's has put there."""
+    P = require_gpu()
+    q, k, v = (draw((B, n, h, D), i) for i, h in enumerate((Hk, Hk, Hk)))
+    g = torch.full((Hk,), -1e-3, device="cuda")
+    state = draw((B, Hk, D, D), 8, 30.0, dtype=torch.float32)
+    want = P.linear_attention(q, k, v, g, state=state, final=True)
+    cache = P.StateCache(1, Hk, B)
+    for _ in range(3):
+        own = state.clone()
+        o, final = P.linear_attention(q, k, v, g, state=own, final=own)
+        assert torch.equal(o, want[0]) and torch.equal(final, want[1])
+        cache.free(list(range(B)))
+        cache.extend(list(range(B)), [1] * B)            # (its states count from here on)
+        cache.states_view()[0].copy_(state)
+        cache.extend(list(range(B)), [n] * B)
+        o = cache.attention(0, q.view(-1, Hk, D), k.view(-1, Hk, D), v.view(-1, Hk, D), g)
+        assert torch.equal(o.view_as(want[0]), want[0]) and torch.equal(cache.states_view()[0], want[1])
+
+
 def test_steps_without_tokens():
     P = require_gpu()
     cache, g = P.StateCache(1, 2, 3), decays(2)
