@@ -178,20 +178,20 @@ struct Shared {
   uint64_t keys[kWaves][kRoom];
   uint64_t out[kMaxSelect];
   uint32_t low[kWaves];
-  int count[kWaves];
+  int count[2][kWaves], all;                           // (as they come, and cut down)
 };
 __device__ inline void join(Shared& s, List& list) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  if (lane == 0) s.low[wave] = list.bar, s.count[wave] = list.count;
+  if (lane == 0) s.low[wave] = list.bar, s.count[0][wave] = list.count;
   for (int i = threadIdx.x; i < list.n; i += kThreads) s.out[i] = 0;
   __syncthreads();
   // what is below any wave's n-th largest is left out (a list's own n-th may equal its bar)
   const uint32_t low = max(max(s.low[0], s.low[1]), max(s.low[2], s.low[3]));
-  const bool many = s.count[0] > kFew || s.count[1] > kFew || s.count[2] > kFew || s.count[3] > kFew;
+  const bool many = max(max(s.count[0][0], s.count[0][1]), max(s.count[0][2], s.count[0][3])) > kFew;   // (the same for all waves)
   if (many) {
     list.keep(uint64_t(low) << 32);
     if (list.count > kFew) list.cut();
-    if (lane == 0) s.count[wave] = list.count;
+    if (lane == 0) s.count[1][wave] = list.count;
     __syncthreads();
   }
   if (wave == 0) {                                     // the others' into the first list
@@ -199,7 +199,7 @@ __device__ inline void join(Shared& s, List& list) {
     list.bar = low - 1;
 #pragma unroll 1
     for (int w = 1; w < kWaves; ++w) {
-      const int c = s.count[w];
+      const int c = s.count[many][w];
 #pragma unroll 1
       for (int i = lane; i - lane < c; i += 64) {
         const uint64_t key = i < c ? s.keys[w][i] : 0;
@@ -208,10 +208,10 @@ __device__ inline void join(Shared& s, List& list) {
     }
     if (list.count > kFew) list.raise();
     if (list.count > kFew) list.cut();
-    if (lane == 0) s.count[0] = list.count;
+    if (lane == 0) s.all = list.count;
   }
   __syncthreads();
-  const int all = s.count[0];                          // (at most kFew)
+  const int all = s.all;                               // (at most kFew)
   if (int(threadIdx.x) < all) {
     const uint64_t mine = s.keys[0][threadIdx.x];
     int rank = 0;

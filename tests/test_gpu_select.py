@@ -113,6 +113,25 @@ def test_logits_that_round_to_one_score(k):
     assert torch.equal(p[0], torch.tensor([0] * 3 * k + [1] * k, dtype=torch.int32))
 
 
+@pytest.mark.parametrize("k", [3, 16, 63])
+def test_rows_with_many_equal_logits_in_places(k):
+    """Lists of very unequal lengths: a few stretches of equal large logits among others, in 200 rows at once."""
+    P = require_gpu()
+    G, W, V = 50, 4, 9001
+    gen = torch.Generator().manual_seed(k)
+    logits = torch.randn((G, W, V), generator=gen)
+    for g in range(G):
+        for w in range(W):
+            at, n = (int(torch.randint(0, m, (), generator=gen)) for m in (V - 1500, 1500))
+            logits[g, w, at:at + n] = 4.0 + (g % 3)
+    logits, scores = logits.cuda(), (-30 * torch.rand((G, W), generator=gen)).cuda()
+    first = P.beam_select(logits, scores, k)
+    check(logits, scores, k, first)
+    for _ in range(20):
+        for a, b in zip(P.beam_select(logits, scores, k), first):
+            assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 def test_sorted_rows(kind):
     """Rising logits pass every bar: lists are cut down again and again."""
