@@ -18,9 +18,10 @@
 // accumulators: its y-dims lie there as the k-slots of the next product want them (Y^T's rows
 // are read in that order), so it is multiplied without leaving registers.  (Four waves of 32
 // z-dims, by 32x32x16: two waves a SIMD hide less; one sequence of 32,768 tokens, 16 heads, in 8 parts 397 us
-// for 336, in 32 216 for 207.  But all of Y is read by twice the waves now, and half of these reads'
-// cycles are bank conflicts, for a wave's rows have one 8-byte half of each 16: the backward pass
-// of 2 x 8,192 tokens, 32 heads, took 466 for 457 to 505.)
+// for 336, in 32 216 for 207.  But the backward pass of 2 x 8,192 tokens, 32 heads, took 466 for 457 to
+// 505: all of Y is read by twice the waves.  Half of these reads' cycles are bank conflicts, for a wave's rows have
+// one 8-byte half of each 16; rows of 16 dimensions side by side, with X read by 8 bytes, have none, a third
+// less of LDS cycles, and the same times.)
 //
 // What bounds it: of 2.4e5 cycles of a SIMD in the walk of 1 x 32,768 tokens, 16 heads (159 us), matrix
 // instructions take 0.94e5 and vector ones 1.34e5, a third of these M's parts, and they run beside
