@@ -15,10 +15,10 @@
 // block's maxima (two of each lane), later of the list's values (n values are at or above it, and
 // what comes later has a higher place).  A list that might not hold the next block is cut down to its n largest.
 //
-// 32 requests of 8 beams over 131,072 tokens, bf16, k 16: 25 us of slices (67 MB at 2.7 TB/s) and 10 of joining.  A workgroup's
+// 32 requests of 8 beams over 131,072 tokens, bf16, k 16: 25 us of slices (67 MB at 2.7 TB/s) and 9 of joining.  A workgroup's
 // eight blocks take 1.2 each, at which rate the slices would be read in 10; before them lie 3 until its first one is there, behind
 // them and between, 5 of raising bars, summing and joining lists, at the same time in all workgroups.  One request of 32 beams
-// over 200,000, k 64: 42 us (190 with the lists' entries all read by the join).
+// over 200,000, k 64: 40 us (190 with the lists' entries all read by the join).
 #include <algorithm>
 #include <type_traits>
 
@@ -278,7 +278,6 @@ struct Logits {
 // A slice's results: its maximum and sum of exponentials, then its list of k + 1 (lanes bound a list to 64).
 __device__ __host__ inline int listed_of(int k) { return k + 1 < 64 ? k + 1 : 64; }
 __device__ __host__ inline size_t slice_bytes(int k) { return 16 + size_t(listed_of(k)) * 8; }
-__device__ inline bool in_use(const SelectArgs& a, int row) { return a.scores[row] > -INFINITY; }
 
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
@@ -289,7 +288,9 @@ __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
   __shared__ float stop[kWaves];
   __shared__ double ssum[kWaves];
   const int row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
-  if (!in_use(a, row) || (a.done != nullptr && a.done[row] != 0)) return;
+  const float score = a.scores[row];                   // (both loads before either is looked at)
+  const int ended = a.done != nullptr ? a.done[row] : 0;
+  if (!(score > -INFINITY) || ended != 0) return;
   const L x(a, row % a.beams, row / a.beams);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the waves take the slice's blocks in turn
@@ -396,6 +397,8 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
     }
   };
   fetch(held, from, 0);
+  auto last_of = [&](int i) { return reinterpret_cast<const uint64_t*>(slice_at(i) + 16)[n - 1]; };
+  const uint64_t last_held = tid < slices ? last_of(tid) : 0;
   // eight lanes a row
   for (int w0 = 0; w0 < W; w0 += kThreads / 8) {
     const int w = w0 + tid / 8, part = tid % 8;
@@ -406,8 +409,8 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kSplits / 8; ++i) {
-      t[i] = make_float2(-INFINITY, 0.f);
-      if (kind == 1 && part + 8 * i < a.splits) t[i] = *reinterpret_cast<const float2*>(slice_at(w * a.splits + part + 8 * i));
+      t[i] = make_float2(-INFINITY, 0.f);              // (anything where the row is not read)
+      if (w < W && part + 8 * i < a.splits) t[i] = *reinterpret_cast<const float2*>(slice_at(w * a.splits + part + 8 * i));
     }
 #pragma unroll
     for (int i = 0; i < kSplits / 8; ++i) top = fmaxf(top, t[i].x);
@@ -431,7 +434,7 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
   auto again = [&](int i, uint32_t limit) {
     const int w = i / a.splits;
     if (skind[w] != 1) return false;
-    const uint64_t last = reinterpret_cast<const uint64_t*>(slice_at(i) + 16)[n - 1];
+    const uint64_t last = i == tid ? last_held : last_of(i);
     if (uint32_t(last >> 32) <= kNone) return false;   // (it has fewer: none was left out)
     const float x = value_of(uint32_t(last >> 32)), score = score_of(w, x);
     return order_of(score) > kNone && order_of(score) >= limit && score_of(w, L::below(x)) == score;
@@ -474,7 +477,7 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
       for (int u = 0; u < kHeld; ++u) held[u] = next[u], from[u] = next_from[u];
     }
     finished(list);
-    list.raise();
+    if (list.count > max(2 * list.n, 24)) list.raise();   // (few: the lists' join takes them as they are)
     join(s, list);
   }
   const uint32_t limit = uint32_t(s.out[a.k - 1] >> 32);

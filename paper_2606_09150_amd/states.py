@@ -21,8 +21,8 @@ def _work(work, need, device):
             raise ValueError(f"work must have {need} bytes or more")
 
 
-def _scratch(work, need, device):
-    return torch.empty(need, dtype=torch.uint8, device=device) if work is None and need else work
+def _scratch(work, need, like):
+    return like.new_empty(need, dtype=torch.uint8) if work is None and need else work
 
 
 def _states(t, name, shape, device):
@@ -33,7 +33,7 @@ def _states(t, name, shape, device):
 
 
 def _like(t):
-    """An uninitialised contiguous tensor of the same shape (a third of torch.empty's time from its parts)."""
+    """An uninitialised contiguous tensor of the same shape (half of torch.empty's time from its parts)."""
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
@@ -82,7 +82,7 @@ def linear_attention(q, k, v, decay, scale=None, lengths=None, state=None, final
     def call(s):
         o = _like(q) if out is None else out
         last = final if isinstance(final, torch.Tensor) else torch.empty(shape, dtype=torch.float32, device=q.device) if final else None
-        S.ufs_linear_fwd(desc, q, k, v, decay, lengths, state, o, last, _scratch(work, need, q.device), need, s)
+        S.ufs_linear_fwd(desc, q, k, v, decay, lengths, state, o, last, _scratch(work, need, q), need, s)
         return o if last is None else (o, last)
 
     return _enqueue(q.device, stream, call, q, k, v, decay, lengths, state, out, work, final if isinstance(final, torch.Tensor) else None)
@@ -105,7 +105,7 @@ def linear_attention_bwd(q, k, v, do, decay, scale=None, lengths=None, state=Non
     def call(s):
         dq, dk, dv = _like(q), _like(k), _like(v)
         dstate = None if state is None else _like(state)
-        S.ufs_linear_bwd(desc, q, k, v, do, decay, lengths, state, dfinal, dq, dk, dv, dstate, _scratch(work, need, q.device), need, s)
+        S.ufs_linear_bwd(desc, q, k, v, do, decay, lengths, state, dfinal, dq, dk, dv, dstate, _scratch(work, need, q), need, s)
         return (dq, dk, dv) if dstate is None else (dq, dk, dv, dstate)
 
     return _enqueue(q.device, stream, call, q, k, v, do, decay, lengths, state, dfinal, work)
@@ -237,7 +237,7 @@ class StateCache:
 
         def call(s):
             o = _like(q) if out is None else out
-            S.ufs_attn(self.handle, layer, desc, q, k, v, decay, o, _scratch(work, need, self.device), need, s)
+            S.ufs_attn(self.handle, layer, desc, q, k, v, decay, o, _scratch(work, need, q), need, s)
             return o
 
         return self._run(stream, call, q, k, v, decay, out, work)
@@ -270,9 +270,9 @@ def beam_select(logits, scores, k, done=None, end=None, work=None, stream=None):
     _work(work, need, dev)
 
     def call(s):
-        best = torch.empty((G, k), dtype=torch.float32, device=dev)
-        parents, tokens = torch.empty((2, G, k), dtype=torch.int32, device=dev).unbind()
-        S.ufs_select(desc, logits, scores, done, best, parents, tokens, _scratch(work, need, dev), need, s)
+        best = scores.new_empty((G, k))
+        parents, tokens = scores.new_empty((2, G, k), dtype=torch.int32).unbind()
+        S.ufs_select(desc, logits, scores, done, best, parents, tokens, _scratch(work, need, logits), need, s)
         return best, parents, tokens
 
     return _enqueue(dev, stream, call, logits, scores, done, work)
