@@ -23,9 +23,10 @@
 // one 8-byte half of each 16; rows of 16 dimensions side by side, with X read by 8 bytes, have none, a third
 // less of LDS cycles, and the same times.)
 //
-// What bounds it: of 2.4e5 cycles of a SIMD in the walk of 1 x 32,768 tokens, 16 heads (159 us), matrix
-// instructions take 0.94e5 and vector ones 1.34e5, a third of these M's parts, and they run beside
-// each other little; each chunk has two barriers.
+// What bounds it is the issue of instructions.  A matrix instruction of 16x16x32 takes 16 cycles, and keeps 11 of
+// them from vector instructions of every wave of its SIMD (32x32x16: 15 of 32; measured by loops of both).  A chunk
+// has 46 of a wave, and 261 vector ones of 4 cycles, of which M's parts are 96: 3,100 cycles for a SIMD's two
+// waves of a workgroup, where 4,200 pass (1 x 32,768 tokens, 16 heads, 159 us); each chunk has two barriers.
 //
 // Rounding: M and P enter their products as two bf16 parts each (one alone would add as much
 // error as the result's own rounding), c Z in three, since M is a result in fp32 and carries
