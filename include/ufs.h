@@ -19,8 +19,9 @@
  * Query head n reads key head n / (q_heads / kv_heads).  Scores, states and
  * accumulators are fp32; weights and states enter their products in two bf16 parts (in
  * steps of few tokens in fp32), what is added to a state in three (backwards in two where
- * d_dstate is not wanted), and every bf16 result is rounded once.  A value that is not finite reaches its own token and those
- * after it (gradients: dk and dv before it), and no others.
+ * d_dstate is not wanted), and every bf16 result is rounded once.  A value that is not
+ * finite reaches its own token and those after it (gradients: dk and dv before it), and no
+ * others.
  */
 #ifndef UFS_H
 #define UFS_H
@@ -38,9 +39,10 @@ extern "C" {
  * head_dim] bf16 (16-byte aligned, strided), d_decay [kv_heads] fp32, d_o [batch,
  * tokens, q_heads, head_dim] bf16 contiguous.  d_lengths, NULL or int32 [batch]
  * (device): tokens from d_lengths[b] on (brought into 0 .. tokens) are padding: not read,
- * and their rows get zeros, in o and in the gradients.  d_state, NULL (zeros) or fp32 [batch, kv_heads, head_dim,
- * head_dim]: the states before the first token; d_final, NULL or the same: those behind
- * the last one (d_final may be d_state; outputs overlap nothing else).
+ * and their rows get zeros, in o and in the gradients.  d_state, NULL (zeros) or fp32
+ * [batch, kv_heads, head_dim, head_dim]: the states before the first token; d_final, NULL
+ * or the same: those behind the last one (d_final may be d_state; outputs overlap nothing
+ * else).
  *
  * Sequences are cut into parts where that fills the GPU; the states between them lie
  * in d_work (16-byte aligned, >= ufs_linear_work_bytes; 0 bytes: may be NULL).  scale:
@@ -49,9 +51,9 @@ extern "C" {
  * Backward: d_do [batch, tokens, q_heads, head_dim] bf16 contiguous; d_dfinal, NULL
  * (zeros) or the gradient of the final states, fp32; outputs d_dq (as q) and d_dk, d_dv
  * (as k) bf16, contiguous, fully overwritten, and d_dstate, NULL or the gradient of
- * d_state, fp32 (also where that is NULL).  Gradients of a key head add over its query heads in
- * fp32.  No atomics: results are reproducible.  A call's
- * work may not be shared with a call that runs at the same time. */
+ * d_state, fp32 (also where that is NULL).  Gradients of a key head add over its query
+ * heads in fp32.  No atomics: results are reproducible.  A call's work may not be shared
+ * with a call that runs at the same time. */
 typedef struct {
   int32_t batch, tokens, q_heads, kv_heads, head_dim;
   float scale;
@@ -125,8 +127,8 @@ int ufs_attn(const ufs_cache* cache, int32_t layer, const ufs_attn_desc* desc, c
              const void* d_v, const float* d_decay, void* d_o, void* d_work, size_t work_bytes, void* stream);
 
 /* Sequences dst[i], empty before, become continuations of src[i]: states are copied,
- * all layers, as they are (so: behind a step's layers, as in ufs_reorder).  Errors: UF_ERR_ARG (a dst twice, or not empty), UF_ERR_EMPTY (src has no
- * token), UF_ERR_HIP. */
+ * all layers, as they are (so: behind a step's layers, as in ufs_reorder).  Errors:
+ * UF_ERR_ARG (a dst twice, or not empty), UF_ERR_EMPTY (src has no token), UF_ERR_HIP. */
 int ufs_fork(ufs_cache* cache, int32_t n, const int32_t* src, const int32_t* dst, void* stream);
 
 /* Reorder states, all layers: the sequences seqs[g * beams + i], i = 0 .. beams-1, of
