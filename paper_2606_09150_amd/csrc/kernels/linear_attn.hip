@@ -18,8 +18,8 @@
 // accumulators: its y-dims lie there as the k-slots of the next product want them (Y^T's rows
 // are read in that order), so it is multiplied without leaving registers.  (Four waves of 32
 // z-dims, by 32x32x16: two waves a SIMD hide less; one sequence of 32,768 tokens, 16 heads, in 8 parts 397 us
-// for 336, in 32 216 for 207.  But the backward pass of 2 x 8,192 tokens, 32 heads, took 466 for 457 to
-// 505: all of Y is read by twice the waves.  Half of these reads' cycles are bank conflicts, for a wave's rows have
+// for 336, in 32 216 for 207; the backward pass of 2 x 8,192 tokens, 32 heads, the same 465.  All of Y
+// is read by twice the waves, and half of these reads' cycles are bank conflicts, for a wave's rows have
 // one 8-byte half of each 16; rows of 16 dimensions side by side, with X read by 8 bytes, have none, a third
 // less of LDS cycles, and the same times.)
 //
@@ -281,7 +281,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   const uint32_t pget = lds0 + kP + uint32_t(rp) * kRow + 16 * q;
   const uint32_t kwt = lds0 + kTable + 4 * (kPowers + 4 * q);
 
-  f32x4 os[2], op[2];                                   // O^T of tokens rp and 16 + rp: of M, without the row's weight, and of P
+  f32x4 os[2];                                         // O^T of tokens rp and 16 + rp
   const int out_heads = geo.kv_heads * (BACK ? 1 : G);
   // a result on its way: through the place of x in LDS, from where whole rows are stored, by the wave that then copies the next
   // item's rows there
@@ -350,7 +350,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     }
     if (kOfM) {
 #pragma unroll
-      for (int tb = 0; tb < 2; ++tb) os[tb] = f32x4{}, op[tb] = f32x4{};
+      for (int tb = 0; tb < 2; ++tb) os[tb] = f32x4{};
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
         fence();
@@ -368,6 +368,9 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
       }
     }
     fence();
+    if (kOfM)
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb) os[tb] *= (full ? row_whole[tb] : row_rest[tb]) * tab[kPowers + kWeights + phase];
     bf16x8 zf = z;
     const uint4 u = __builtin_bit_cast(uint4, z);
     const uint32_t bits = odd_halves(u.x) | odd_halves(u.y) | odd_halves(u.z) | odd_halves(u.w);
@@ -393,7 +396,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int tb = 0; tb < 2; ++tb)
-        op[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zf, lds_row(pget + 64 * k + 16 * kRow * tb), op[tb], 0, 0, 0);
+        os[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zf, lds_row(pget + 64 * k + 16 * kRow * tb), os[tb], 0, 0, 0);
     if (seldom(any_odd)) {
       stay();
 #pragma unroll
@@ -401,18 +404,14 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
         const int of = __shfl(odd, 4 * q + r);
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb)
-          if (BACK ? 16 * tb + rp <= of : 16 * tb + rp >= of) op[tb][r] = __builtin_nanf("");
+          if (BACK ? 16 * tb + rp <= of : 16 * tb + rp >= of) os[tb][r] = __builtin_nanf("");
       }
     }
   };
   auto keep = [&](int g) {                             // the result, to be stored behind the next barrier
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
-      const float weight = (full ? row_whole[tb] : row_rest[tb]) * tab[kPowers + kWeights + phase];
-      float r[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(os[tb][i], weight, op[tb][i]);
-      *(lds_u32x2*)(uintptr_t)(put + 2048 * tb) = u32x2{pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
+      *(lds_u32x2*)(uintptr_t)(put + 2048 * tb) = u32x2{pack_bf16x2(os[tb][0], os[tb][1]), pack_bf16x2(os[tb][2], os[tb][3])};
     }
     held_n = n;
     held_at = (int64_t(chunk) * kChunk * out_heads + (BACK ? h : h * G + g)) * kD;
