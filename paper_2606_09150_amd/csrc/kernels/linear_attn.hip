@@ -34,8 +34,9 @@
 // of thousands of chunks: the part of it that fp32 drops is carried on and added to the next factor.
 //
 // Memory: three tiles of 8 KB an item (a chunk and query head), in two blocks of 64 dimensions in 128-byte
-// rows (swz_k), copied by global_load_lds two items ahead into three buffers.  Rows past the
-// sequence's end take its last row, and weigh nothing.
+// rows (swz_k), copied by global_load_lds two items ahead into three buffers.  Forward walks of several
+// query heads take two an item, which share y, z, M's parts and the barriers: four tiles, an item ahead
+// into two buffers.  Rows past the sequence's end take its last row, and weigh nothing.
 #include "linear_place.h"
 #include "token_common.h"
 
@@ -55,15 +56,22 @@ using tok::lds_tr2;
 using tok::swz_k;
 
 constexpr int kThreads = 512;
-constexpr uint32_t kTile = 8192, kHalf = 4096, kStage = 3 * kTile;
-constexpr int kStages = 3;
+constexpr uint32_t kTile = 8192, kHalf = 4096;
 // LDS behind the stages: P, a row of 32 values in two parts (and 16 bytes, so that rows begin in banks of their own) for each
 // token; then, in floats, L^e for e = 0 .. 32, the key weights of a period's chunks and of the last one, and what M is read with.
-constexpr uint32_t kRow = 144, kP = kStages * kStage, kTable = kP + kChunk * kRow;
+constexpr uint32_t kRow = 144;
 constexpr int kPowers = 36;
 constexpr int kPeriod = 4, kWeights = (kPeriod + 1) * kChunk;
-constexpr uint32_t kShared = kTable + 4 * (kPowers + kWeights + kPeriod);
-static_assert(2 * kShared <= 163840, "two workgroups a CU");
+// HEADS: query heads of an item.  One: tiles of x, y and z in three stages; two, whose x share y, z and M's parts: four tiles in two.
+template <int HEADS>
+struct Lds {
+  static constexpr int kStages = HEADS == 1 ? 3 : 2;
+  static constexpr uint32_t kY = HEADS * kTile, kZ = kY + kTile, kStage = kZ + kTile, kP = kStages * kStage, kTable = kP + HEADS * kChunk * kRow;
+  static constexpr uint32_t kShared = kTable + 4 * (kPowers + kWeights + kPeriod);
+  static_assert(2 * kShared <= 163840, "two workgroups a CU");
+};
+constexpr uint32_t kShared = Lds<1>::kShared;
+static_assert(Lds<2>::kShared <= kShared);
 
 // x as parts of 8 bits each, the first ones cut off and the last one rounded.  (Three operations a value and part; by dot products with
 // (-1, 0), which leave out the masking, the copies and waits that those need cost as much.)
@@ -118,9 +126,12 @@ struct Powers {
 // OUT: results are wanted, not M alone: a part's own M is summed against the walk, so that what is read last is what the
 // walk reads first, with a factor for each chunk in the place of M's.  begin: M where the walk begins, or null; last: where
 // to put it at the end, or null.
-template <bool BACK, bool OUT, int PARTS>
+template <bool BACK, bool OUT, int PARTS, int HEADS>
 __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& xs, const Src& ys, const Src& zs, uint16_t* out,
                                      const float* begin, const float* sums, bool trans, float* last, uint8_t* smem) {
+  static_assert(HEADS == 1 || (OUT && !BACK));
+  constexpr uint32_t kStage = Lds<HEADS>::kStage, kY = Lds<HEADS>::kY, kZ = Lds<HEADS>::kZ, kP = Lds<HEADS>::kP, kTable = Lds<HEADS>::kTable;
+  constexpr int kStages = Lds<HEADS>::kStages;
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, q = lane >> 4, rp = lane & 15;
@@ -154,16 +165,17 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   auto issue = [&](uint32_t stage) {
     const int row = min(crow, p.tokens - 1 - next_t);
     const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + stage * kStage + mine);
-    auto copy = [&](const Tile& t, uint32_t at) { dma16(t.at, uint32_t(row) * uint32_t(t.token) + cchunk, dst + at); };
-    if (OUT) copy(tx, 0);
-    copy(ty, kTile);
-    copy(tz, 2 * kTile);
+    auto copy = [&](const uint8_t* from, const Tile& t, uint32_t at) { dma16(from, uint32_t(row) * uint32_t(t.token) + cchunk, dst + at); };
+    if (OUT) copy(tx.at, tx, 0);
+    if (HEADS == 2) copy(next_g + 1 < heads ? tx.at + tx.head : tx.at, tx, kTile);   // (or the last one once more)
+    copy(ty.at, ty, kY);
+    copy(tz.at, tz, kZ);
     // past the end the last item is copied again, and not read
-    if (next_g + 1 < heads) {
-      ++next_g;
-      tx.at += tx.head, ty.at += ty.head, tz.at += tz.head;
+    if (next_g + HEADS < heads) {
+      next_g += HEADS;
+      tx.at += HEADS * tx.head, ty.at += ty.head, tz.at += tz.head;
     } else if (next_c + 1 < p.chunks) {
-      auto on = [&](Tile& t) { t.at += int64_t(kDown ? -kChunk : kChunk) * t.token - (heads - 1) * t.head; };
+      auto on = [&](Tile& t) { t.at += int64_t(kDown ? -kChunk : kChunk) * t.token - next_g * t.head; };
       on(tx), on(ty), on(tz);
       ++next_c, next_g = 0;
       next_t += kDown ? -kChunk : kChunk;
@@ -171,7 +183,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   };
   if (p.chunks > 0) {
     issue(0);
-    issue(1);
+    if (HEADS == 1) issue(1);
   }
 
   // M: y-dim 32 (b / 2) + 8 q + 4 (b % 2) + r, z-dim 16 wave + rp
@@ -247,9 +259,9 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   const double dp = period == kPeriod ? dw4 : dw;
   const float whole_hi = float(dp), whole_lo = float(dp - double(whole_hi)), rest_dec = float(power(max(rest, 0)));
   meet_lds();                                          // (M and the first copies are on their way)
-  // P: a quarter for each of the first four waves, x_t.y_j for j = pj .. pj + 3 and t = pt
-  const bool scores = OUT && wave < 4;
-  const int pj = 16 * (wave >> 1) + 4 * q, pt = 16 * (wave & 1) + rp;
+  // P: a quarter for each of the first four waves (of the second head for the others), x_t.y_j for j = pj .. pj + 3 and t = pt
+  const bool scores = OUT && (HEADS == 2 || wave < 4);
+  const int pj = 16 * ((wave >> 1) & (HEADS == 2 ? 1 : 3)) + 4 * q, pt = 16 * (wave & 1) + rp;
   float pw[4];
   bool seen[4];
 #pragma unroll
@@ -272,16 +284,16 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     px[k] = lds0 + uint32_t(rp * 128 + 16 * ((4 * k + q) ^ swz_k(rp)));
-    yt[k] = lds0 + kTile + uint32_t(r0 * 128 + 16 * ((4 * k + (rp & 3)) ^ swz_k(r0)));
+    yt[k] = lds0 + kY + uint32_t(r0 * 128 + 16 * ((4 * k + (rp & 3)) ^ swz_k(r0)));
   }
-  zt = lds0 + 2 * kTile + uint32_t(half) * kHalf + uint32_t(r0 * 128 + 16 * ((2 * (wave & 3) + ((rp >> 1) & 1)) ^ swz_k(r0)) + 8 * (rp & 1));
-  const uint32_t py_at = kTile + 2048 * uint32_t((wave >> 1) & 1), px_at = 2048 * uint32_t(wave & 1);
+  zt = lds0 + kZ + uint32_t(half) * kHalf + uint32_t(r0 * 128 + 16 * ((2 * (wave & 3) + ((rp >> 1) & 1)) ^ swz_k(r0)) + 8 * (rp & 1));
+  const uint32_t py_at = kY + 2048 * uint32_t((wave >> 1) & 1), px_at = 2048 * uint32_t(wave & 1) + (HEADS == 2 ? kTile * uint32_t(half) : 0);
   // P's place of j: 8 (j % 16 / 4) + 4 (j / 16) + j % 4, as the k-slots of Z^T
-  const uint32_t pput = lds0 + kP + uint32_t(pt) * kRow + 2 * (8 * q + 4 * ((wave >> 1) & 1));
+  const uint32_t pput = lds0 + kP + (HEADS == 2 ? uint32_t(half) * kChunk * kRow : 0) + uint32_t(pt) * kRow + 2 * (8 * q + 4 * ((wave >> 1) & 1));
   const uint32_t pget = lds0 + kP + uint32_t(rp) * kRow + 16 * q;
   const uint32_t kwt = lds0 + kTable + 4 * (kPowers + 4 * q);
 
-  f32x4 os[2];                                         // O^T of tokens rp and 16 + rp
+  f32x4 os[HEADS][2];                                  // O^T of tokens rp and 16 + rp
   const int out_heads = geo.kv_heads * (BACK ? 1 : G);
   // a result on its way: through the place of x in LDS, from where whole rows are stored, by the wave that then copies the next
   // item's rows there
@@ -289,15 +301,20 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   const uint32_t get = lds0 + mine + 16 * lane;
   uint16_t* const out_row = OUT ? out + (p.row + (geo.step == nullptr ? int64_t(p.seq) * p.rows : 0)) * out_heads * kD + 64 * half +
                                       int64_t(crow) * out_heads * kD + cchunk / 2 : nullptr;
-  int held_n = 0;                                      // its rows, or none
+  int held_n = 0, held_heads = 0;                      // its rows, or none
   int64_t held_at = 0;
-  bf16x8 going;
-  auto fetch = [&](uint32_t stage) { going = lds_row(get + stage * kStage); };
+  bf16x8 going[HEADS];
+  auto fetch = [&](uint32_t stage) {
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) going[i] = lds_row(get + stage * kStage + i * kTile);
+  };
   auto store = [&] {                                   // (waits for what was read: before the copies to its place)
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     __builtin_amdgcn_s_waitcnt(waitcnt_lds());
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    if (crow < held_n) *reinterpret_cast<bf16x8*>(out_row + held_at) = going;
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i)
+      if (crow < held_n && (i == 0 || held_heads > 1)) *reinterpret_cast<bf16x8*>(out_row + held_at + i * kD) = going[i];
     held_n = 0;
   };
   float err = 0.f;                                     // of the factors so far, relative
@@ -307,13 +324,13 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   bool full = true;
   bf16x8 z;                                            // Z^T: z-dim zd, tokens 4 q .. + 3 and 16 more
   auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-  auto before = [&] { return stage == 0 ? 2 : stage - 1; };
+  auto before = [&] { return stage == 0 ? kStages - 1 : stage - 1; };
 
   // An item's way to its result; FIRST: the first query head of the chunk.  Products and vector work are dealt out so that each
   // has the other to run beside.
   auto result = [&](auto first, int g) {
     constexpr bool kOfM = decltype(first)::value || !BACK;   // (backwards the sum over the query heads begins)
-    // (its parts are formed anew for each query head: held, they would take 32 registers that are not there)
+    // (its parts are formed anew for each item: held, they would take 32 registers that are not there)
     if (kOfM) asm volatile("" : "+v"(S[0]), "+v"(S[1]), "+v"(S[2]), "+v"(S[3]), "+v"(S[4]), "+v"(S[5]), "+v"(S[6]), "+v"(S[7]));
     // this wave's quarter of P^T = Y X^T
     f32x4 s = f32x4{};
@@ -324,7 +341,8 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_row(c + py_at), lds_row(c + px_at), s, 0, 0, 0);
       }
     }
-    auto row = [&](int ks, int tb) { return lds_row(px[ks & 1] + (ks >> 1) * kHalf + 2048 * tb); };
+    // X of step u / HEADS, query head u % HEADS
+    auto row = [&](int u, int tb) { return lds_row(px[(u / HEADS) & 1] + (u / HEADS >> 1) * kHalf + (u % HEADS) * kTile + 2048 * tb); };
     bf16x8 x[2][2];
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) x[0][tb] = row(0, tb);
@@ -350,27 +368,35 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     }
     if (kOfM) {
 #pragma unroll
-      for (int tb = 0; tb < 2; ++tb) os[tb] = f32x4{};
+      for (int i = 0; i < 2 * HEADS; ++i) os[i >> 1][i & 1] = f32x4{};
+      bf16x8 hi, lo;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
+      for (int u = 0; u < 4 * HEADS; ++u) {
+        const int ks = u / HEADS, i = u % HEADS;
         fence();
-        if (ks + 1 < 4)
+        if (u + 1 < 4 * HEADS)
 #pragma unroll
-          for (int tb = 0; tb < 2; ++tb) x[(ks + 1) & 1][tb] = row(ks + 1, tb);
-        float m[8];
+          for (int tb = 0; tb < 2; ++tb) x[(u + 1) & 1][tb] = row(u + 1, tb);
+        if (i == 0) {
+          float m[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m[e] = S[2 * ks + (e >> 2)][e & 3];
-        const bf16x8 hi = top_part(m), lo = last_part(m);
+          for (int e = 0; e < 8; ++e) m[e] = S[2 * ks + (e >> 2)][e & 3];
+          hi = top_part(m), lo = last_part(m);
+        }
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb) os[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, x[ks & 1][tb], os[tb], 0, 0, 0);
+        for (int tb = 0; tb < 2; ++tb) os[i][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, x[u & 1][tb], os[i][tb], 0, 0, 0);
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb) os[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, x[ks & 1][tb], os[tb], 0, 0, 0);
+        for (int tb = 0; tb < 2; ++tb) os[i][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, x[u & 1][tb], os[i][tb], 0, 0, 0);
       }
     }
     fence();
     if (kOfM)
 #pragma unroll
-      for (int tb = 0; tb < 2; ++tb) os[tb] *= (full ? row_whole[tb] : row_rest[tb]) * tab[kPowers + kWeights + phase];
+      for (int tb = 0; tb < 2; ++tb) {
+        const float weight = (full ? row_whole[tb] : row_rest[tb]) * tab[kPowers + kWeights + phase];
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) os[i][tb] *= weight;
+      }
     bf16x8 zf = z;
     const uint4 u = __builtin_bit_cast(uint4, z);
     const uint32_t bits = odd_halves(u.x) | odd_halves(u.y) | odd_halves(u.z) | odd_halves(u.w);
@@ -393,10 +419,12 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     }
     meet_lds();                                        // P is there, and nobody needs x any more
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int i = 0; i < HEADS; ++i)
 #pragma unroll
-      for (int tb = 0; tb < 2; ++tb)
-        os[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zf, lds_row(pget + 64 * k + 16 * kRow * tb), os[tb], 0, 0, 0);
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+          os[i][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zf, lds_row(pget + 64 * k + 16 * kRow * tb + i * kChunk * kRow), os[i][tb], 0, 0, 0);
     if (seldom(any_odd)) {
       stay();
 #pragma unroll
@@ -404,16 +432,21 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
         const int of = __shfl(odd, 4 * q + r);
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb)
-          if (BACK ? 16 * tb + rp <= of : 16 * tb + rp >= of) os[tb][r] = __builtin_nanf("");
+          if (BACK ? 16 * tb + rp <= of : 16 * tb + rp >= of)
+#pragma unroll
+            for (int i = 0; i < HEADS; ++i) os[i][tb][r] = __builtin_nanf("");
       }
     }
   };
   auto keep = [&](int g) {                             // the result, to be stored behind the next barrier
 #pragma unroll
-    for (int tb = 0; tb < 2; ++tb) {
-      *(lds_u32x2*)(uintptr_t)(put + 2048 * tb) = u32x2{pack_bf16x2(os[tb][0], os[tb][1]), pack_bf16x2(os[tb][2], os[tb][3])};
-    }
+    for (int i = 0; i < HEADS; ++i)
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb)
+        *(lds_u32x2*)(uintptr_t)(put + 2048 * tb + i * kTile) =
+            u32x2{pack_bf16x2(os[i][tb][0], os[i][tb][1]), pack_bf16x2(os[i][tb][2], os[i][tb][3])};
     held_n = n;
+    held_heads = G - g;
     held_at = (int64_t(chunk) * kChunk * out_heads + (BACK ? h : h * G + g)) * kD;
   };
   // M past the chunk (of its first query head, backwards), and the present item's part.
@@ -460,7 +493,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     fence();
   };
   auto begin_item = [&] {
-    meet<OUT ? 3 : 2>();                               // this item has landed, and the last one's buffer is free
+    meet<HEADS == 2 ? 0 : OUT ? 3 : 2>();              // this item has landed, and the last one's buffer is free
     if (OUT) fetch(before());
     else issue(before());
     z = lds_tr2(zt, zt + 2048);
@@ -472,8 +505,8 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     }
   };
   auto end_item = [&] {
-    const uint32_t d = stage == 2 ? uint32_t(-2) * kStage : kStage;
-    stage = stage == 2 ? 0 : stage + 1;
+    const uint32_t d = stage == kStages - 1 ? uint32_t(1 - kStages) * kStage : kStage;
+    stage = stage == kStages - 1 ? 0 : stage + 1;
 #pragma unroll
     for (int k = 0; k < 2; ++k) px[k] += d, yt[k] += d;
     zt += d, put += d;
@@ -497,14 +530,15 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
         end_item();
       }
     } else {
-      for (int g = 0; g < heads - 1; ++g) {            // (without results there is one item a chunk)
+      int g = 0;
+      for (; g + HEADS < heads; g += HEADS) {          // (without results there is one item a chunk)
         result(yes, g);
         keep(g);
         end_item();
         begin_item();
       }
-      if (OUT) result(yes, G - 1);
-      advance(yes, [&] { if (OUT) keep(G - 1); });
+      if (OUT) result(yes, g);
+      advance(yes, [&] { if (OUT) keep(g); });
       end_item();
     }
     if (!OUT) far *= full ? dw : double(rest_dec);
@@ -536,7 +570,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
   }
 }
 
-template <bool BACK, int PARTS>
+template <bool BACK, int PARTS, int HEADS>
 __device__ __forceinline__ void run_walk(const Geo& geo, const Walk& w, bool trans, int idx, uint8_t* smem) {
   const Place p = place(geo, idx);
   if (p.seq < 0) return;
@@ -551,22 +585,23 @@ __device__ __forceinline__ void run_walk(const Geo& geo, const Walk& w, bool tra
     else begin = w.first + at;
   }
   if (!geo.scanned) sums = start;
-  walk<BACK, true, PARTS>(geo, p, w.x, w.y, w.z, w.out, begin, sums, trans, ends && w.last != nullptr ? w.last + at : nullptr, smem);
+  walk<BACK, true, PARTS, HEADS>(geo, p, w.x, w.y, w.z, w.out, begin, sums, trans, ends && w.last != nullptr ? w.last + at : nullptr, smem);
 }
 
+template <int HEADS>
 __global__ __launch_bounds__(kThreads, 4) void linear_fwd_kernel(WalkArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kShared];
-  run_walk<false, 3>(a.geo, a.walk[0], false, blockIdx.x, smem);
+  run_walk<false, 3, HEADS>(a.geo, a.walk[0], false, blockIdx.x, smem);
 }
 
 // dk, dv and dq (dk's and dq's M are what is given transposed) of eight workgroups' places one after the other: a place's three lie on one XCD, and share their reads there.
-template <int PARTS>
+template <int PARTS, int HEADS>
 __global__ __launch_bounds__(kThreads, 4) void linear_bwd_kernel(WalkArgs a, int groups) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kShared];
   const int b = blockIdx.x / 24, r = blockIdx.x % 24, idx = 8 * b + r % 8;
   if (idx >= groups) return;
-  if (r < 16) run_walk<true, PARTS>(a.geo, a.walk[r / 8], r < 8, idx, smem);
-  else run_walk<false, 2>(a.geo, a.walk[2], true, idx, smem);
+  if (r < 16) run_walk<true, PARTS, 1>(a.geo, a.walk[r / 8], r < 8, idx, smem);
+  else run_walk<false, 2, HEADS>(a.geo, a.walk[2], true, idx, smem);
 }
 
 template <int PARTS>
@@ -578,13 +613,13 @@ __global__ __launch_bounds__(kThreads, 4) void linear_parts_kernel(PartArgs a, i
   if (p.seq < 0 || p.chunks == 0) return;
   float* const to = s.starts + size_t(idx) * kState;
   if (s.back) {
-    if (p.part > 0) walk<true, false, PARTS>(a.geo, p, s.y, s.y, s.z, nullptr, nullptr, nullptr, false, to, smem);
+    if (p.part > 0) walk<true, false, PARTS, 1>(a.geo, p, s.y, s.y, s.z, nullptr, nullptr, nullptr, false, to, smem);
   } else if (p.part == p.parts - 1) {
     if (a.geo.scanned || s.first == nullptr || !p.held) return;
     const float* const from = s.first + (size_t(p.seq) * a.geo.kv_heads + p.h) * kState;
     for (int i = 4 * threadIdx.x; i < kState; i += 4 * kThreads) *reinterpret_cast<f32x4*>(to + i) = *reinterpret_cast<const f32x4*>(from + i);
   } else {
-    walk<false, false, PARTS>(a.geo, p, s.y, s.y, s.z, nullptr, nullptr, nullptr, false, to, smem);
+    walk<false, false, PARTS, 1>(a.geo, p, s.y, s.y, s.z, nullptr, nullptr, nullptr, false, to, smem);
   }
 }
 
@@ -662,14 +697,16 @@ hipError_t launch_linear_scan(const PartArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, hipStream_t stream) {
-  linear_fwd_kernel<<<dim3(unsigned(groups)), kThreads, 0, stream>>>(a);
+  if (!two_heads(a.geo.group)) linear_fwd_kernel<1><<<dim3(unsigned(groups)), kThreads, 0, stream>>>(a);
+  else linear_fwd_kernel<2><<<dim3(unsigned(groups)), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_linear_bwd(const WalkArgs& a, int32_t groups, bool exact, hipStream_t stream) {
   const unsigned grid = (unsigned(groups) + 7) / 8 * 24;
-  if (exact) linear_bwd_kernel<3><<<dim3(grid), kThreads, 0, stream>>>(a, groups);
-  else linear_bwd_kernel<2><<<dim3(grid), kThreads, 0, stream>>>(a, groups);
+  auto run = [&](auto kernel) { kernel<<<dim3(grid), kThreads, 0, stream>>>(a, groups); };
+  if (!two_heads(a.geo.group)) exact ? run(linear_bwd_kernel<3, 1>) : run(linear_bwd_kernel<2, 1>);
+  else exact ? run(linear_bwd_kernel<3, 2>) : run(linear_bwd_kernel<2, 2>);
   return hipGetLastError();
 }
 

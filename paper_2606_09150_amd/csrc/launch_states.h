@@ -68,6 +68,10 @@ struct PartArgs {
 };
 
 constexpr int kScanSlices = 16;              // of a state, workgroups of the scan
+// Whether forward walks (o, dq) take two query heads an item, which share M's parts, y, z and the barriers.  One / two (us): 1 x 16,384
+// tokens, 8 key heads of 4, forward 143 / 128, backward 325 / 317; 2 x 4,000, 16 of 2, 83 / 73, 184 / 182; 2 x 6,000, 8 of 8, 164 / 148,
+// 447 / 423; 1 x 16,000, 6 of 3 (an item of one head twice), 94 / 97, 190 / 197.
+inline bool two_heads(int group) { return group % 2 == 0 || group > 3; }
 // exact: states are results in fp32, or bear on one
 hipError_t launch_linear_parts(const PartArgs& a, int32_t groups, bool exact, hipStream_t stream);
 hipError_t launch_linear_scan(const PartArgs& a, hipStream_t stream);

@@ -78,7 +78,7 @@ bool scanned(int64_t parts, double groups, int walks) { return parts > 4 && (wal
 // heads, 192: 95, 384: 77, 576: 87, 768: 83.
 int32_t part_chunks(int64_t all, int64_t longest, int64_t n, int64_t heads, int walks, int group) {
   const int sums = walks > 1 ? 2 : 1;
-  const double item = 0.35 + 0.65 * group, sum = walks > 1 ? 0.5 + 0.5 * group : 1.0;   // of a group's heads, for one's
+  const double item = 0.35 + (walks == 1 && lin::two_heads(group) ? 0.58 : 0.65) * group, sum = walks > 1 ? 0.5 + 0.5 * group : 1.0;   // of a group's heads, for one's
   auto time = [&](int64_t c) {
     const double parts = double((longest + c - 1) / c);
     const double groups = double(heads) * (all == n * longest ? double(n) * parts

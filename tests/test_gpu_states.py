@@ -89,6 +89,9 @@ WHOLE = [
     (3, 515, 1, 2, [515, 1, 257], True),
     (1, 1100, 7, 1, None, True),                     # every decay
     (2, 800, 1, 4, [0, 799], True),
+    (2, 330, 1, 7, [330, 31], True),
+    (1, 161, 2, 6, None, False),
+    (1, 70, 1, 8, [65], True),
     # cut into parts both ways
     (1, 2500, 1, 1, None, True),
     (3, 1500, 1, 2, [1500, 37, 1409], True),
@@ -211,6 +214,33 @@ def test_values_that_are_not_finite_reach_what_sees_them(at, kind):
                     rest = torch.arange(D) != 77
                     assert torch.equal(a[0, :, 1][:, rest.cuda()], b[0, :, 1][:, rest.cuda()]), (which, name)
             assert torch.equal(a[0, keep.cuda(), 1], b[0, keep.cuda(), 1]), (which, name)
+
+
+@pytest.mark.parametrize("G", [2, 3, 5])
+@pytest.mark.parametrize("at", [0, 40, 95])
+def test_values_that_are_not_finite_and_shared_heads(G, at):
+    """A query's value stays with its head and token, a key head's reaches its own query heads only."""
+    P = require_gpu()
+    n = 110
+    q, k, v, do = (draw((1, n, h, D), i) for i, h in enumerate((2 * G, 2, 2, 2 * G)))
+    g = torch.tensor([-0.01, -0.3], device="cuda")
+    o, (dq, _, _) = P.linear_attention(q, k, v, g), P.linear_attention_bwd(q, k, v, do, g)
+    for kind in (math.nan, math.inf):
+        for name, t, head, (hit_o, hit_q) in (("q", q, G + 1, ((at, at + 1, G + 1, G + 2, None), None)),
+                                              ("k", k, 1, ((at, n, G, 2 * G, None), (at, n, G, 2 * G, 77))),
+                                              ("v", v, 1, ((at, n, G, 2 * G, 77), (at, n, G, 2 * G, None))),
+                                              ("do", do, G + 1, (None, (at, at + 1, G + 1, G + 2, None)))):
+            was = t[0, at, head, 77].item()
+            t[0, at, head, 77] = kind
+            got = (P.linear_attention(q, k, v, g), P.linear_attention_bwd(q, k, v, do, g)[0])
+            t[0, at, head, 77] = was
+            for a, b, hit in zip(got, (o, dq), (hit_o, hit_q)):
+                same = torch.ones_like(a, dtype=torch.bool)
+                if hit is not None:
+                    t0, t1, h0, h1, column = hit
+                    same[0, t0:t1, h0:h1, column if column is not None else slice(None)] = False
+                    assert not a[~same].isfinite().any(), (name, kind)
+                assert torch.equal(a[same], b[same]), (name, kind)
 
 
 # ---- the cache ----------------------------------------------------------------------
