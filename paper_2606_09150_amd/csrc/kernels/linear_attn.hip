@@ -58,7 +58,7 @@ using tok::swz_k;
 constexpr int kThreads = 512;
 constexpr uint32_t kTile = 8192, kHalf = 4096;
 // LDS behind the stages: P, a row of 32 values in two parts (and 16 bytes, so that rows begin in banks of their own) for each
-// token; then, in floats, L^e for e = 0 .. 32, the key weights of a period's chunks and of the last one, and what M is read with.
+// token; then, in floats, L^e for e = 0 .. 32 and M's factors, the key weights of a period's chunks and of the last one, and what M is read with.
 constexpr uint32_t kRow = 144;
 constexpr int kPowers = 36;
 constexpr int kPeriod = 4, kWeights = (kPeriod + 1) * kChunk;
@@ -257,7 +257,12 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     tab[kPowers + kWeights + tid - 192] = float(1.0 / f);
   }
   const double dp = period == kPeriod ? dw4 : dw;
-  const float whole_hi = float(dp), whole_lo = float(dp - double(whole_hi)), rest_dec = float(power(max(rest, 0)));
+  // (M's factors, in two floats, and the last chunk's: in LDS, for a spilled register's load waits for the copies on their way)
+  if (tid == 256) {
+    tab[33] = float(dp);
+    tab[34] = float(dp - double(float(dp)));
+    tab[35] = float(power(max(rest, 0)));
+  }
   meet_lds();                                          // (M and the first copies are on their way)
   // P: a quarter for each of the first four waves (of the second head for the others), x_t.y_j for j = pj .. pj + 3 and t = pt
   const bool scores = OUT && (HEADS == 2 || wave < 4);
@@ -270,13 +275,9 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     pw[r] = scale * tab[min(max(age, 0), 32)];
     seen[r] = age >= 0;
   }
-  float row_whole[2], row_rest[2];                     // of tokens rp and 16 + rp
+  float row_whole[2];                                  // of tokens rp and 16 + rp
 #pragma unroll
-  for (int tb = 0; tb < 2; ++tb) {
-    const int t = 16 * tb + rp;
-    row_whole[tb] = BACK ? tab[31 - t] : scale * tab[t + 1];
-    row_rest[tb] = BACK ? tab[max(rest - 1 - t, 0)] : row_whole[tb];
-  }
+  for (int tb = 0; tb < 2; ++tb) row_whole[tb] = BACK ? tab[31 - 16 * tb - rp] : scale * tab[16 * tb + rp + 1];
 
   // operand addresses within a stage (16 rows further: 2,048 bytes)
   uint32_t px[2], yt[2], zt, put;                      // (of the present stage)
@@ -393,7 +394,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     if (kOfM)
 #pragma unroll
       for (int tb = 0; tb < 2; ++tb) {
-        const float weight = (full ? row_whole[tb] : row_rest[tb]) * tab[kPowers + kWeights + phase];
+        const float weight = (BACK && !full ? tab[max(rest - 1 - 16 * tb - rp, 0)] : row_whole[tb]) * tab[kPowers + kWeights + phase];
 #pragma unroll
         for (int i = 0; i < HEADS; ++i) os[i][tb] *= weight;
       }
@@ -455,9 +456,9 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
     const bool forget = OUT && decltype(first)::value && (phase == 0 || !full);
     float dec = 1.f;
     if (forget) {
-      const float want = whole_lo + err;
-      dec = full ? whole_hi + want : rest_dec * tab[kPowers + kWeights + phase];
-      if (full) err = want - (dec - whole_hi);
+      const float whole = tab[33], want = tab[34] + err;
+      dec = full ? whole + want : tab[35] * tab[kPowers + kWeights + phase];
+      if (full) err = want - (dec - whole);
     }
     const uint32_t kw = kwt + 4u * kChunk * uint32_t(full ? phase : kPeriod);
     if (forget) {
@@ -541,7 +542,7 @@ __device__ __forceinline__ void walk(const Geo& geo, const Place& p, const Src& 
       advance(yes, [&] { if (OUT) keep(g); });
       end_item();
     }
-    if (!OUT) far *= full ? dw : double(rest_dec);
+    if (!OUT) far *= full ? dw : double(tab[35]);
     phase = full && phase + 1 < period ? phase + 1 : 0;
   }
   meet<0>();                                           // no copy outlives the walk
