@@ -12,8 +12,7 @@
 //
 // Where states are few a wave has 32 of their rows, all tokens' k, v and queries come through LDS at once,
 // and the waves' sums meet there behind the last token: a wave's way through a token is as long as its part of a state.
-// Rows split / whole (us): 8 states, 8 tokens 6.8 / 10.3; 192 states of 2 query heads, 7 tokens 13.3 / 14.6; 512 states, 2 tokens
-// 14.9 / 11.8.
+// Rows split / whole (us): 192 states of 2 query heads, 4 tokens 9.6 / 10.9; 512 states, 2 tokens 14.9 / 11.8.
 //
 // L goes as two floats: one would be off by the same 2^-25 in each of thousands of steps.
 #include <algorithm>

@@ -78,9 +78,10 @@ hipError_t launch_linear_scan(const PartArgs& a, hipStream_t stream);
 hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, hipStream_t stream);
 hipError_t launch_linear_bwd(const WalkArgs& a, int32_t groups, bool exact, hipStream_t stream);
 
-// Few tokens a sequence: token by token.  So / in chunks (us): 24 sequences of 8 key heads of 2, 2 tokens 7.4 / 12.6, 4 9.6 / 12.6,
-// 7 13.0 / 12.5; 64 of 8, 4 14.2 / 18.1, 8 20.3 / 18.3; 64 of 32, 2 41.8 / 58.4, 8 58.4 / 59.5; 1 of 8 heads of 8, 4 11.6 / 18.3.
-constexpr int kFewTokens = 8;
+// Few tokens a sequence: token by token.  So / in chunks (us): 1 sequence of 8 key heads, 4 tokens 5.0 / 7.1, 8 6.8 / 7.1; 24 of 8 heads of 2,
+// 4 9.7 / 10.6, 5 10.8 / 10.5, 7 13.1 / 10.1; 64 of 8, 4 14.3 / 15.1, 6 17.4 / 15.4; 64 of 32, 4 46.6 / 52.5, 6 51.6 / 53.2, 8 58.6 /
+// 52.7; 64 of 32 heads of 4, 4 60.2 / 63.8; 16 of 32 heads of 8, 2 18.9 / 26.1, 4 30.0 / 26.5.
+constexpr int kFewTokens = 4;
 struct StepArgs {
   Geo geo;                    // of a step
   Src q, k, v;

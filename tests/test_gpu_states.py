@@ -283,6 +283,7 @@ STEPS = [
     (1, 1, [([0], [1]), ([0], [1]), ([0], [33])]),
     (2, 3, [([2, 0], [5, 8]), ([0, 1, 2], [1, 0, 8]), ([1, 2], [9, 1])]),
     (1, 11, [([0, 1], [3, 2]), ([1], [1])]),                                   # more query heads than a block takes
+    (1, 20, [([0, 2], [4, 3]), ([2], [2])]),
     (3, 1, [([0, 1, 2], [700, 1, 33]), ([2, 1, 0], [1, 1, 1]), ([0, 2], [257, 300])]),   # parts; unequal
     (2, 2, [([3, 1], [0, 290]), ([3], [31]), ([3, 1], [2, 70])]),
 ]

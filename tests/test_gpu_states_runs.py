@@ -71,6 +71,7 @@ REPLAYED = [
     (2, 2, [3, 0], [1, 1]),
     (64, 2, [4, 1, 2, 0, 3], [1, 2, 1, 1, 0]),
     (1, 11, [0, 2], [8, 3]),
+    (1, 18, [0, 2], [4, 3]),
     (2, 1, [1, 3, 2], [40, 40, 1]),
     (1, 2, [2, 0, 1], [1300, 1300, 5]),
 ]
