@@ -45,8 +45,9 @@ extern "C" {
  * else).
  *
  * Sequences are cut into parts where that fills the GPU; the states between them lie
- * in d_work (16-byte aligned, >= ufs_linear_work_bytes; 0 bytes: may be NULL).  scale:
- * finite.  Errors: UF_ERR_ARG, UF_ERR_UNSUPPORTED (head_dim), UF_ERR_HIP.
+ * in d_work (16-byte aligned, >= ufs_linear_work_bytes; 0 bytes: may be NULL).  A part of
+ * a sequence's key head is a workgroup, of which there are at most 2^23 - 1 (else
+ * UF_ERR_ARG, of the sizes' queries too).  scale: finite.  Errors: UF_ERR_ARG, UF_ERR_UNSUPPORTED (head_dim), UF_ERR_HIP.
  *
  * Backward: d_do [batch, tokens, q_heads, head_dim] bf16 contiguous; d_dfinal, NULL
  * (zeros) or the gradient of the final states, fp32; outputs d_dq (as q) and d_dk, d_dv

@@ -40,6 +40,7 @@
 #include "linear_place.h"
 #include "token_common.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace uf {
@@ -55,7 +56,7 @@ using tok::lds_row;
 using tok::lds_tr2;
 using tok::swz_k;
 
-constexpr int kThreads = 512;
+constexpr int kThreads = kWalkThreads;
 constexpr uint32_t kTile = 8192, kHalf = 4096;
 // LDS behind the stages: P, a row of 32 values in two parts (and 16 bytes, so that rows begin in banks of their own) for each
 // token; then, in floats, L^e for e = 0 .. 32 and M's factors, the key weights of a period's chunks and of the last one, and what M is read with.
@@ -596,10 +597,11 @@ __global__ __launch_bounds__(kThreads, 4) void linear_fwd_kernel(WalkArgs a) {
 }
 
 // dk, dv and dq (dk's and dq's M are what is given transposed) of eight workgroups' places one after the other: a place's three lie on one XCD, and share their reads there.
+// Places first .. groups - 1, as far as the launch reaches.
 template <int PARTS, int HEADS>
-__global__ __launch_bounds__(kThreads, 4) void linear_bwd_kernel(WalkArgs a, int groups) {
+__global__ __launch_bounds__(kThreads, 4) void linear_bwd_kernel(WalkArgs a, int first, int groups) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kShared];
-  const int b = blockIdx.x / 24, r = blockIdx.x % 24, idx = 8 * b + r % 8;
+  const int b = blockIdx.x / 24, r = blockIdx.x % 24, idx = first + 8 * b + r % 8;
   if (idx >= groups) return;
   if (r < 16) run_walk<true, PARTS, 1>(a.geo, a.walk[r / 8], r < 8, idx, smem);
   else run_walk<false, 2, HEADS>(a.geo, a.walk[2], true, idx, smem);
@@ -627,8 +629,8 @@ __global__ __launch_bounds__(kThreads, 4) void linear_parts_kernel(PartArgs a, i
 // Parts' beginnings from their own M, part by part, kAhead of them read at once.  A workgroup per (sequence, key head,
 // sixteenth of M).
 constexpr int kAhead = 16;
-static_assert(kScanSlices * 1024 == kState);
-__global__ __launch_bounds__(256) void linear_scan_kernel(PartArgs a) {
+static_assert(kScanSlices * 4 * kOtherThreads == kState);
+__global__ __launch_bounds__(kOtherThreads) void linear_scan_kernel(PartArgs a) {
   const Geo& geo = a.geo;
   int k = blockIdx.x;
   const int slice = k % kScanSlices;
@@ -693,7 +695,7 @@ hipError_t launch_linear_parts(const PartArgs& a, int32_t groups, bool exact, hi
 }
 
 hipError_t launch_linear_scan(const PartArgs& a, hipStream_t stream) {
-  linear_scan_kernel<<<dim3(unsigned(kScanSlices * a.geo.kv_heads) * a.geo.n * a.n), 256, 0, stream>>>(a);
+  linear_scan_kernel<<<dim3(unsigned(kScanSlices * a.geo.kv_heads) * a.geo.n * a.n), kOtherThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -704,11 +706,16 @@ hipError_t launch_linear_fwd(const WalkArgs& a, int32_t groups, hipStream_t stre
 }
 
 hipError_t launch_linear_bwd(const WalkArgs& a, int32_t groups, bool exact, hipStream_t stream) {
-  const unsigned grid = (unsigned(groups) + 7) / 8 * 24;
-  auto run = [&](auto kernel) { kernel<<<dim3(grid), kThreads, 0, stream>>>(a, groups); };
-  if (!two_heads(a.geo.group)) exact ? run(linear_bwd_kernel<3, 1>) : run(linear_bwd_kernel<2, 1>);
-  else exact ? run(linear_bwd_kernel<3, 2>) : run(linear_bwd_kernel<2, 2>);
-  return hipGetLastError();
+  // three walks a place: as many launches as their threads need (no walk waits for another)
+  constexpr int32_t kMost = int32_t(most_groups(kThreads) / 24 * 8);
+  for (int32_t first = 0; first < groups; first += std::min(kMost, groups - first)) {
+    const unsigned grid = unsigned((std::min(kMost, groups - first) + 7) / 8 * 24);
+    auto run = [&](auto kernel) { kernel<<<dim3(grid), kThreads, 0, stream>>>(a, first, groups); };
+    if (!two_heads(a.geo.group)) exact ? run(linear_bwd_kernel<3, 1>) : run(linear_bwd_kernel<2, 1>);
+    else exact ? run(linear_bwd_kernel<3, 2>) : run(linear_bwd_kernel<2, 2>);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace lin

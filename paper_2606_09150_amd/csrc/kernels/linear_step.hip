@@ -27,7 +27,7 @@ using namespace attn;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kOtherThreads;
 
 // Sums over the lanes of the same columns (lane % 8), in all of them.
 __device__ inline float column_sum(float x) {

@@ -30,7 +30,7 @@ namespace uf {
 namespace lin {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = kOtherThreads, kWaves = 4;
 constexpr int kEach = 16;                              // values of a lane and block
 constexpr int kBlock = 64 * kEach;                     // of a wave and block
 constexpr int kRoom = kBlock + 128, kMine = kRoom / 64;   // keys of a wave's list; of a lane

@@ -14,6 +14,10 @@ constexpr int kD = 128;
 constexpr int kState = kD * kD;              // floats of a state
 constexpr int kChunk = 32;                   // tokens of a chunk
 
+// Threads of a workgroup: of the walks and the parts' sums, and of all other kernels.  A launch has 2^32 - 1 threads at most.
+constexpr int kWalkThreads = 512, kOtherThreads = 256;
+constexpr int64_t most_groups(int threads) { return ((int64_t(1) << 32) - 1) / threads; }
+
 // The cache's device table, the step: kHeader words (sequences, tokens, parts, chunks of a part), then kEntry words for
 // each sequence: its number, its first token of the step, its new tokens, the tokens it held before, its first part.
 constexpr int kHeader = 4;

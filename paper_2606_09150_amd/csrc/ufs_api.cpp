@@ -22,7 +22,6 @@ using uf::ok;
 namespace lin = uf::lin;
 namespace tok = uf::tok;
 
-constexpr double kMostGroups = 16777215.0;   // workgroups of a launch: 2^32 - 1 threads
 constexpr size_t kStateBytes = size_t(lin::kState) * 4;
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -134,7 +133,12 @@ int check_linear(const ufs_linear_desc* d, int walks, lin::Geo* g) {
   g->chunks = part_chunks(chunks * d->batch, chunks, d->batch, d->kv_heads, walks, g->group);
   g->parts = int32_t((chunks + g->chunks - 1) / g->chunks);
   g->scanned = scanned(g->parts, units * g->parts, walks);
-  if ((units * std::max(g->parts, g->parts > 1 ? lin::kScanSlices : 1) + 8) * 3 > kMostGroups || double(chunks) * g->group > 2.0e9)
+  // (the backward's walks take as many launches as they need)
+  const double sums = walks > 1 ? 2.0 : 1.0;
+  if (units * g->parts > double(lin::most_groups(lin::kWalkThreads)) ||
+      (g->parts > 1 && (units * g->parts * sums > double(lin::most_groups(lin::kWalkThreads)) ||
+                        units * lin::kScanSlices * sums > double(lin::most_groups(lin::kOtherThreads)))) ||
+      double(chunks) * g->group > 2.0e9)
     return fail(UF_ERR_ARG, "shape too large: batch * q_heads * tokens");
   return UF_OK;
 }
@@ -413,7 +417,11 @@ int ufs_extend(ufs_cache* c, int32_t n, const int32_t* seqs, const int32_t* coun
       most = std::max(most, (own + part - 1) / part);
     }
     words[2] = parts;
-    if (double(std::max(parts, most > 1 ? lin::kScanSlices * n : n)) * c->d.kv_heads > kMostGroups) return fail(UF_ERR_ARG, "step too large for one launch");
+    // token by token, or walks, sums and what carries them on
+    const double heads = c->d.kv_heads, other = double(lin::most_groups(lin::kOtherThreads));
+    if (longest <= lin::kFewTokens ? n * heads > other
+                                   : parts * heads > double(lin::most_groups(lin::kWalkThreads)) || (most > 1 && lin::kScanSlices * n * heads > other))
+      return fail(UF_ERR_ARG, "step too large for one launch");
     if (!c->dry())
       for (size_t k = 0; k < words.size();) {
         tok::PokeArgs a;

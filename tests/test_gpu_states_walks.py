@@ -173,3 +173,21 @@ def test_values_that_are_not_finite_in_a_later_period(at):
                     same[1, hit, 0] = False
                     assert not a[1, hit, 0, 77].isfinite().any(), (which, name)
                 assert torch.equal(a[same], b[same]), (which, name)
+
+
+def test_more_places_than_a_launch_of_the_backward_takes():
+    """One token each: o = scale (q.k) v, dq = scale (do.v) k, dk = scale (do.v) q, dv = scale (q.k) do, at every place."""
+    P = require_gpu()
+    B, Hk = 43900, 64                                    # 2.8 million sequences and heads, of which a launch has 2,796,200
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v, do = (torch.randn((B, 1, Hk, D), generator=gen, device="cuda", dtype=torch.bfloat16) for _ in range(4))
+    g = decays(Hk)
+    got = [P.linear_attention(q, k, v, g), *P.linear_attention_bwd(q, k, v, do, g)]
+    torch.cuda.synchronize()
+    for at in range(0, B, 1000):
+        a, b, c, d = (t[at:at + 1000].double() for t in (q, k, v, do))
+        for x, y, z, result in ((a, b, c, got[0]), (d, c, b, got[1]), (c, d, a, got[2]), (b, a, d, got[3])):
+            want = SCALE * (x * y).sum(-1, keepdim=True) * z
+            a0 = SCALE * (x * y).abs().sum(-1, keepdim=True) * z.abs() * (3 * 2.0 ** -15 + O.steps(1))
+            bound = a0 + (want.abs() + a0) * O.BF16 + 1e-30        # (as the oracle's bound of a bf16 result)
+            assert ((result[at:at + 1000].double() - want).abs() <= bound).all(), at

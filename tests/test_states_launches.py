@@ -1,0 +1,126 @@
+"""Launches of the state operators as the runtime is asked for them: a host program calls libuf.so, and has the runtime's launch
+functions itself, which write down what would be launched."""
+
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+PROGRAM = r"""
+#include <cstdint>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <vector>
+#include "ufs.h"
+
+struct Dim { uint32_t x, y, z; };
+static Dim grid, block;
+static int launched = 0, fails_at = 0, error = 0;
+extern "C" {
+int __hipPushCallConfiguration(Dim g, Dim b, size_t, void*) { grid = g, block = b; return 0; }
+int __hipPopCallConfiguration(Dim* g, Dim* b, size_t* shared, void** stream) {
+  *g = grid, *b = block, *shared = 0, *stream = nullptr;
+  return 0;
+}
+int hipLaunchKernel(const void*, Dim g, Dim b, void**, size_t, void*) {
+  if (++launched == fails_at) return error = 719;
+  printf("launch %u %u %u %u\n", g.x, g.y, g.z, b.x * b.y * b.z);
+  return 0;
+}
+int hipGetLastError() { const int e = error; error = 0; return e; }
+}
+
+int main(int c, char** v) {
+  auto arg = [&](int i) { return i < c ? atoi(v[i]) : 0; };
+  char* const p = reinterpret_cast<char*>(uintptr_t(1) << 32);   // (never read: nothing runs)
+  float* const f = reinterpret_cast<float*>(p);
+  int32_t* const words = reinterpret_cast<int32_t*>(p);
+  if (!strcmp(v[1], "whole")) {                                  // batch, tokens, key heads, group
+    const int64_t H = int64_t(arg(4)) * arg(5), D = 128;
+    const uft_stride s{H * D * arg(3), H * D, D}, t{int64_t(arg(4)) * D * arg(3), arg(4) * D, D};
+    const ufs_linear_desc d{arg(2), arg(3), int32_t(H), arg(4), int32_t(D), 1.f, s, t, t};
+    for (int back = 0; back < 2; ++back) {
+      size_t need = 0;
+      int rc = back ? ufs_linear_bwd_work_bytes(&d, &need) : ufs_linear_work_bytes(&d, &need);
+      printf("size %d %zu\n", rc, need);
+      rc = back ? ufs_linear_bwd(&d, p, p, p, p, f, nullptr, f, f, p, p, p, f, p, need, nullptr)
+                : ufs_linear_fwd(&d, p, p, p, f, nullptr, f, p, f, p, need, nullptr);
+      printf("call %d\n", rc);
+    }
+  }
+  return 0;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def run(tmp_path_factory):
+    import paper_2606_09150_amd._lib as L
+    L.load()
+    d = tmp_path_factory.mktemp("launches")
+    (d / "launches.cpp").write_text(PROGRAM)
+    exe, where = str(d / "launches"), os.path.dirname(L.LIB_PATH)
+    rocm = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "lib")
+    subprocess.run(["g++", "-std=c++17", "-rdynamic", f"-I{ROOT}/include", str(d / "launches.cpp"), L.LIB_PATH, "-o", exe, f"-Wl,-rpath,{where}",
+                    f"-Wl,-rpath,{rocm}", f"-Wl,-rpath-link,{rocm}", "-Wl,--allow-shlib-undefined"], check=True)
+
+    def call(*args):
+        lines = subprocess.check_output([exe, *map(str, args)], text=True).splitlines()
+        return [(x.split()[0], *map(int, x.split()[1:])) for x in lines]
+
+    return call
+
+
+OK, BAD = 0, -1                             # status codes
+THREADS = 2 ** 32 - 1                                # of a launch
+
+
+def launches(lines):
+    return [x[1:] for x in lines if x[0] == "launch"]
+
+
+@pytest.mark.parametrize("batch,tokens,heads,group", [
+    (1, 1, 1, 1), (3, 5000, 7, 2),
+    (43690, 1, 64, 1),                               # 2,796,160 places: the backward's walks in one launch
+    (43691, 1, 64, 1), (50000, 32, 64, 1), (65535, 1, 64, 1), (65535, 1, 64, 3),   # in two
+    (131071, 1, 64, 1),                              # the most places of a launch of walks, but for 63
+])
+def test_every_call_that_is_accepted_fits_its_launches(run, batch, tokens, heads, group):
+    lines = run("whole", batch, tokens, heads, group)
+    back = max(i for i, x in enumerate(lines) if x[0] == "size")
+    assert lines[0][1] == lines[back][1] == OK
+    assert [x for x in lines if x[0] == "call"] == [("call", OK)] * 2
+    for x, y, z, threads in launches(lines):
+        assert x * threads <= THREADS and y == z == 1
+    if lines[back][2] == 0:                                    # each place once, and three walks of each backwards, of eight places together
+        places = batch * heads
+        assert launches(lines[:back]) == [(places, 1, 1, 512)]
+        walks = [x for x, _, _, _ in launches(lines[back:])]
+        assert sum(walks) == -(-places // 8) * 24 and all(x % 24 == 0 for x in walks)
+
+
+@pytest.mark.parametrize("batch,tokens,heads,group", [(131072, 1, 64, 1), (2 ** 23, 1, 1, 1), (2 ** 24, 40, 1, 1), (2 ** 30, 1, 4, 1)])
+def test_calls_of_more_places_than_a_launch_has_are_refused(run, batch, tokens, heads, group):
+    lines = run("whole", batch, tokens, heads, group)
+    bad = [x[1] for x in lines if x[0] in ("size", "call")]
+    assert len(bad) == 4 and set(bad) == {BAD} and not launches(lines)
+
+
+@pytest.mark.parametrize("heads,few,many", [(128, OK, OK), (129, OK, BAD), (256, OK, BAD), (257, BAD, BAD)])
+def test_steps_of_more_places_than_a_launch_has_are_refused(heads, few, many):
+    """Token by token a place has 256 threads, in chunks 512."""
+    import paper_2606_09150_amd as P
+    n = 65535
+    cache = P.StateCache(1, heads, n, flags=P._lib.UF_F_DRYRUN)
+    for count, status in ((4, few), (5, many)):
+        held = cache.tokens(0)
+        if status == OK:
+            cache.extend(range(n), [count] * n)
+            assert cache.step_tokens() == n * count
+        else:
+            with pytest.raises(P.UfError) as e:
+                cache.extend(range(n), [count] * n)
+            assert e.value.status == BAD and cache.tokens(0) == held
