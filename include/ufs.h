@@ -47,7 +47,8 @@ extern "C" {
  * Sequences are cut into parts where that fills the GPU; the states between them lie
  * in d_work (16-byte aligned, >= ufs_linear_work_bytes; 0 bytes: may be NULL).  A part of
  * a sequence's key head is a workgroup, of which there are at most 2^23 - 1 (else
- * UF_ERR_ARG, of the sizes' queries too).  scale: finite.  Errors: UF_ERR_ARG, UF_ERR_UNSUPPORTED (head_dim), UF_ERR_HIP.
+ * UF_ERR_ARG, of the sizes' queries too).  scale: finite.  Errors: UF_ERR_ARG,
+ * UF_ERR_UNSUPPORTED (head_dim), UF_ERR_HIP.
  *
  * Backward: d_do [batch, tokens, q_heads, head_dim] bf16 contiguous; d_dfinal, NULL
  * (zeros) or the gradient of the final states, fp32; outputs d_dq (as q) and d_dk, d_dv
@@ -106,7 +107,8 @@ int ufs_destroy(ufs_cache* cache); /* NULL is accepted */
  * holds once one of its sequences is reordered or freed.  A sequence appears once.  A
  * captured graph of ufs_attn reads the step from the table when it is replayed: it may
  * be replayed after any later step of as many sequences with the same counts.
- * Errors: UF_ERR_ARG (also: a sequence of more than 2^31 - 1 tokens), UF_ERR_HIP. */
+ * Errors: UF_ERR_ARG (also: a sequence of more than 2^31 - 1 tokens), UF_ERR_HIP (no
+ * sequence has grown; the step before may no longer hold). */
 int ufs_extend(ufs_cache* cache, int32_t n, const int32_t* seqs, const int32_t* counts, void* stream);
 
 /* Linear attention of the step's tokens: d_q [step tokens, q_heads, head_dim], d_k, d_v
@@ -137,7 +139,8 @@ int ufs_fork(ufs_cache* cache, int32_t n, const int32_t* src, const int32_t* dst
  * group had before the call; d_parents int32 [groups, beams] (device).  A parent that
  * is none of 0 .. beams-1 leaves its sequence as it is.  The sequences of a group hold
  * the same number of tokens, at least one; a sequence appears once; beams is 1 .. 64.
- * Errors: UF_ERR_ARG, UF_ERR_EMPTY (a sequence has no token), UF_ERR_HIP. */
+ * Errors: UF_ERR_ARG, UF_ERR_EMPTY (a sequence has no token), UF_ERR_HIP (the first
+ * groups may be reordered). */
 int ufs_reorder(ufs_cache* cache, int32_t groups, int32_t beams, const int32_t* seqs, const int32_t* d_parents, void* stream);
 
 /* Empty the sequences.  Host metadata only.  Errors: UF_ERR_ARG. */

@@ -4,7 +4,8 @@
 //
 // The host holds how many tokens each sequence has taken; kernels read a step's
 // sequences from a table in device memory, whose words ride in launch arguments.  A call
-// first checks, then launches, then commits: a failed call leaves the handle as it was.
+// first checks, then launches, then commits: a failed call leaves the handle as it was, but
+// for a step whose table or states some of its launches have changed, which is over.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -318,15 +319,18 @@ int check_seqs(ufs_cache* c, int64_t n, const int32_t* seqs, const char* name) {
   return s;
 }
 
+void end_step(ufs_cache* c) {
+  c->step.clear();
+  c->step_tokens = c->step_longest = c->step_parts = c->step_most = 0;
+}
+
 // A step with one of these sequences is over.
 void leave_step(ufs_cache* c, int64_t n, const int32_t* seqs) {
   for (int64_t i = 0; i < n; ++i) c->seen[size_t(seqs[i])] = 1;
   bool found = false;
   for (const Entry& e : c->step) found = found || c->seen[size_t(e.seq)];
   for (int64_t i = 0; i < n; ++i) c->seen[size_t(seqs[i])] = 0;
-  if (!found) return;
-  c->step.clear();
-  c->step_tokens = c->step_longest = c->step_parts = c->step_most = 0;
+  if (found) end_step(c);
 }
 
 bool few(const ufs_cache* c) { return c->step_longest <= lin::kFewTokens; }
@@ -430,8 +434,11 @@ int ufs_extend(ufs_cache* c, int32_t n, const int32_t* seqs, const int32_t* coun
         a.dense = a.runs = int32_t(std::min(words.size() - k, size_t(tok::kWords)));
         a.n_runs = 0;
         std::copy_n(words.begin() + k, a.dense, a.words);
+        if (int s = check_hip(tok::launch_poke(a, a.dense, static_cast<hipStream_t>(stream)), "table")) {
+          if (k > 0) end_step(c);                        // (the table is no step's any more)
+          return s;
+        }
         k += size_t(a.dense);
-        if (int s = check_hip(tok::launch_poke(a, a.dense, static_cast<hipStream_t>(stream)), "table")) return s;
       }
     for (int32_t i = 0; i < n; ++i) c->tokens[size_t(seqs[i])] += counts[i];
     c->step.swap(step);
@@ -579,7 +586,10 @@ int ufs_reorder(ufs_cache* c, int32_t groups, int32_t beams, const int32_t* seqs
         a.groups = std::min(most, groups - g);
         a.beams = beams;
         std::copy_n(seqs + int64_t(g) * beams, a.groups * beams, a.seqs);
-        if (int s = check_hip(lin::launch_state_reorder(a, static_cast<hipStream_t>(stream)), "reorder")) return s;
+        if (int s = check_hip(lin::launch_state_reorder(a, static_cast<hipStream_t>(stream)), "reorder")) {
+          if (g > 0) leave_step(c, int64_t(g) * beams, seqs);   // (those groups' states have moved)
+          return s;
+        }
       }
     }
     leave_step(c, n, seqs);

@@ -176,8 +176,9 @@ class StateCache:
     def extend(self, seqs, counts, stream=None):
         """Begin a step: sequence seqs[i] grows by counts[i] tokens."""
         counts = S.ints(counts)
+        self._step = self._need = None                   # (a failed launch can end the step before)
         self._run(stream, lambda s: S.ufs_extend(self.handle, seqs, counts, s))
-        self._step, self._need = sum(counts), None
+        self._step = sum(counts)
 
     def fork(self, src, dst, stream=None):
         """Sequences dst[i], empty before, continue src[i]: their states are copied."""
@@ -197,8 +198,8 @@ class StateCache:
         if len(seqs) != shape[0] * shape[1]:
             raise ValueError(f"parents of {tuple(shape)} need as many sequences (got {len(seqs)})")
         tensor = None if self.dry else parents
-        self._run(stream, lambda s: S.ufs_reorder(self.handle, _int(shape[1], "beams"), seqs, tensor, s), tensor)
         self._step = self._need = None
+        self._run(stream, lambda s: S.ufs_reorder(self.handle, _int(shape[1], "beams"), seqs, tensor, s), tensor)
 
     def free(self, seqs):
         S.ufs_free(self.handle, seqs)

@@ -51,6 +51,38 @@ int main(int c, char** v) {
       printf("call %d\n", rc);
     }
   }
+  if (!strcmp(v[1], "fails")) {                                  // which call, and which of its launches fails
+    const int n = 1200, beams = 4;
+    std::vector<int32_t> seqs(n), more(n), counts(n, 7);
+    for (int i = 0; i < n; ++i) seqs[i] = i, more[i] = n + i;
+    const ufs_desc d{2, 1, 128, 2 * n, 0};
+    ufs_cache* cache;
+    size_t pool, table;
+    if (ufs_pool_bytes(&d, &pool) || ufs_table_bytes(&d, &table) || ufs_create(&d, p, pool, p, table, &cache) ||
+        ufs_extend(cache, n, seqs.data(), counts.data(), nullptr))
+      return 1;
+    launched = 0, fails_at = arg(3);
+    for (int i = 0; i < n; ++i) counts[i] = 5 + i % 2;
+    auto call = [&] {
+      return !strcmp(v[2], "extend")    ? ufs_extend(cache, n, seqs.data(), counts.data(), nullptr)
+             : !strcmp(v[2], "reorder") ? ufs_reorder(cache, n / beams, beams, seqs.data(), words, nullptr)
+                                        : ufs_fork(cache, n, seqs.data(), more.data(), nullptr);
+    };
+    auto tell = [&](int rc) {
+      ufs_info info;
+      int32_t held[2];
+      ufs_get_info(cache, &info);
+      ufs_seq_tokens(cache, 0, held);
+      ufs_seq_tokens(cache, n, held + 1);
+      const uft_stride s{0, 128, 128};
+      const ufs_attn_desc a{1, 1.f, s, s, s};
+      const int attn = ufs_attn(cache, 0, &a, p, p, p, f, p, p, 1 << 30, nullptr);
+      printf("after %d %d %d %d %d\n", rc, info.step_tokens, held[0], held[1], attn);
+    };
+    tell(call());
+    fails_at = 0;
+    tell(call());
+  }
   return 0;
 }
 """
@@ -74,7 +106,7 @@ def run(tmp_path_factory):
     return call
 
 
-OK, BAD = 0, -1                             # status codes
+OK, BAD, EMPTY, HIP = 0, -1, -4, -5                 # status codes
 THREADS = 2 ** 32 - 1                                # of a launch
 
 
@@ -124,3 +156,15 @@ def test_steps_of_more_places_than_a_launch_has_are_refused(heads, few, many):
             with pytest.raises(P.UfError) as e:
                 cache.extend(range(n), [count] * n)
             assert e.value.status == BAD and cache.tokens(0) == held
+
+
+@pytest.mark.parametrize("what,at,step,after", [
+    # tokens of the step that holds, those of a sequence and of its fork, when the launch fails and when the call is made again
+    ("extend", 1, 8400, (6600, 12, 0)), ("extend", 2, 0, (6600, 12, 0)),
+    ("reorder", 1, 8400, (0, 7, 0)), ("reorder", 2, 0, (0, 7, 0)),
+    ("fork", 1, 8400, (8400, 7, 7)), ("fork", 2, 8400, (8400, 7, 7)),
+])
+def test_a_launch_that_fails_leaves_no_step_over_what_others_changed(run, what, at, step, after):
+    lines = [x[1:] for x in run("fails", what, at) if x[0] == "after"]
+    assert lines[0] == (HIP, step, 7, 0, OK if step else EMPTY)
+    assert lines[1] == (OK, *after, OK if after[0] else EMPTY)
