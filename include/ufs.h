@@ -106,7 +106,8 @@ int ufs_destroy(ufs_cache* cache); /* NULL is accepted */
  * states past them; tokens are counted sequence by sequence.  A step no longer
  * holds once one of its sequences is reordered or freed.  A sequence appears once.  A
  * captured graph of ufs_attn reads the step from the table when it is replayed: it may
- * be replayed after any later step of as many sequences with the same counts.
+ * be replayed after any later step of as many sequences with the same counts (after
+ * another it stays within its buffers, and some sequences are left out).
  * Errors: UF_ERR_ARG (also: a sequence of more than 2^31 - 1 tokens), UF_ERR_HIP (no
  * sequence has grown; the step before may no longer hold). */
 int ufs_extend(ufs_cache* cache, int32_t n, const int32_t* seqs, const int32_t* counts, void* stream);

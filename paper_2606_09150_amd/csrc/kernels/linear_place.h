@@ -65,9 +65,11 @@ __device__ inline Place place(const Geo& g, int idx) {
   p.seq = -1;
   if (n < 1 || k >= head[2]) return p;
   entry_of(g, lo, p);
-  p.part = k - head[kHeader + kEntry * lo + 4];
+  const int first = head[kHeader + kEntry * lo + 4];
+  p.part = k - first;
   cut_into(p, chunks);
-  if (p.part >= p.parts) p.seq = -1;
+  // (a captured launch after a step that is cut otherwise: parts' states behind its own are not in its scratch)
+  if (p.part >= p.parts || first + p.parts > g.parts) p.seq = -1;
   return p;
 }
 
