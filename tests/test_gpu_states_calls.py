@@ -1,13 +1,33 @@
-"""Calls over the states of a cache that other calls do not fit: graphs that are replayed after steps of other counts."""
+"""Calls over the states of a cache at the borders of their kernels: steps of few tokens where the waves of a workgroup share a
+state, and graphs that are replayed after steps that they do not fit."""
 
 import pytest
 import torch
 
+from tests import test_gpu_states as states
 from tests import test_gpu_states_runs as runs
 from tests.gpu_common import require_gpu
 from tests.test_gpu_states import D, decays, draw
 
 pytestmark = pytest.mark.gpu
+
+
+# Few states: the waves of a workgroup have rows of the same columns, up to 4 tokens and 64 sums of tokens and query heads
+FEW = [
+    # key heads, group, sequences, counts
+    (2, 1, [1], [4]), (1, 16, [0, 2], [4, 3]),       # the last row of k and v; of queries and sums
+    (1, 17, [0, 2], [4, 3]), (1, 16, [2], [4]),      # a sum more: columns
+    (3, 21, [1, 0], [3, 3]), (63, 1, [0, 3, 2, 1], [1, 4, 2, 3]), (64, 1, [0, 3, 2, 1], [1, 4, 2, 3]),   # 252 and 256 states
+    (2, 1, [1], [5]), (1, 16, [0, 2], [5, 3]),       # in chunks
+]
+
+
+@pytest.mark.parametrize("Hk,G,seqs,counts", FEW)
+def test_steps_of_few_tokens(Hk, G, seqs, counts):
+    """Sequences that begin, and that go on."""
+    if Hk < 10:
+        states.test_steps_of_a_cache(Hk, G, [(seqs, counts)] * 2)
+    runs.test_a_captured_layer_follows_later_steps(Hk, G, seqs, counts)
 
 
 @pytest.mark.parametrize("first,second", [([2000, 1005], [1505, 1500]), ([1505, 1500], [2000, 1005])])

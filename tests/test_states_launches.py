@@ -51,6 +51,20 @@ int main(int c, char** v) {
       printf("call %d\n", rc);
     }
   }
+  if (!strcmp(v[1], "step")) {                                   // key heads, group, sequences, tokens of each
+    const int n = arg(4);
+    std::vector<int32_t> seqs(n), counts(n, arg(5));
+    for (int i = 0; i < n; ++i) seqs[i] = i;
+    const ufs_desc d{1, arg(2), 128, n, 0};
+    ufs_cache* cache;
+    size_t pool, table;
+    if (ufs_pool_bytes(&d, &pool) || ufs_table_bytes(&d, &table) || ufs_create(&d, p, pool, p, table, &cache)) return 1;
+    ufs_extend(cache, n, seqs.data(), counts.data(), nullptr);
+    const uft_stride s{0, 128 * arg(2), 128}, t{0, 128 * arg(2) * arg(3), 128};
+    const ufs_attn_desc a{arg(2) * arg(3), 1.f, t, s, s};
+    printf("size %d\n", ufs_attn_work_bytes(cache, &pool));
+    printf("call %d %zu\n", ufs_attn(cache, 0, &a, p, p, p, f, p, p, 1 << 30, nullptr), pool);
+  }
   if (!strcmp(v[1], "fails")) {                                  // which call, and which of its launches fails
     const int n = 1200, beams = 4;
     std::vector<int32_t> seqs(n), more(n), counts(n, 7);
@@ -168,3 +182,15 @@ def test_a_launch_that_fails_leaves_no_step_over_what_others_changed(run, what, 
     lines = [x[1:] for x in run("fails", what, at) if x[0] == "after"]
     assert lines[0] == (HIP, step, 7, 0, OK if step else EMPTY)
     assert lines[1] == (OK, *after, OK if after[0] else EMPTY)
+
+
+@pytest.mark.parametrize("heads,group,seqs,tokens,launch", [
+    # token by token, the columns of a state in four workgroups, or all in one (workgroups, threads); and in chunks
+    (2, 1, 1, 4, (8, 256)), (2, 1, 1, 5, (2, 512)), (1, 16, 2, 4, (8, 256)), (1, 17, 2, 4, (2, 256)), (1, 16, 2, 5, (2, 512)),
+    (3, 21, 2, 3, (24, 256)), (3, 22, 2, 3, (6, 256)), (255, 1, 1, 1, (1020, 256)), (256, 1, 1, 1, (256, 256)), (64, 1, 4, 4, (256, 256)),
+])
+def test_steps_of_few_tokens(run, heads, group, seqs, tokens, launch):
+    lines = run("step", heads, group, seqs, tokens)
+    at = lines.index(("size", OK))
+    assert lines[-1] == ("call", OK, 0)
+    assert [(x, threads) for x, _, _, threads in launches(lines[at:])] == [launch]
