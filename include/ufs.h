@@ -155,8 +155,10 @@ int ufs_seq_tokens(const ufs_cache* cache, int32_t seq, int32_t* tokens);
 /* Each of `groups` requests has `beams` hypotheses with scores (sums of log
  * probabilities; -inf: not in use) and logits over a vocabulary.  Continuation (w, t) has
  * the score
- *     score_w + (logit_wt - lse_w),   lse_w = log sum_t exp(logit_wt) rounded to fp32,
- * each step rounded to fp32.  A finished hypothesis (d_done, NULL or one byte each, not 0)
+ *     score_w + (logit_wt - lse_w),   lse_w = log sum_t exp(logit_wt),
+ * each step rounded to fp32.  lse_w comes of fp32 exponentials: before its rounding it is off
+ * by at most 2^-19 + 2^-22 m, m the mean of the row's largest logit less each, by the row's
+ * probabilities; rows of the same logits have the same bits of it.  A finished hypothesis (d_done, NULL or one byte each, not 0)
  * has the one continuation (w, end) with score_w itself, and its logits are not read.  A
  * continuation whose score is NaN or -inf is none.
  *

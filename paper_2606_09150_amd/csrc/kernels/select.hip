@@ -275,7 +275,7 @@ struct Logits {
   }
 };
 
-// A slice's results: its maximum and sum of exponentials, then its list of k + 1 (lanes bound a list to 64).
+// A slice's results: its maximum, rounded up, and sum of exponentials by it, then its list of k + 1 (lanes bound a list to 64).
 __device__ __host__ inline int listed_of(int k) { return k + 1 < 64 ? k + 1 : 64; }
 __device__ __host__ inline size_t slice_bytes(int k) { return 16 + size_t(listed_of(k)) * 8; }
 
@@ -298,7 +298,10 @@ __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
   const int v0 = split * a.slice + wave * 64 * kVectors;
 
   List list(s.keys[wave], listed_of(a.k), true, L::kRest);
-  float top = -INFINITY, sum = 0.f;
+  // Exponentials go by the maximum so far rounded up to an integer, so that a sum is weighed anew only where it falls to 1 / e or
+  // less; a block's sixteen are added in fp32, blocks in 64 bits (1,024 blocks of equal terms in fp32 had lse off by 1.5e-5).
+  float top = -INFINITY;
+  double sum = 0.0;
   uint4 next[2][kVectors];                             // two blocks ahead
   auto fetch = [&](uint4 (&to)[kVectors], int v) {
 #pragma unroll
@@ -315,8 +318,9 @@ __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
       for (int e = 0; e < kE; ++e) half[2 * u / kVectors] = fmaxf(half[2 * u / kVectors], y[u][e]);
     const float most = fmaxf(half[0], half[1]);
     if (most > top) {
-      sum *= __builtin_amdgcn_exp2f((top - most) * kLog2e);
-      top = most;
+      const float up = ceilf(most);
+      sum *= double(__builtin_amdgcn_exp2f((top - up) * kLog2e));
+      top = up;
     }
     const float off = top > -INFINITY ? top : 0.f;
     float part[4] = {0.f, 0.f, 0.f, 0.f};
@@ -324,7 +328,7 @@ __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
     for (int u = 0; u < kVectors; ++u)
 #pragma unroll
       for (int e = 0; e < kE; ++e) part[e & 3] += __builtin_amdgcn_exp2f((y[u][e] - off) * kLog2e);
-    sum += (part[0] + part[1]) + (part[2] + part[3]);
+    sum += double((part[0] + part[1]) + (part[2] + part[3]));
     if (v == v0) list.begin(ordered(half[0]), ordered(half[1]));
     // the bar as a value: -inf where all pass; the place between 0 and the largest value below it is no other value's
     const float bar = value_of(list.bar == 0x7fffffffu ? 0x7ffffffeu : list.bar);
@@ -360,10 +364,10 @@ __global__ __launch_bounds__(kThreads) void select_slices_kernel(SelectArgs a) {
   if (lane == 0) stop[wave] = all;
   __syncthreads();
   all = fmaxf(fmaxf(stop[0], stop[1]), fmaxf(stop[2], stop[3]));
-  float part = sum != 0.f ? sum * __builtin_amdgcn_exp2f((top - all) * kLog2e) : 0.f;
+  double part = sum != 0.0 ? sum * double(__builtin_amdgcn_exp2f((top - all) * kLog2e)) : 0.0;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) part += __shfl_xor(part, d);
-  if (lane == 0) ssum[wave] = double(part);
+  if (lane == 0) ssum[wave] = part;
   join(s, list);
   uint8_t* const to = a.work + size_t(blockIdx.x) * slice_bytes(a.k);
   if (tid == 0) *reinterpret_cast<float2*>(to) = make_float2(all, float((ssum[0] + ssum[1]) + (ssum[2] + ssum[3])));
