@@ -5,8 +5,8 @@
 // sum of exponentials online, and the slice's k + 1 largest logits; a second joins a request's
 // slices, forms the scores, and selects among them.  Scores are rounded, so that different logits
 // can give equal ones, and a slice's list, which goes by logits, may have left out an equal
-// score of a lower token: where the last of a list has the score of the last selected, and a smaller logit could have
-// it too, that slice is read again by scores.
+// score of a lower token: where the last of a list has the score of the last selected, and the next smaller or larger logit
+// has it too, that score is looked for in the slice again.
 //
 // A list holds 64-bit keys, the value in an order of integers, then the place, lowest
 // first: all different, so that what is selected does not depend on the order in
@@ -239,12 +239,12 @@ struct Logits {
     if (TYPE == UFS_FP16) return __half2float(__ushort_as_half(uint16_t(bits)));
     return __uint_as_float(bits);
   }
-  // The largest value below a finite one, in the logits' own type.
-  __device__ static float below(float x) {
-    auto down = [](uint32_t u, uint32_t sign) { return (u & ~sign) == 0 ? (sign | 1u) : (u & sign) ? u + 1 : u - 1; };
-    if (TYPE == UFS_BF16) return value(down(__float_as_uint(x) >> 16, 0x8000u));
-    if (TYPE == UFS_FP16) return value(down(__half_as_ushort(__float2half(x)), 0x8000u));
-    return value(down(__float_as_uint(x), 0x80000000u));
+  // The value next to a finite one, in the logits' own type.
+  __device__ static float next(float x, bool up) {
+    auto step = [&](uint32_t u, uint32_t sign) { return (u & ~sign) == 0 ? (up ? 1u : sign | 1u) : ((u & sign) != 0) == up ? u - 1 : u + 1; };
+    if (TYPE == UFS_BF16) return value(step(__float_as_uint(x) >> 16, 0x8000u));
+    if (TYPE == UFS_FP16) return value(step(__half_as_ushort(__float2half(x)), 0x8000u));
+    return value(step(__float_as_uint(x), 0x80000000u));
   }
   // A vector's bits; elements that the row does not have are -inf.
   __device__ uint4 bits(int vector) const {
@@ -434,14 +434,15 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
   __syncthreads();
   auto score_of = [&](int w, float logit) { return sscore[w] + (logit - slse[w]); };   // (float32 each)
   auto order_of = [&](float score) { return score > -INFINITY ? ordered(score) : 0u; };   // NaN is no candidate
-  // Whether a slice has to be read again where `limit` is the score that decides.
+  // Whether a slice may have left out one that is selected, where `limit` is the lowest score selected: an equal one of a lower place than a
+  // listed one, which has a larger logit then: the last one's next smaller logit has the limit's score too, or the last one's next larger.
   auto again = [&](int i, uint32_t limit) {
     const int w = i / a.splits;
     if (skind[w] != 1) return false;
     const uint64_t last = i == tid ? last_held : last_of(i);
     if (uint32_t(last >> 32) <= kNone) return false;   // (it has fewer: none was left out)
     const float x = value_of(uint32_t(last >> 32)), score = score_of(w, x);
-    return order_of(score) > kNone && order_of(score) >= limit && score_of(w, L::below(x)) == score;
+    return order_of(score) > kNone && order_of(score) >= limit && (score_of(w, L::next(x, false)) == score || score_of(w, L::next(x, true)) == score);
   };
   // An entry of a slice as a candidate: its score, and its place.
   auto candidate = [&](int slice, uint64_t key, uint32_t* place) {
@@ -487,30 +488,43 @@ __global__ __launch_bounds__(kThreads) void select_join_kernel(SelectArgs a) {
   const uint32_t limit = uint32_t(s.out[a.k - 1] >> 32);
   int reads = 0;
   for (int i = tid; i < slices; i += kThreads) reads |= again(i, limit);
-  if (__syncthreads_or(reads)) {                       // those slices by their scores, and the others' lists
+  if (__syncthreads_or(reads)) {
+    // All scores above the limit are listed (a slice that left one out would list k of them).  Equal ones of those slices are looked for in the
+    // order of their places, until there are k: rows of equal logits have them at once (one request, 131,072 of them: 176 us, of which
+    // cutting the lists down to k takes most; 4,210 where slices were read to their ends, and each block's entries put in order).
     List list(s.keys[wave], a.k, false, 10);
+    list.bar = limit - 1;
     for (int i0 = 0; i0 < listed; i0 += kThreads) {
       const int i = i0 + tid;
       uint32_t place = 0, o = 0;
       if (i < listed) o = candidate(i / n, reinterpret_cast<const uint64_t*>(slice_at(i / n) + 16)[i % n], &place);
-      if (o != 0 && again(i / n, limit)) o = 0;
+      if (o == limit && again(i / n, limit)) o = 0;
       list.room(64, false);
       list.push(o, place);
     }
     finished(list);
-    for (int i = 0; i < slices; ++i) {
-      if (!again(i, limit)) continue;
+    int found = 0;                                     // in the slices so far
+    for (int i = 0; i < slices && found < a.k; ++i) {
+      if (__ballot(again(i, limit)) == 0) continue;    // (the same for all threads)
       const int w = i / a.splits;
       const L x(a, w, g);
       const int v1 = min((i % a.splits + 1) * a.slice, (a.vocab + kE - 1) / kE);
-      for (int v = (i % a.splits) * a.slice + wave * 64; v < v1; v += kThreads) {
+      int own = 0;                                     // this wave's: k of them have lower places than what it has not read
+      for (int v = (i % a.splits) * a.slice + wave * 64; v < v1 && own < a.k; v += kThreads) {
         float y[kE];
         L::unpack(x.bits(v + lane < v1 ? v + lane : (1 << 27)), y);
         list.room(64 * kE, false);
 #pragma unroll
-        for (int e = 0; e < kE; ++e)
-          list.push(order_of(score_of(w, y[e])), uint32_t(w) * uint32_t(a.vocab) + uint32_t((v + lane) * kE + e));
+        for (int e = 0; e < kE; ++e) {
+          const bool equal = order_of(score_of(w, y[e])) == limit;
+          list.push(equal ? limit : 0u, uint32_t(w) * uint32_t(a.vocab) + uint32_t((v + lane) * kE + e));
+          own += __popcll(__ballot(equal));
+        }
       }
+      if (lane == 0) s.count[0][wave] = own;
+      __syncthreads();
+      found += (s.count[0][0] + s.count[0][1]) + (s.count[0][2] + s.count[0][3]);
+      __syncthreads();
     }
     list.raise();
     __syncthreads();
