@@ -19,9 +19,9 @@
  * Query head n reads key head n / (q_heads / kv_heads).  Scores, states and
  * accumulators are fp32; weights and states enter their products in two bf16 parts (in
  * steps of few tokens in fp32), what is added to a state in three (backwards in two where
- * d_dstate is not wanted), and every bf16 result is rounded once.  A value that is not
- * finite reaches its own token and those after it (gradients: dk and dv before it), and no
- * others.
+ * d_dstate is not wanted, and for dq's walks always: their states are no results), and every
+ * bf16 result is rounded once.  A value that is not finite reaches its own token and those
+ * after it (gradients: dk and dv before it), and no others.
  */
 #ifndef UFS_H
 #define UFS_H

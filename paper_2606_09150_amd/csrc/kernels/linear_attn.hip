@@ -30,7 +30,7 @@
 //
 // Rounding: M and P enter their products as two bf16 parts each (one alone would add as much
 // error as the result's own rounding), c Z in three, since M is a result in fp32 and carries
-// each error on (two backwards, where it is none).  L^32 in fp32 would be off by the same 2^-25 in each
+// each error on (two backwards, where it is none, as dq's never is).  L^32 in fp32 would be off by the same 2^-25 in each
 // of thousands of chunks: the part of it that fp32 drops is carried on and added to the next factor.
 //
 // Memory: three tiles of 8 KB an item (a chunk and query head), in two blocks of 64 dimensions in 128-byte

@@ -147,7 +147,9 @@ __global__ __launch_bounds__(kThreads) void linear_step_kernel(StepArgs a) {
   }
 }
 
-// States of a sequence in a layer, copied, at HBM's rate: a workgroup per (pair, layer, 16 KB).
+// States of a sequence in a layer, copied: a workgroup per (pair, layer, 16 KB).  A source is read for each of its copies: 8 sequences
+// to 56, 32 layers of 8 heads, 316 us, 1.88 GB at 5.9 TB/s; 16 to 48, 4 layers, 25 us, 201 MB at 8.0 TB/s, for the sources of 34 MB
+// stay in caches.
 constexpr int kCopy = 4;                               // float4 of a thread
 __global__ __launch_bounds__(kThreads) void state_fork_kernel(ForkArgs a) {
   const int64_t at = (int64_t(blockIdx.x) * kThreads * kCopy + threadIdx.x) * 4;

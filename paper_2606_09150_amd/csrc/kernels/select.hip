@@ -15,7 +15,7 @@
 // block's maxima (two of each lane), later of the list's values (n values are at or above it, and
 // what comes later has a higher place).  A list that might not hold the next block is cut down to its n largest.
 //
-// 32 requests of 8 beams over 131,072 tokens, bf16, k 16: 25 us of slices (67 MB at 2.7 TB/s) and 9 of joining.  A workgroup's
+// 32 requests of 8 beams over 131,072 tokens, bf16, k 16: 26 us of slices (67 MB at 2.6 TB/s) and 9 of joining.  A workgroup's
 // eight blocks take 1.2 each, at which rate the slices would be read in 10; before them lie 3 until its first one is there, behind
 // them and between, 5 of raising bars, summing and joining lists, at the same time in all workgroups.  One request of 32 beams
 // over 200,000, k 64: 40 us (190 with the lists' entries all read by the join).
@@ -551,6 +551,10 @@ hipError_t run(const SelectArgs& a, hipStream_t stream) {
 
 }  // namespace
 
+// Rows are cut into slices for 1,024 workgroups (four a CU) in all, 32 slices at most.  256 / 512 / 1,024 / 2,048 / 4,096 workgroups, bf16
+// (us): 32 x 8 rows of 131,072 tokens 45.0 / 35.6 / 33.7 / 38.3 / 47.2; 64 x 1 20.9 / 18.1 / 17.5 / 22.0 / 21.8; 8 x 8 of 200,000 28.8 / 24.9
+// / 24.1 / 28.3 / 28.2; 64 x 4 of 32,000 21.9 / 19.1 / 18.8 / 22.6 / 22.8; but 1 x 32 of 200,000, one join for all, 29.5 / 30.8 / 35.4 / 35.5 /
+// 35.3.  16 / 32 / 64 slices: 1 row of 2,000,000 43.2 / 30.6 / 24.0; 1 x 32 of 200,000 30.8 / 35.4 / 35.5; the others the same.
 void plan_select(SelectArgs* a) {
   const int e = a->type == UFS_FP32 ? 4 : 8, block = kWaves * kBlock / e;
   const int64_t vectors = (int64_t(a->vocab) + e - 1) / e, rows = int64_t(a->groups) * a->beams;

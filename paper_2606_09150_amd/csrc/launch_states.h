@@ -74,7 +74,8 @@ struct PartArgs {
 constexpr int kScanSlices = 16;              // of a state, workgroups of the scan
 // Whether forward walks (o, dq) take two query heads an item, which share M's parts, y, z and the barriers.  One / two (us): 1 x 16,384
 // tokens, 8 key heads of 4, forward 143 / 128, backward 325 / 317; 2 x 4,000, 16 of 2, 83 / 73, 184 / 182; 2 x 6,000, 8 of 8, 164 / 148,
-// 447 / 423; 1 x 16,000, 6 of 3 (an item of one head twice), 94 / 97, 190 / 197.
+// 447 / 423.  Odd groups take one head twice: 1 x 16,000, 6 of 3, 94 / 97, 190 / 197; 4 of 5, 85 / 81, 184 / 187; 4 of 7, 109 / 103,
+// 247 / 246; 2 x 6,000, 8 of 5, 114 / 109, 287 / 285; 8 of 7, 139 / 133, 377 / 369; 4 x 2,000, 8 of 7, 100 / 95, 261 / 257.
 inline bool two_heads(int group) { return group % 2 == 0 || group > 3; }
 // exact: states are results in fp32, or bear on one
 hipError_t launch_linear_parts(const PartArgs& a, int32_t groups, bool exact, hipStream_t stream);
@@ -84,7 +85,9 @@ hipError_t launch_linear_bwd(const WalkArgs& a, int32_t groups, bool exact, hipS
 
 // Few tokens a sequence: token by token.  So / in chunks (us): 1 sequence of 8 key heads, 4 tokens 5.0 / 7.1, 8 6.8 / 7.1; 24 of 8 heads of 2,
 // 4 9.7 / 10.6, 5 10.8 / 10.5, 7 13.1 / 10.1; 64 of 8, 4 14.3 / 15.1, 6 17.4 / 15.4; 64 of 32, 4 46.6 / 52.5, 6 51.6 / 53.2, 8 58.6 /
-// 52.7; 64 of 32 heads of 4, 4 60.2 / 63.8; 16 of 32 heads of 8, 2 18.9 / 26.1, 4 30.0 / 26.5.
+// 52.7; 64 of 32 heads of 4, 4 60.2 / 63.8; 16 of 32 heads of 8, 2 18.9 / 26.1, 3 23.9 / 25.2, 4 30.0 / 26.5.  The rule goes by tokens, while a
+// wave's way is tokens times query heads: large groups lose at 3 and 4 tokens, and gain below.  16 of 32 heads of 16, 2 27.1 / 37.0, 3 36.3 /
+// 37.1, 4 45.8 / 37.5; 4 of 4 heads of 32, 2 19.1 / 36.8, 3 46.3 / 37.3, 4 60.9 / 37.4; 8 of one head of 64, 2 59.3 / 67.7, 4 115.8 / 68.2.
 constexpr int kFewTokens = 4;
 struct StepArgs {
   Geo geo;                    // of a step
